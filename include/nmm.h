@@ -443,6 +443,74 @@ typedef struct {
 nmm_status nmm_mla_decode_step(const nmm_mla_chain* chain, const nmm_latent_attn* attn, void* workspace,
                                size_t workspace_bytes, void* stream);
 
+/*
+ * The latent cache of a batch: rows addressed one by one (a paged pool), in one of two formats.
+ *
+ *   NMM_CACHE_BF16  row = kv_lora latents and rope values, bf16: the rows nmm_mla_kv_update writes
+ *   NMM_CACHE_E4M3  row = kv_lora e4m3 codes | 16 scale bytes | rope values in bf16.  Latents
+ *                   32 b .. 32 b + 31 share scale byte b: code c stands for e4m3(c) * 2^(byte - 127).
+ *                   656 bytes at kv_lora 512, rope 64, against 1152.
+ *
+ *   data     16-byte aligned; row r starts at data + r * ld, ld in BYTES, a multiple of 16 and at least
+ *            nmm_latent_cache_row_bytes(format, kv_lora, rope).  Offsets are 64-bit: a pool may be of any size.
+ *   rows     rows of the pool, < 2^31.
+ *   kv_lora  a multiple of 32 in [32, 512];   rope  a multiple of 8 in [0, 64].
+ */
+typedef enum { NMM_CACHE_BF16 = 1, NMM_CACHE_E4M3 = 2 } nmm_cache_format;
+
+typedef struct {
+    void* data;
+    int64_t rows, ld;
+    int64_t kv_lora, rope;
+    nmm_cache_format format;
+} nmm_latent_cache;
+
+size_t nmm_latent_cache_row_bytes(nmm_cache_format format, int64_t kv_lora, int64_t rope);
+
+/*
+ * nmm_latent_cache_write -- the cache rows of many tokens in one launch (a decode batch, a prefill
+ * chunk, rows converted from another cache).  For t < tokens with 0 <= slots[t] < cache->rows:
+ *   c, k         = src[t, :kv_lora], src[t, kv_lora : kv_lora + rope]     fp32 or bf16
+ *   c            = c / sqrt(mean(c^2) + eps) * gamma                      where gamma is given
+ *   k            = RoPE(k, positions[t])                                  where positions is given
+ *   row slots[t] = bf16([c | k]), in 8-bit rows the bf16 latents quantised
+ * RMSNorm and RoPE as in nmm_mla_kv_update (rounded to nearest, ties to even); src is a product of
+ * nmm_gemv with M tokens, say.  Quantising: per 32 latents the least e >= -117 with every finite
+ * |value| <= 448 * 2^e, and code = value * 2^-e rounded to e4m3 (nearest, ties to even), so nothing
+ * saturates and what a row stands for is a bf16 number (magnitudes from 1.9375 * 2^127 on round to 2^128, which
+ * reads as infinity).  Values that are not finite are kept as NaN.
+ * A slot outside the pool (-1 for a padded token) is skipped.  Slots of one call must differ: two
+ * tokens of one slot leave that row, and no other, undefined.  src may not overlap the rows written.
+ *   src, ld_src  16-byte aligned, ld_src >= kv_lora + rope a multiple of 16 bytes (elements).
+ *   slots        [tokens], positions [tokens] or NULL: int64 on the device; positions in [0, 2^31).
+ *   gamma        [kv_lora] bf16, 16-byte aligned, or NULL.
+ *   eps          finite, >= 0 (with gamma).   rope_theta  finite, > 0 (with positions).
+ * Needs no workspace.
+ */
+typedef enum { NMM_SRC_F32 = 0, NMM_SRC_BF16 = 1 } nmm_src_type;
+
+typedef struct {
+    int64_t tokens;
+    const void* src;
+    nmm_src_type src_type;
+    int64_t ld_src;
+    const int64_t* slots;
+    const void* gamma;
+    float eps;
+    const int64_t* positions;
+    float rope_theta;
+} nmm_cache_entries;
+
+nmm_status nmm_latent_cache_write(const nmm_latent_cache* cache, const nmm_cache_entries* entries, void* stream);
+
+/*
+ * nmm_latent_cache_read -- out[t, :kv_lora + rope] = what row slots[t] stands for, bf16 (exact), for
+ * t < tokens.  A slot outside the pool leaves its row of out as it was; a slot may be named any
+ * number of times.  out 16-byte aligned, ldo >= kv_lora + rope a multiple of 8 (elements).
+ */
+nmm_status nmm_latent_cache_read(const nmm_latent_cache* cache, int64_t tokens, const int64_t* slots, void* out,
+                                 int64_t ldo, void* stream);
+
 /* Workspace sizes in bytes (0 when none is needed; never fails: invalid sizes give 0). */
 size_t nmm_gemv_workspace_size(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_path path);
 size_t nmm_batched_gemv_workspace_size(int64_t batch, int64_t M, int64_t K, int64_t N,

@@ -22,6 +22,8 @@ NMM_OK, NMM_ERR_NULL, NMM_ERR_SHAPE, NMM_ERR_DTYPE, NMM_ERR_ALIGN, NMM_ERR_WORKS
 NMM_F16, NMM_BF16 = 1, 2
 NMM_PATH_AUTO, NMM_PATH_GEMV, NMM_PATH_MFMA = 0, 1, 2
 NMM_ROUND_EVEN, NMM_ROUND_AWAY = 0, 1
+NMM_CACHE_BF16, NMM_CACHE_E4M3 = 1, 2
+NMM_SRC_F32, NMM_SRC_BF16 = 0, 1
 NMM_NOALLOC_SCRATCH_BYTES = 8 << 20   # nmm_gemv_noalloc's scratch per GPU
 
 _i64 = ctypes.c_int64
@@ -81,6 +83,15 @@ class nmm_mla_query_path(ctypes.Structure):
                [(n, _p) for n in ("down_f32", "cq_bf16", "q_f32", "q_bf16", "qlat_f32", "query")] + [("ldq", _i64)]
 
 
+class nmm_latent_cache(ctypes.Structure):
+    _fields_ = [("data", _p), ("rows", _i64), ("ld", _i64), ("kv_lora", _i64), ("rope", _i64), ("format", ctypes.c_int)]
+
+
+class nmm_cache_entries(ctypes.Structure):
+    _fields_ = [("tokens", _i64), ("src", _p), ("src_type", ctypes.c_int), ("ld_src", _i64), ("slots", _p), ("gamma", _p),
+                ("eps", ctypes.c_float), ("positions", _p), ("rope_theta", ctypes.c_float)]
+
+
 EXPORTS = {
     "nmm_gemv": (ctypes.c_int, [_i64, _i64, _i64, ctypes.c_int, _p, _i64, _p, _i64, _p, _i64,
                                 ctypes.c_int, _p, _sz, _p]),
@@ -111,6 +122,9 @@ EXPORTS = {
     "nmm_mla_decode_step_workspace_size": (_sz, [ctypes.POINTER(nmm_mla_chain), ctypes.POINTER(nmm_latent_attn)]),
     "nmm_latent_attention": (ctypes.c_int, [_i64, _i64, _i64, _i64, _p, _i64, _p, _i64,
                                             ctypes.c_float, _p, _i64, _p, _sz, _p]),
+    "nmm_latent_cache_row_bytes": (_sz, [ctypes.c_int, _i64, _i64]),
+    "nmm_latent_cache_write": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), ctypes.POINTER(nmm_cache_entries), _p]),
+    "nmm_latent_cache_read": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), _i64, _p, _p, _i64, _p]),
     "nmm_gemv_workspace_size": (_sz, [_i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_batched_gemv_workspace_size": (_sz, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_mla_decode_chain_workspace_size": (_sz, [ctypes.POINTER(nmm_mla_chain)]),
@@ -608,6 +622,78 @@ def nmm_latent_attention_ex(q: torch.Tensor, kv: torch.Tensor, out: torch.Tensor
           (heads, seq, d_qk, d_v, q.data_ptr(), _ld(q), kv.data_ptr(), _ld(kv), float(scale), out.data_ptr(), _ld(out),
            out_bf16.data_ptr() if out_bf16 is not None else None, _ld(out_bf16) if out_bf16 is not None else 0,
            int(splits)), workspace, q.device, stream)
+    return out
+
+
+def _same_device(where: str, *tensors) -> None:
+    """Every tensor on the current device: the library launches there and reads plain pointers."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.get_device() == dev):
+            raise ValueError(f"{where}: every tensor must be on the current device (cuda:{dev}), one is on {t.device}")
+
+
+def _index(where: str, t: torch.Tensor, dtype: torch.dtype, n: int) -> int:
+    """The address of n contiguous indices."""
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{where}: indices must be a contiguous {dtype} vector of at least {n}")
+    return t.data_ptr()
+
+
+def nmm_latent_cache_row_bytes(kv_lora: int, rope: int, format: int = NMM_CACHE_E4M3) -> int:
+    """Bytes of one latent-cache row (0 for sizes that no cache has)."""
+    return int(lib().nmm_latent_cache_row_bytes(format, kv_lora, rope))
+
+
+def _cache_struct(cache: torch.Tensor, kv_lora: int, rope: int) -> nmm_latent_cache:
+    """The pool [rows, >= row] of a tensor: uint8 for 8-bit rows (in bytes), bfloat16 for bf16 ones."""
+    if cache.dim() != 2 or cache.dtype not in (torch.uint8, torch.bfloat16):
+        raise TypeError("a latent cache is a 2-D uint8 (8-bit rows) or bfloat16 tensor")
+    c = nmm_latent_cache()
+    c.data, c.rows, c.ld = cache.data_ptr(), cache.shape[0], _ld(cache) * cache.element_size()
+    c.kv_lora, c.rope = int(kv_lora), int(rope)
+    c.format = NMM_CACHE_E4M3 if cache.dtype == torch.uint8 else NMM_CACHE_BF16
+    if cache.shape[1] * cache.element_size() < nmm_latent_cache_row_bytes(kv_lora, rope, c.format):
+        raise ValueError("the cache's rows are shorter than its format's")
+    return c
+
+
+def nmm_latent_cache_write(src: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor, *, kv_lora: int, rope: int,
+                           gamma: torch.Tensor | None = None, eps: float = 0.0, positions: torch.Tensor | None = None,
+                           theta: float = 10000.0, stream=None) -> torch.Tensor:
+    """cache[slots[t]] = [RMSNorm(src[t, :kv_lora]) * gamma | RoPE(src[t, kv_lora:], positions[t])], rounded to bf16
+    and, where the cache is uint8, its latents to 8 bits.  src [tokens, >= kv_lora + rope] fp32 or bf16; slots and
+    positions int64 [tokens]; without gamma no RMSNorm, without positions no RoPE.  A slot outside the cache is skipped."""
+    _same_device("nmm_latent_cache_write", src, slots, cache, gamma, positions)
+    if src.dim() != 2 or src.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("src must be a 2-D float32 or bfloat16 tensor")
+    if src.shape[1] < kv_lora + rope:
+        raise ValueError("src's rows are shorter than kv_lora + rope")
+    if gamma is not None and (gamma.dtype != torch.bfloat16 or gamma.shape != (kv_lora,) or gamma.stride(0) != 1):
+        raise ValueError("gamma must be a contiguous bfloat16 vector of kv_lora values")
+    n = src.shape[0]
+    e = nmm_cache_entries()
+    e.tokens, e.src, e.ld_src = n, src.data_ptr(), _ld(src)
+    e.src_type = NMM_SRC_F32 if src.dtype == torch.float32 else NMM_SRC_BF16
+    e.slots = _index("slots", slots, torch.int64, n)
+    e.gamma, e.eps = gamma.data_ptr() if gamma is not None else None, float(eps)
+    e.positions = _index("positions", positions, torch.int64, n) if positions is not None else None
+    e.rope_theta = float(theta)
+    _check(lib().nmm_latent_cache_write(ctypes.byref(_cache_struct(cache, kv_lora, rope)), ctypes.byref(e),
+                                        _stream(stream)), "nmm_latent_cache_write")
+    return cache
+
+
+def nmm_latent_cache_read(cache: torch.Tensor, slots: torch.Tensor, out: torch.Tensor, *, kv_lora: int, rope: int,
+                          stream=None) -> torch.Tensor:
+    """out[t, :kv_lora + rope] = what cache row slots[t] stands for (bf16); a slot outside the cache leaves its row."""
+    _same_device("nmm_latent_cache_read", cache, slots, out)
+    if out.dim() != 2 or out.dtype != torch.bfloat16 or out.shape[1] < kv_lora + rope:
+        raise ValueError("out must be a bfloat16 tensor [tokens, >= kv_lora + rope]")
+    n = out.shape[0]
+    _check(lib().nmm_latent_cache_read(ctypes.byref(_cache_struct(cache, kv_lora, rope)), n,
+                                       _index("slots", slots, torch.int64, n), out.data_ptr(), _ld(out),
+                                       _stream(stream)), "nmm_latent_cache_read")
     return out
 
 
