@@ -511,6 +511,56 @@ nmm_status nmm_latent_cache_write(const nmm_latent_cache* cache, const nmm_cache
 nmm_status nmm_latent_cache_read(const nmm_latent_cache* cache, int64_t tokens, const int64_t* slots, void* out,
                                  int64_t ldo, void* stream);
 
+/*
+ * nmm_latent_attention_batch -- latent attention of a decode batch over a paged cache whose sequences
+ * share a prefix.  For sequence b < batch, token t < tokens of this step and head h < heads:
+ *     out[b, t, h] = sum_j softmax_j(scale * q[b, t, h] . k_j) v_j
+ * over the prefix's positions 0 .. prefix_len - 1 and the sequence's own positions 0 .. n - 1 with
+ * n = lens[b] - (tokens - 1 - t): lens[b] counts this step's tokens, whose rows are in the cache already, and
+ * a token sees those up to its own.  k_j is a cache row's kv_lora + rope values, v_j its kv_lora latents.
+ * Prefix position j is row j % page_size of page prefix_pages[j / page_size], own position j of
+ * sequence b of page pages[b * ld_pages + j / page_size]; page i of the pool is its rows
+ * i * page_size and on.  The prefix is computed once for all rows (b, t, h), not once per sequence.
+ *
+ * Scores, softmax and sums are fp32; probabilities are rounded to bf16 for the product with v and out is
+ * rounded to bf16 (nearest, ties to even), the operand of the per-head W_UV that follows.
+ *   batch, tokens, heads  >= 0, batch * tokens * heads < 2^24 (0: nothing to do).
+ *   q     bf16, q[b * stride_qb + t * stride_qt + h * ldq + d], d < kv_lora + rope: latent part, then RoPE's,
+ *         as nmm_mla_query makes it; 16-byte aligned, strides and ldq >= kv_lora + rope multiples of 8.
+ *   cache the pool in either format.  Rows past a length are never read; a row below it that holds NaN or
+ *         infinity spoils every token of its sequence, whether the token sees it or not.
+ *   page_size     a power of two up to 65536.
+ *   prefix_pages  int32 [ceil(prefix_len / page_size)] on the device (unused where prefix_len is 0).
+ *   pages, lens   int32 [batch, ld_pages] and [batch] on the device, ld_pages >= ceil(max_len / page_size);
+ *                 unused where max_len is 0.  Entries past a sequence's length are not read.
+ *   max_len       what the launch is planned for: lens[b] above it counts as max_len, below 0 as 0.
+ *                 The plan does not look at lens, so a captured call follows them as they change.
+ *   out   bf16, out[b * stride_ob + t * stride_ot + h * ldo + c], c < kv_lora; 8-byte aligned, strides
+ *         and ldo >= kv_lora multiples of 4.
+ * Positions on a page outside the pool are left out; a row that sees no position gives zeros.  Results are
+ * deterministic.  Workspace: nmm_latent_attention_batch_workspace_size.
+ */
+typedef struct {
+    int64_t batch, tokens, heads;
+    const void* q;
+    int64_t stride_qb, stride_qt, ldq;
+    nmm_latent_cache cache;
+    int64_t page_size;
+    const int32_t* prefix_pages;
+    int64_t prefix_len;
+    const int32_t* pages;
+    int64_t ld_pages;
+    const int32_t* lens;
+    int64_t max_len;
+    float scale;
+    void* out;
+    int64_t stride_ob, stride_ot, ldo;
+} nmm_latent_attn_batch;
+
+nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* workspace, size_t workspace_bytes,
+                                      void* stream);
+size_t nmm_latent_attention_batch_workspace_size(const nmm_latent_attn_batch* attn);
+
 /* Workspace sizes in bytes (0 when none is needed; never fails: invalid sizes give 0). */
 size_t nmm_gemv_workspace_size(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_path path);
 size_t nmm_batched_gemv_workspace_size(int64_t batch, int64_t M, int64_t K, int64_t N,

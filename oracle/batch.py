@@ -89,7 +89,8 @@ def dequantise_rows(data, kv: int, rope: int) -> np.ndarray:
     return np.concatenate((v.reshape(len(data), kv), k.reshape(len(data), rope)), 1)
 
 
-def attention_batch(q, rows, scale: float, kv: int, page: int, pages, lens, prefix_pages=(), prefix_len: int = 0):
+def attention_batch(q, rows, scale: float, kv: int, page: int, pages, lens, max_len: int, prefix_pages=(),
+                    prefix_len: int = 0):
     """out [B, T, H, kv] and sum_j p_j |v_j| of q [B, T, H, d] over cache rows [n, d] (fp64 values).  Positions
     on a page outside the pool do not exist; a row with no position gives zeros."""
     q = np.asarray(q, dtype=np.float64)
@@ -105,10 +106,10 @@ def attention_batch(q, rows, scale: float, kv: int, page: int, pages, lens, pref
 
     _, shared = locate(prefix_pages, prefix_len)
     for b in range(B):
-        n = min(max(0, int(lens[b])), len(pages[b]) * page)
+        n = min(max(0, int(lens[b])), max_len)
         _, mine = locate(pages[b], n)
         for t in range(T):
-            at = np.concatenate((shared, mine[:max(0, int(lens[b]) - (T - 1 - t))]))
+            at = np.concatenate((shared, mine[:max(0, n - (T - 1 - t))]))
             at = at[at >= 0]
             if len(at) == 0:
                 continue

@@ -92,6 +92,13 @@ class nmm_cache_entries(ctypes.Structure):
                 ("eps", ctypes.c_float), ("positions", _p), ("rope_theta", ctypes.c_float)]
 
 
+class nmm_latent_attn_batch(ctypes.Structure):
+    _fields_ = [("batch", _i64), ("tokens", _i64), ("heads", _i64), ("q", _p), ("stride_qb", _i64), ("stride_qt", _i64),
+                ("ldq", _i64), ("cache", nmm_latent_cache), ("page_size", _i64), ("prefix_pages", _p),
+                ("prefix_len", _i64), ("pages", _p), ("ld_pages", _i64), ("lens", _p), ("max_len", _i64),
+                ("scale", ctypes.c_float), ("out", _p), ("stride_ob", _i64), ("stride_ot", _i64), ("ldo", _i64)]
+
+
 EXPORTS = {
     "nmm_gemv": (ctypes.c_int, [_i64, _i64, _i64, ctypes.c_int, _p, _i64, _p, _i64, _p, _i64,
                                 ctypes.c_int, _p, _sz, _p]),
@@ -125,6 +132,8 @@ EXPORTS = {
     "nmm_latent_cache_row_bytes": (_sz, [ctypes.c_int, _i64, _i64]),
     "nmm_latent_cache_write": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), ctypes.POINTER(nmm_cache_entries), _p]),
     "nmm_latent_cache_read": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), _i64, _p, _p, _i64, _p]),
+    "nmm_latent_attention_batch": (ctypes.c_int, [ctypes.POINTER(nmm_latent_attn_batch), _p, _sz, _p]),
+    "nmm_latent_attention_batch_workspace_size": (_sz, [ctypes.POINTER(nmm_latent_attn_batch)]),
     "nmm_gemv_workspace_size": (_sz, [_i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_batched_gemv_workspace_size": (_sz, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_mla_decode_chain_workspace_size": (_sz, [ctypes.POINTER(nmm_mla_chain)]),
@@ -694,6 +703,47 @@ def nmm_latent_cache_read(cache: torch.Tensor, slots: torch.Tensor, out: torch.T
     _check(lib().nmm_latent_cache_read(ctypes.byref(_cache_struct(cache, kv_lora, rope)), n,
                                        _index("slots", slots, torch.int64, n), out.data_ptr(), _ld(out),
                                        _stream(stream)), "nmm_latent_cache_read")
+    return out
+
+
+def nmm_latent_attention_batch(q: torch.Tensor, cache: torch.Tensor, out: torch.Tensor, scale: float, *, kv_lora: int,
+                               rope: int, page_size: int, pages: torch.Tensor | None = None,
+                               lens: torch.Tensor | None = None, max_len: int = 0,
+                               prefix_pages: torch.Tensor | None = None, prefix_len: int = 0, workspace=None,
+                               stream=None) -> torch.Tensor:
+    """out[b, t, h] = attention of query q[b, t, h] over the shared prefix and sequence b's own cache rows, up to
+    token t's (see nmm.h).  q [batch, (tokens,) heads, >= kv_lora + rope] and out [batch, (tokens,) heads, >= kv_lora]
+    bf16; cache [rows, ...] uint8 (8-bit rows) or bf16 in pages of page_size rows; pages int32 [batch, >= pages of
+    max_len], lens int32 [batch] (this step's tokens counted), prefix_pages int32."""
+    _same_device("nmm_latent_attention_batch", q, cache, out, pages, lens, prefix_pages)
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.dim() not in (3, 4) or out.dim() != q.dim():
+        raise TypeError("q and out must be bfloat16 tensors [batch, (tokens,) heads, width]")
+    if out.shape[:-1] != q.shape[:-1] or q.shape[-1] < kv_lora + rope or out.shape[-1] < kv_lora:
+        raise ValueError("q and out must have the same batch, tokens and heads, and rows of kv_lora + rope and kv_lora")
+    a = nmm_latent_attn_batch()
+    a.batch, a.tokens, a.heads = q.shape[0], q.shape[1] if q.dim() == 4 else 1, q.shape[-2]
+    a.q, a.stride_qb, a.stride_qt, a.ldq = q.data_ptr(), q.stride(0), q.stride(1) if q.dim() == 4 else 0, _ld(q)
+    a.cache, a.page_size = _cache_struct(cache, kv_lora, rope), int(page_size)
+    if prefix_len > 0:
+        if prefix_pages is None:
+            raise ValueError("prefix_pages: a prefix needs its pages")
+        a.prefix_pages = _index("prefix_pages", prefix_pages, torch.int32, -(-prefix_len // max(1, page_size)))
+    a.prefix_len, a.max_len = int(prefix_len), int(max_len)
+    if max_len > 0:
+        if pages is None or pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] < a.batch or \
+                pages.shape[1] * page_size < max_len or (pages.shape[1] > 1 and pages.stride(1) != 1):
+            raise ValueError("pages must be an int32 tensor [batch, >= pages of max_len], its last dimension contiguous")
+        if lens is None:
+            raise ValueError("lens: sequences need their lengths")
+        a.pages, a.ld_pages = pages.data_ptr(), max(pages.stride(0), pages.shape[1])
+        if a.batch > 1 and pages.stride(0) < pages.shape[1]:
+            raise ValueError("pages: rows may not overlap")
+        a.lens = _index("lens", lens, torch.int32, a.batch)
+    a.scale = float(scale)
+    a.out, a.stride_ob, a.stride_ot, a.ldo = out.data_ptr(), out.stride(0), out.stride(1) if q.dim() == 4 else 0, _ld(out)
+    L, ref = lib(), ctypes.byref(a)
+    _call(L.nmm_latent_attention_batch, "nmm_latent_attention_batch",
+          lambda: L.nmm_latent_attention_batch_workspace_size(ref), (ref,), workspace, q.device, stream)
     return out
 
 

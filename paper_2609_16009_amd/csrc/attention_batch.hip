@@ -1,0 +1,730 @@
+// Latent attention of a decode batch over a paged cache whose sequences share a prefix (gfx950).
+//
+//   row r = (b T + t) H + h:   out_r = sum_j p_j v_j,  p = softmax_j(scale * q_r . k_j)
+//   over the prefix's positions, shared by every row, and positions j < lens[b] - (T - 1 - t) of sequence b
+//
+// The prefix's keys are the same for every row, so it is one attention of all B T H rows over one cache,
+// taken in tiles of 64 rows: its cache rows are read once per tile, where a pass per sequence would read
+// them for each.  A sequence's own positions are attended by its T H rows in tiles of 16, 32 or 64.  Both
+// kinds of tile are cut into spans of positions so that their workgroups fill the chip, run in one launch, and
+// leave (reference, sum, unnormalised output) partials which a merge launch joins in a fixed order.
+//
+// One workgroup (4 waves) takes a tile of 16 HT rows over a span, in chunks of 64 positions:
+//  * Staging.  A chunk's rows lie in LDS as bf16, [9 column blocks][64 rows][8 pieces of 16 bytes]: the latents'
+//    eight blocks of 64 columns, then RoPE's (columns that the cache lacks are zeros).  Piece c of row r sits in
+//    slot c ^ f(r), which keeps the key reads (8 rows, one column) and the transposed value reads (4 rows, 2 pieces)
+//    free of bank conflicts.  bf16 rows come by LDS-direct loads of 8 rows x 128 bytes; 8-bit rows come into
+//    registers a chunk ahead and are widened on their way to LDS (exact: a power of two per 32 values).  A wave's
+//    lanes look up one position's cache row each; rows that do not exist (past the end, on a page outside the
+//    pool) read a row of zeros and are masked.
+//  * S^T = K Q^T, 16 positions a wave, Q in registers as fragments; P = 2^(s - reference), the
+//    reference moved only when a chunk exceeds it by 2^8; O^T = V^T P^T, a quarter of the columns a wave.
+//    Scores, sums and outputs are fp32; P is rounded to bf16 for the matrix cores (2^-9 relative, where the output
+//    itself is rounded to bf16) and summed before its rounding.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "attention_core.h"
+#include "bf16_cast.h"
+#include "latent_row.h"
+#include "nmm_internal.h"
+
+namespace nmm {
+namespace {
+
+using attn::as_bf16x8;
+using attn::bf16x4;
+using attn::cols4_max;
+using attn::cols4_sum;
+using attn::f32x4;
+using attn::i32x4;
+using attn::lds_bf16x4;
+using attn::lds_sync;
+using attn::lds_void;
+using attn::pack_bf16;
+using attn::wave_max;
+using attn::wave_sum;
+
+constexpr int kWavesB = 4, kThreadsB = 64 * kWavesB;
+constexpr int kChunk = 64;                             // positions per chunk, rows of the largest tile
+constexpr int kBlocks = 9;                             // column blocks of 64: 8 of latents, 1 of RoPE
+constexpr int kBlockElems = kChunk * 64;               // elements of one column block of a chunk
+constexpr int kSteps = 2 * kBlocks;                    // k-steps of 32 columns
+constexpr int kTilesW = 8;                             // 16-column output tiles per wave
+constexpr int kPPitchB = kChunk + 8;
+constexpr int kAhead = 6;                              // K fragments in flight
+constexpr float kLazy = 8.f;
+constexpr int kMaxSlots = 64;                          // partials of a row: one lane of a wave each
+
+struct BatchParams {
+    const uint16_t* q;
+    int64_t sqb, sqt, ldq;
+    const uint8_t* cache;
+    int64_t ld;
+    int kv, rope;
+    int page_shift, n_pages;
+    const int32_t* prefix_pages;
+    int prefix_len;
+    const int32_t* pages;
+    int64_t ld_pages;
+    const int32_t* lens;
+    int max_len;
+    float scale_log2;
+    uint16_t* out;
+    int64_t sob, sot, ldo;
+    float* part_o;           // [slots][rows][kv]
+    float* part_ml;          // [slots][rows][2]
+    int B, T, H, rows;
+    int pre_tiles, pre_spans, pre_span, pre_items, pre_wide, pre_xcd;
+    int own_tiles, own_spans, own_span;
+    int direct;              // one slot: rows go straight to out
+};
+
+// Cache rows that do not exist read zeros here.
+__device__ __attribute__((aligned(128))) const uint8_t g_zero_row[2 * (kLatentMax + kLatentRopeMax)] = {};
+
+struct Item {
+    int r0, nrows;           // first row and rows of the tile
+    int seq;                 // sequence of an own item, -1: the prefix
+    const int32_t* table;
+    int begin, end;          // positions of the span (end <= the length)
+    int len;                 // own length of the sequence
+    int slot;
+};
+
+// Global memory, said so: a pointer that may also be the zero row's would otherwise be read by flat loads, which
+// count as LDS operations too.
+typedef const __attribute__((address_space(1))) uint8_t* gbytes;
+__device__ __forceinline__ uint4 load16(gbytes p) {
+    typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+    const u32x4_t v = *(const __attribute__((address_space(1))) u32x4_t*)p;
+    return uint4{v[0], v[1], v[2], v[3]};
+}
+// The zero row's address, its contents unknown to the compiler: knowing them it splits every select between
+// a cache row and this one into branches.
+__device__ __forceinline__ gbytes opaque_zero_row() {
+    gbytes z = (gbytes)g_zero_row;
+    asm("" : "+s"(z));
+    return z;
+}
+
+__device__ __forceinline__ int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+
+__device__ __forceinline__ int64_t row_offset(int r, int T, int H, int64_t sb, int64_t st, int64_t ld) {
+    const int bt = r / H, h = r - bt * H;
+    const int b = bt / T, t = bt - b * T;
+    return int64_t(b) * sb + int64_t(t) * st + int64_t(h) * ld;
+}
+
+// One (tile, span).  kv_a, kv_b: chunk buffers; pbuf: P [16 HT][kPPitchB]; red: [4][16 HT].
+template <int HT, bool E4M3>
+__device__ __forceinline__ void batch_block(const BatchParams& p, const Item it, uint16_t* const kv_a, uint16_t* const kv_b,
+                                            uint16_t* const pbuf, float* const red, int* const flags) {
+    constexpr int HB = 16 * HT;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int pw = __builtin_amdgcn_readfirstlane(tid >> 6) & (kWavesB - 1);
+    const int g = lane >> 4, j = lane & 15;
+    const int nchunks = (it.end - it.begin + kChunk - 1) / kChunk;
+    const gbytes cache = (gbytes)p.cache;
+    const gbytes zero_row = opaque_zero_row();
+
+    // ---- staging.  Cache row of position c0 + lane, or -1
+    auto row_of = [&](int c0) {
+        const int pos = c0 + lane;
+        int r = -1;
+        if (pos < it.end) {
+            const int page = it.table[pos >> p.page_shift];
+            if (page >= 0 && page < p.n_pages) r = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+        }
+        return r;
+    };
+    auto ptr_of = [&](int rows, int row) {
+        const int r = __builtin_amdgcn_ds_bpermute(row << 2, rows);
+        return r < 0 ? zero_row : cache + int64_t(r) * p.ld;
+    };
+    // 8 rows x 128 bytes per LDS-direct load; the wave's rows are 16 pw .. 16 pw + 15
+    const int c_st = (lane & 7) ^ swz(lane >> 3);
+    auto stage_bf16 = [&](gbytes row_ptr, uint16_t* buf, int cb, int half) {
+        const bool has = cb < 8 ? 64 * cb + 8 * c_st < p.kv : 8 * c_st < p.rope;
+        const gbytes src = has ? row_ptr + (cb < 8 ? cb * 128 : 2 * p.kv) + c_st * 16 : zero_row;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                         (lds_void*)(buf + cb * kBlockElems + (16 * pw + 8 * half) * 64), 16, 0, 0);
+    };
+    // 8-bit rows: a thread takes pieces 8 i + (tid & 7) of 16 codes of rows tid / 8 and tid / 8 + 32, a scale
+    // row and one piece of RoPE
+    struct Raw {
+        uint4 code[2][4], scale[2], rope[2];
+    };
+    auto load_raw = [&](Raw& w, int rows) {
+#pragma unroll
+        for (int ps = 0; ps < 2; ++ps) {
+            const gbytes src = ptr_of(rows, (tid >> 3) + 32 * ps);
+            const int l = tid & 7;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = 16 * (l + 8 * i);
+                w.code[ps][i] = load16((c < p.kv ? src : zero_row) + c);
+            }
+            w.scale[ps] = load16(src + p.kv);
+            w.rope[ps] = load16(8 * l < p.rope ? src + p.kv + kScaleBytes + 16 * l : zero_row);
+        }
+    };
+    auto commit_raw = [&](const Raw& w, uint16_t* buf) {
+#pragma unroll
+        for (int ps = 0; ps < 2; ++ps) {
+            const int row = (tid >> 3) + 32 * ps, l = tid & 7, f = swz(row);
+            const uint32_t sc[4] = {w.scale[ps].x, w.scale[ps].y, w.scale[ps].z, w.scale[ps].w};
+            const int hi = l >> 2;
+            uint16_t* const dst = buf + row * 64;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // piece l + 8 i: column block 2 i + l / 4, pieces 2 (l % 4) and + 1 of it
+                const float s = scale_of(sc[i] >> (8 * (l >> 1)));
+                const uint2 a = dequant4(w.code[ps][i].x, s), b = dequant4(w.code[ps][i].y, s);
+                const uint2 c = dequant4(w.code[ps][i].z, s), d = dequant4(w.code[ps][i].w, s);
+                const uint4 lo{a.x, a.y, b.x, b.y}, up{c.x, c.y, d.x, d.y};
+                uint16_t* const blk = dst + (2 * i + hi) * kBlockElems;
+                const int c0 = 2 * (l & 3);
+                // lanes 4 to 7 write their upper half first: the eight lanes of a row then hit eight slots
+                *reinterpret_cast<uint4*>(blk + (((c0 + hi) ^ f) << 3)) = hi ? up : lo;
+                *reinterpret_cast<uint4*>(blk + (((c0 + 1 - hi) ^ f) << 3)) = hi ? lo : up;
+            }
+            *reinterpret_cast<uint4*>(dst + 8 * kBlockElems + ((l ^ f) << 3)) = w.rope[ps];
+        }
+    };
+
+    // ---- Q rows to buffer b, in the chunk's layout (rows past the tile's and columns past the cache's: zeros)
+    {
+        int64_t qo = -1;
+        if (lane < it.nrows && lane < HB) qo = row_offset(it.r0 + lane, p.T, p.H, p.sqb, p.sqt, p.ldq);
+        for (int ins = pw; ins < 2 * HT * kBlocks; ins += kWavesB) {
+            const int cb = ins / (2 * HT), grp = ins - cb * 2 * HT;
+            const int row = 8 * grp + (lane >> 3);
+            const int c = (lane & 7) ^ swz(row);
+            const uint32_t lo = __builtin_amdgcn_ds_bpermute(row << 2, int(uint32_t(qo)));
+            const uint32_t hi = __builtin_amdgcn_ds_bpermute(row << 2, int(uint32_t(uint64_t(qo) >> 32)));
+            const int64_t o = int64_t((uint64_t(hi) << 32) | lo);
+            const bool ok = o >= 0 && (cb < 8 ? 64 * cb + 8 * c < p.kv : 8 * c < p.rope);
+            const gbytes src = ok ? (gbytes)(p.q + o + (cb < 8 ? 64 * cb : p.kv) + 8 * c) : zero_row;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             (lds_void*)(kv_b + cb * kBlockElems + 8 * grp * 64), 16, 0, 0);
+        }
+    }
+    int rows_cur = row_of(it.begin);
+    Raw raw;
+    if constexpr (E4M3) {
+        load_raw(raw, rows_cur);
+        commit_raw(raw, kv_a);
+    } else {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const gbytes rp = ptr_of(rows_cur, 16 * pw + 8 * half + (lane >> 3));
+#pragma unroll
+            for (int cb = 0; cb < kBlocks; ++cb) stage_bf16(rp, kv_a, cb, half);
+        }
+    }
+    int rows_next = row_of(it.begin + kChunk);
+    __builtin_amdgcn_s_waitcnt(0);
+    lds_sync();
+    // fragment addresses: row j of a 16-row tile, piece 4 (u & 1) + g of column block u / 2
+    const int fj = swz(j);
+    const int fr0 = j * 64 + ((g ^ fj) << 3), fr1 = j * 64 + (((4 + g) ^ fj) << 3);
+    i32x4 qf[HT][kSteps];
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u)
+            qf[t][u] = *reinterpret_cast<const i32x4*>(kv_b + (u >> 1) * kBlockElems + 16 * t * 64 + (u & 1 ? fr1 : fr0));
+    lds_sync();
+
+    // positions that a row sees: those below its limit
+    int limit[HT];
+#pragma unroll
+    for (int t = 0; t < HT; ++t) {
+        limit[t] = it.end;
+        if (it.seq >= 0 && p.T > 1) {
+            const int tok = (it.r0 + 16 * t + j - it.seq * p.T * p.H) / p.H;
+            limit[t] = min(it.end, it.len - (p.T - 1 - tok));
+        }
+    }
+
+    f32x4 o[kTilesW][HT];     // O^T: lane (g, j) holds columns 16 (pw + 4 i) + 4 g .. + 3 of row 16 t + j
+#pragma unroll
+    for (int i = 0; i < kTilesW; ++i)
+#pragma unroll
+        for (int t = 0; t < HT; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_ref[HT], l_acc[HT];
+#pragma unroll
+    for (int t = 0; t < HT; ++t) {
+        m_ref[t] = -INFINITY;
+        l_acc[t] = 0.f;
+    }
+    const int a4 = j >> 2, b4 = j & 3;
+    // value fragments: rows 8 g + a4 and + 4 of a k-step, piece 2 pw + b4 / 2 of column block i
+    const int vrow = 8 * g + a4;
+    const int v_lo = vrow * 64 + (((2 * pw + (b4 >> 1)) ^ swz(a4)) << 3) + 4 * (b4 & 1);
+    const int v_hi = (vrow + 4) * 64 + (((2 * pw + (b4 >> 1)) ^ swz(a4 + 4)) << 3) + 4 * (b4 & 1);
+
+    auto chunk = [&](const uint16_t* cur, uint16_t* nxt, int ck) {
+        const int c0 = it.begin + ck * kChunk;
+        const bool stage_next = ck + 1 < nchunks;
+        const uint64_t present = __builtin_amdgcn_ballot_w64(rows_cur >= 0);
+        gbytes rp[2];
+        if (stage_next) {
+            if constexpr (E4M3) {
+                load_raw(raw, rows_next);
+            } else {
+                rp[0] = ptr_of(rows_next, 16 * pw + (lane >> 3));
+                rp[1] = ptr_of(rows_next, 16 * pw + 8 + (lane >> 3));
+            }
+        }
+        const int rows_after = row_of(c0 + 2 * kChunk);
+
+        // ---- S^T, K fragments read kAhead steps ahead, the next chunk's loads between the steps
+        f32x4 s[HT];
+#pragma unroll
+        for (int t = 0; t < HT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const uint16_t* krow = cur + 16 * pw * 64;
+        auto k_frag = [&](int u) {
+            return *reinterpret_cast<const i32x4*>(krow + (u >> 1) * kBlockElems + (u & 1 ? fr1 : fr0));
+        };
+        i32x4 kf[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) kf[u] = k_frag(u);
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+#pragma unroll
+            for (int t = 0; t < HT; ++t)
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[u % kAhead]), as_bf16x8(qf[t][u]), s[t], 0, 0, 0);
+            if (u + kAhead < kSteps) kf[u % kAhead] = k_frag(u + kAhead);
+            if constexpr (!E4M3) {
+                if (stage_next) stage_bf16(rp[u & 1], nxt, u >> 1, u & 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+
+        // ---- scores in log2 units, masked, and the wave's maximum per row
+        const int at = 16 * pw + 4 * g;
+        const uint32_t here = uint32_t(present >> at);
+        float mx[HT];
+        bool need = false;
+#pragma unroll
+        for (int t = 0; t < HT; ++t) {
+            mx[t] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool seen = ((here >> i) & 1u) && c0 + at + i < limit[t];
+                const float v = seen ? s[t][i] * p.scale_log2 : -INFINITY;
+                s[t][i] = v;
+                mx[t] = fmaxf(mx[t], v);
+            }
+            mx[t] = cols4_max(mx[t]);
+            need |= !(mx[t] <= m_ref[t] + kLazy);
+        }
+        float lc[HT];
+        auto write_p = [&]() {
+#pragma unroll
+            for (int t = 0; t < HT; ++t) {
+                float pv[4];
+                lc[t] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v = s[t][i];
+                    pv[i] = (v == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(v - m_ref[t]);
+                    lc[t] += pv[i];
+                }
+                *reinterpret_cast<uint2*>(pbuf + (16 * t + j) * kPPitchB + at) =
+                    uint2{pack_bf16(pv[0], pv[1]), pack_bf16(pv[2], pv[3])};
+            }
+        };
+        if (g == 0) {
+#pragma unroll
+            for (int t = 0; t < HT; ++t) red[pw * HB + 16 * t + j] = mx[t];
+        }
+        bool any = ck == 0;
+        if (ck > 0) {
+            write_p();
+            const bool wave_needs = __builtin_amdgcn_ballot_w64(need) != 0;
+            if (lane == 0) flags[pw] = wave_needs ? 1 : 0;
+        }
+        lds_sync();
+        if (ck > 0) {
+            const i32x4 f0 = *reinterpret_cast<const i32x4*>(flags);
+            any = (f0[0] | f0[1] | f0[2] | f0[3]) != 0;
+        }
+        // a reference moves (every wave reads the same maxima): the output rescaled, P written again
+        if (any) {
+            bool resc = false;
+            float alpha[HT];
+#pragma unroll
+            for (int t = 0; t < HT; ++t) {
+                const int hh = 16 * t + j;
+                const float mc = fmaxf(fmaxf(red[hh], red[HB + hh]), fmaxf(red[2 * HB + hh], red[3 * HB + hh]));
+                alpha[t] = 1.f;
+                if (mc > m_ref[t] + kLazy) {
+                    alpha[t] = (m_ref[t] == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m_ref[t] - mc);
+                    m_ref[t] = mc;
+                    l_acc[t] *= alpha[t];
+                    resc = true;
+                }
+            }
+            if (__builtin_amdgcn_ballot_w64(resc)) {
+#pragma unroll
+                for (int i = 0; i < kTilesW; ++i)
+#pragma unroll
+                    for (int t = 0; t < HT; ++t) o[i][t] *= alpha[t];
+            }
+            write_p();
+            lds_sync();
+        }
+#pragma unroll
+        for (int t = 0; t < HT; ++t) l_acc[t] += lc[t];
+
+        // ---- O^T += V^T P^T over two steps of 32 positions
+#pragma unroll
+        for (int kk = 0; kk < kChunk / 32; ++kk) {
+            i32x4 pf[HT];
+#pragma unroll
+            for (int t = 0; t < HT; ++t)
+                pf[t] = *reinterpret_cast<const i32x4*>(pbuf + (16 * t + j) * kPPitchB + 32 * kk + 8 * g);
+            i32x4 vf[kTilesW];
+#pragma unroll
+            for (int i = 0; i < kTilesW; ++i) {
+                const uint16_t* base = cur + i * kBlockElems + 32 * kk * 64;
+                const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + v_lo));
+                const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + v_hi));
+                const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
+                vf[i] = i32x4{int(ulo.x), int(ulo.y), int(uhi.x), int(uhi.y)};
+            }
+#pragma unroll
+            for (int i = 0; i < kTilesW; ++i)
+#pragma unroll
+                for (int t = 0; t < HT; ++t)
+                    o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[i]), as_bf16x8(pf[t]), o[i][t], 0, 0, 0);
+        }
+        if constexpr (E4M3) {
+            if (stage_next) commit_raw(raw, nxt);
+        }
+        rows_cur = rows_next;
+        rows_next = rows_after;
+        // the next chunk has landed, and every wave is done with this one and with P
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+    };
+    for (int ck = 0; ck < nchunks; ck += 2) {
+        chunk(kv_a, kv_b, ck);
+        if (ck + 1 < nchunks) chunk(kv_b, kv_a, ck + 1);
+    }
+
+    // ---- the rows' sums: the wave's four lanes of a row, then the waves in order
+#pragma unroll
+    for (int t = 0; t < HT; ++t) {
+        const float lw = cols4_sum(l_acc[t]);
+        if (g == 0) red[pw * HB + 16 * t + j] = lw;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < HT; ++t) {
+        const int row = 16 * t + j;
+        const float lsum = ((red[row] + red[HB + row]) + red[2 * HB + row]) + red[3 * HB + row];
+        if (row >= it.nrows) continue;
+        const int r = it.r0 + row;
+        if (p.direct) {
+            // a row that sees nothing is zeros
+            const float scl = lsum == 0.f ? 0.f : 1.f / lsum;
+            uint16_t* dst = p.out + row_offset(r, p.T, p.H, p.sob, p.sot, p.ldo) + 4 * g;
+#pragma unroll
+            for (int i = 0; i < kTilesW; ++i) {
+                const int c = 16 * (pw + 4 * i);
+                const f32x4 v = o[i][t] * scl;
+                if (c < p.kv) *reinterpret_cast<uint2*>(dst + c) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            }
+        } else {
+            const int64_t at = int64_t(it.slot) * p.rows + r;
+            float* const dst = p.part_o + at * p.kv + 4 * g;
+#pragma unroll
+            for (int i = 0; i < kTilesW; ++i) {
+                const int c = 16 * (pw + 4 * i);
+                if (c < p.kv) __builtin_nontemporal_store(o[i][t], reinterpret_cast<f32x4*>(dst + c));
+            }
+            if (pw == 0 && g == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = float2{m_ref[t], lsum};
+        }
+    }
+}
+
+// HT: row tiles of an own item (and of the prefix's where its rows fit one such tile).
+template <int HT, bool E4M3>
+__global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchParams p) {
+    __shared__ __attribute__((aligned(128))) uint16_t kv_a[kBlocks * kBlockElems];
+    __shared__ __attribute__((aligned(128))) uint16_t kv_b[kBlocks * kBlockElems];
+    __shared__ __attribute__((aligned(16))) uint16_t pbuf[kChunk * kPPitchB];
+    __shared__ __attribute__((aligned(16))) float red[kWavesB * kChunk];
+    __shared__ __attribute__((aligned(16))) int flags[4];
+    const int bid = static_cast<int>(blockIdx.x);
+    Item it;
+    if (bid < p.pre_items) {
+        int sp, tile;
+        if (p.pre_xcd) {     // the tiles of a span on one XCD (ids 8 apart), whose L2 serves its cache rows to all
+            sp = (bid & 7) + 8 * (bid / (8 * p.pre_tiles));
+            tile = (bid >> 3) % p.pre_tiles;
+        } else {
+            tile = bid % p.pre_tiles;
+            sp = bid / p.pre_tiles;
+        }
+        const int tr = p.pre_wide ? 64 : 16 * HT;
+        it.r0 = tile * tr;
+        it.nrows = min(tr, p.rows - it.r0);
+        it.seq = -1;
+        it.table = p.prefix_pages;
+        it.begin = sp * p.pre_span;
+        it.end = min(p.prefix_len, it.begin + p.pre_span);
+        it.len = 0;
+        it.slot = sp;
+        if (HT < 4 && p.pre_wide) batch_block<4, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+        else batch_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+        return;
+    }
+    const int i = bid - p.pre_items;
+    const int unit = i / p.own_tiles, tile = i - unit * p.own_tiles;
+    const int b = unit / p.own_spans, sp = unit - b * p.own_spans;
+    const int th = p.T * p.H;
+    it.r0 = b * th + tile * 16 * HT;
+    it.nrows = min(16 * HT, th - tile * 16 * HT);
+    it.seq = b;
+    it.table = p.pages + b * p.ld_pages;
+    it.len = max(0, min(p.lens[b], p.max_len));
+    it.begin = sp * p.own_span;
+    it.end = min(it.len, it.begin + p.own_span);
+    it.slot = p.pre_spans + sp;
+    if (it.begin >= it.end && !p.direct) return;     // the merge knows how many spans a sequence has
+    it.end = max(it.end, it.begin);
+    batch_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+}
+
+// out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), the prefix's spans, then the sequence's own.  A block
+// takes a row, a thread four columns; lane s of each wave weighs slot s.
+constexpr int kMergeT = 128;
+constexpr int kMergeB = 8;       // slots loaded at once
+__global__ __launch_bounds__(kMergeT) void attention_batch_merge_kernel(const BatchParams p) {
+    const int r = static_cast<int>(blockIdx.x), lane = threadIdx.x & 63;
+    const int b = r / (p.T * p.H);
+    int n = p.pre_spans;
+    if (p.own_spans) {
+        const int len = max(0, min(p.lens[b], p.max_len));
+        n += (len + p.own_span - 1) / p.own_span;
+    }
+    n = __builtin_amdgcn_readfirstlane(n);
+    float2 ml{-INFINITY, 0.f};
+    if (lane < n) ml = *reinterpret_cast<const float2*>(p.part_ml + (int64_t(lane) * p.rows + r) * 2);
+    const int c = 4 * static_cast<int>(threadIdx.x);
+    const bool has = c < p.kv;
+    const float* src = p.part_o + int64_t(r) * p.kv + (has ? c : 0);
+    const int64_t step = int64_t(p.rows) * p.kv;
+    const float top = wave_max(ml.x);
+    // a NaN reference cannot occur (a maximum skips NaN); a NaN sum stays one
+    const float w = (ml.x == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+    const float total = wave_sum(w * ml.y);
+    f32x4 acc{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < n; s0 += kMergeB) {
+        f32x4 v[kMergeB];
+#pragma unroll
+        for (int u = 0; u < kMergeB; ++u) v[u] = *reinterpret_cast<const f32x4*>(src + int64_t(min(s0 + u, n - 1)) * step);
+#pragma unroll
+        for (int u = 0; u < kMergeB; ++u) {
+            if (s0 + u < n) {
+                const float wu = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s0 + u));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wu, v[u][e], acc[e]);
+            }
+        }
+    }
+    if (!has) return;
+    const float scl = total == 0.f ? 0.f : 1.f / total;
+    uint16_t* dst = p.out + row_offset(r, p.T, p.H, p.sob, p.sot, p.ldo) + c;
+    *reinterpret_cast<uint2*>(dst) = uint2{pack_bf16(acc[0] * scl, acc[1] * scl), pack_bf16(acc[2] * scl, acc[3] * scl)};
+}
+
+// ---------------------------------------------------------------------------------------------
+// The partition.
+// ---------------------------------------------------------------------------------------------
+struct BatchPlan {
+    int ht = 1;                        // row tiles of an own item
+    int pre_tiles = 0, pre_spans = 0, pre_span = kChunk, pre_wide = 0, pre_xcd = 0;
+    int own_tiles = 1, own_spans = 0, own_span = kChunk;
+    int64_t pre_items = 0, items = 0;
+    size_t ws_bytes = 0;
+};
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Time of a chunk in a tile of 16 ht rows, relative to 16 rows.
+int chunk_cost(int ht) { return ht == 4 ? 16 : ht == 2 ? 11 : 10; }
+
+void plan_batch(const nmm_latent_attn_batch& a, BatchPlan* out) {
+    constexpr int64_t kCus = 256;
+    BatchPlan q;
+    const int64_t th = a.tokens * a.heads, rows = a.batch * th;
+    q.ht = th <= 16 ? 1 : th <= 32 ? 2 : 4;
+    q.own_tiles = static_cast<int>(cdiv(th, 16 * q.ht));
+    const int64_t pc = cdiv(a.prefix_len, kChunk), oc = cdiv(a.max_len, kChunk);
+    q.pre_wide = rows > 16 * q.ht ? 1 : 0;
+    const int pre_ht = q.pre_wide ? 4 : q.ht;
+    q.pre_tiles = pc ? static_cast<int>(cdiv(rows, 16 * pre_ht)) : 0;
+    const int64_t own_groups = oc ? a.batch * q.own_tiles : 0;
+    const int cp = chunk_cost(pre_ht), co = chunk_cost(q.ht);
+    // For each number of prefix spans, own spans of about the same time; the pair with the least estimated
+    // time: the longest item where one round of the CUs holds all, else the CUs' share and a last item, and
+    // the merge's reads.
+    int64_t best = -1, best_ps = 0, best_os = 0;
+    const int64_t ps_max = pc ? std::min<int64_t>(pc, kMaxSlots - (oc ? 1 : 0)) : 0;
+    const int64_t tries = pc ? ps_max : std::min<int64_t>(oc, kMaxSlots);
+    for (int64_t i = 1; i <= tries; ++i) {
+        int64_t ps = 0, os = 0;
+        if (pc) {
+            ps = cdiv(pc, cdiv(pc, i));
+            if (oc) os = std::min<int64_t>({oc, kMaxSlots - ps, cdiv(oc * co, cdiv(pc, ps) * cp)});
+        } else {
+            os = i;
+        }
+        if (os) os = cdiv(oc, cdiv(oc, os));
+        const int64_t ip = ps ? cdiv(pc, ps) * cp : 0, io = os ? cdiv(oc, os) * co : 0;
+        const int64_t items = ps * q.pre_tiles + os * own_groups;
+        const int64_t work = ps * q.pre_tiles * ip + os * own_groups * io;
+        int64_t t = items <= kCus ? std::max(ip, io) : work / kCus + std::max(ip, io);
+        t = t * 16 + (ps + os > 1 ? 64 + (ps + os) * rows / 64 : 0);
+        if (best < 0 || t < best) {
+            best = t;
+            best_ps = ps;
+            best_os = os;
+        }
+    }
+    if (pc) {
+        q.pre_span = static_cast<int>(cdiv(pc, best_ps) * kChunk);
+        q.pre_spans = static_cast<int>(cdiv(a.prefix_len, q.pre_span));
+    }
+    if (oc) {
+        q.own_span = static_cast<int>(cdiv(oc, best_os) * kChunk);
+        q.own_spans = static_cast<int>(cdiv(a.max_len, q.own_span));
+    }
+    q.pre_xcd = q.pre_spans % 8 == 0 && q.pre_spans > 0 ? 1 : 0;
+    q.pre_items = int64_t(q.pre_tiles) * q.pre_spans;
+    q.items = q.pre_items + own_groups * q.own_spans;
+    const int64_t slots = q.pre_spans + q.own_spans;
+    if (slots > 1) q.ws_bytes = size_t(kTicketBytes) + size_t(slots) * size_t(rows) * (size_t(a.cache.kv_lora) + 2) * 4;
+    *out = q;
+}
+
+constexpr int64_t kLim = int64_t(1) << 31;
+constexpr int64_t kMaxPositions = int64_t(1) << 30;
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// The sizes that the partition depends on.
+nmm_status validate_sizes(const nmm_latent_attn_batch& a) {
+    const nmm_status st = validate_latent_cache(a.cache);
+    if (st != NMM_OK) return st;
+    if (a.batch < 0 || a.tokens < 0 || a.heads < 0 || a.batch >= (1 << 20) || a.tokens >= (1 << 16) || a.heads >= (1 << 16))
+        return NMM_ERR_SHAPE;
+    if (a.batch * a.tokens * a.heads >= (1 << 24)) return NMM_ERR_SHAPE;
+    if (a.prefix_len < 0 || a.max_len < 0 || a.prefix_len >= kMaxPositions || a.max_len >= kMaxPositions) return NMM_ERR_SHAPE;
+    if (a.page_size < 1 || a.page_size > 65536 || (a.page_size & (a.page_size - 1))) return NMM_ERR_SHAPE;
+    return NMM_OK;
+}
+
+}  // namespace
+}  // namespace nmm
+
+using namespace nmm;
+
+extern "C" {
+
+size_t nmm_latent_attention_batch_workspace_size(const nmm_latent_attn_batch* attn) {
+    if (!attn || validate_sizes(*attn) != NMM_OK || attn->batch * attn->tokens * attn->heads == 0) return 0;
+    BatchPlan q;
+    plan_batch(*attn, &q);
+    return q.ws_bytes;
+}
+
+nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+    if (!attn) return NMM_ERR_NULL;
+    const nmm_latent_attn_batch& a = *attn;
+    nmm_status st = validate_sizes(a);
+    if (st != NMM_OK) return st;
+    if (!std::isfinite(a.scale)) return NMM_ERR_ARG;
+    const int64_t d = a.cache.kv_lora + a.cache.rope;
+    if (a.ldq < d || a.ldo < a.cache.kv_lora || a.ldq >= kLim || a.ldo >= kLim) return NMM_ERR_SHAPE;
+    const int64_t strides[] = {a.stride_qb, a.stride_qt, a.stride_ob, a.stride_ot};
+    for (int64_t v : strides)
+        if (v < 0 || v >= (int64_t(1) << 40)) return NMM_ERR_SHAPE;
+    if (a.max_len > 0 && (a.ld_pages < cdiv(a.max_len, a.page_size) || a.ld_pages >= kLim)) return NMM_ERR_SHAPE;
+    const int64_t rows = a.batch * a.tokens * a.heads;
+    if (rows == 0) return NMM_OK;
+    if (!a.q || !a.out) return NMM_ERR_NULL;
+    if (a.prefix_len > 0 && !a.prefix_pages) return NMM_ERR_NULL;
+    if (a.max_len > 0 && (!a.pages || !a.lens)) return NMM_ERR_NULL;
+    if (!a.cache.data && a.cache.rows > 0) return NMM_ERR_NULL;
+    if (!aligned(a.q, 16) || a.ldq % 8 || a.stride_qb % 8 || a.stride_qt % 8 || !aligned(a.out, 8) || a.ldo % 4 ||
+        a.stride_ob % 4 || a.stride_ot % 4 || !aligned(a.prefix_pages, 4) || !aligned(a.pages, 4) || !aligned(a.lens, 4))
+        return NMM_ERR_ALIGN;
+    BatchPlan q;
+    plan_batch(a, &q);
+    if (q.items >= (int64_t(1) << 32) / kThreadsB || q.pre_items >= kLim) return NMM_ERR_SHAPE;
+    st = validate_workspace(workspace, workspace_bytes, q.ws_bytes);
+    if (st != NMM_OK) return st;
+
+    BatchParams p{};
+    p.q = static_cast<const uint16_t*>(a.q);
+    p.sqb = a.stride_qb; p.sqt = a.stride_qt; p.ldq = a.ldq;
+    p.cache = static_cast<const uint8_t*>(a.cache.data);
+    p.ld = a.cache.ld;
+    p.kv = static_cast<int>(a.cache.kv_lora);
+    p.rope = static_cast<int>(a.cache.rope);
+    while ((int64_t(1) << p.page_shift) < a.page_size) ++p.page_shift;
+    p.n_pages = static_cast<int>(a.cache.rows / a.page_size);
+    p.prefix_pages = a.prefix_pages;
+    p.prefix_len = static_cast<int>(a.prefix_len);
+    p.pages = a.pages;
+    p.ld_pages = a.ld_pages;
+    p.lens = a.lens;
+    p.max_len = static_cast<int>(a.max_len);
+    p.scale_log2 = a.scale * 1.4426950408889634f;
+    p.out = static_cast<uint16_t*>(a.out);
+    p.sob = a.stride_ob; p.sot = a.stride_ot; p.ldo = a.ldo;
+    if (q.ws_bytes) {
+        p.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kTicketBytes);
+        p.part_ml = p.part_o + size_t(q.pre_spans + q.own_spans) * size_t(rows) * size_t(a.cache.kv_lora);
+    }
+    p.B = static_cast<int>(a.batch);
+    p.T = static_cast<int>(a.tokens);
+    p.H = static_cast<int>(a.heads);
+    p.rows = static_cast<int>(rows);
+    p.pre_tiles = q.pre_tiles; p.pre_spans = q.pre_spans; p.pre_span = q.pre_span;
+    p.pre_items = static_cast<int>(q.pre_items);
+    p.pre_wide = q.pre_wide; p.pre_xcd = q.pre_xcd;
+    p.own_tiles = q.own_tiles; p.own_spans = q.own_spans; p.own_span = q.own_span;
+    p.direct = q.pre_spans + q.own_spans == 1 ? 1 : 0;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (q.items > 0) {
+        const dim3 grid(static_cast<uint32_t>(q.items)), block(kThreadsB);
+        const bool q8 = a.cache.format == NMM_CACHE_E4M3;
+        if (q.ht == 1) {
+            if (q8) hipLaunchKernelGGL((attention_batch_kernel<1, true>), grid, block, 0, s, p);
+            else hipLaunchKernelGGL((attention_batch_kernel<1, false>), grid, block, 0, s, p);
+        } else if (q.ht == 2) {
+            if (q8) hipLaunchKernelGGL((attention_batch_kernel<2, true>), grid, block, 0, s, p);
+            else hipLaunchKernelGGL((attention_batch_kernel<2, false>), grid, block, 0, s, p);
+        } else {
+            if (q8) hipLaunchKernelGGL((attention_batch_kernel<4, true>), grid, block, 0, s, p);
+            else hipLaunchKernelGGL((attention_batch_kernel<4, false>), grid, block, 0, s, p);
+        }
+    }
+    // no position anywhere: the merge of no slots writes the zeros
+    if (!p.direct) hipLaunchKernelGGL(attention_batch_merge_kernel, dim3(static_cast<uint32_t>(rows)), dim3(kMergeT), 0, s, p);
+    return hipGetLastError() == hipSuccess ? NMM_OK : NMM_ERR_HIP;
+}
+
+}  // extern "C"
