@@ -444,6 +444,34 @@ nmm_status nmm_mla_decode_step(const nmm_mla_chain* chain, const nmm_latent_attn
                                size_t workspace_bytes, void* stream);
 
 /*
+ * nmm_gemv_w4 -- y[M,N] = x[M,K] . W[N,K]^T for a weight of 4-bit codes with a scale per group of K
+ * (nmm_gemv_nt's product for quantised weights):
+ *   W[n,k] = s[n, k / group] * c[n,k]
+ *   NMM_W4_INT  c = code - z, code in 0 .. 15, z = zeros[n, k / group] (any 8-bit number) or 8 without zeros;
+ *               s in x's type
+ *   NMM_W4_MX   c = the e2m1 value of the code (bit 3 the sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6); s = 2^(b - 127) of a
+ *               byte b (255: NaN), group = 32, no zeros
+ * Codes are widened exactly, products summed in fp32, and a group's scale is applied to its fp32 sum: no
+ * weight is rounded.  Any M (in blocks of up to 32 rows, each reading the weight once).
+ *   dt, x, ldx   as for nmm_gemv_nt.
+ *   Wq, ldwq     codes, row-major [N, ceil(K / 2)] bytes, k even in the low four bits; 16-byte aligned, ldwq
+ *                in bytes, >= ceil(K / 2) and a multiple of 16 (a row's last 16 bytes are read whole; codes past K
+ *                are not used).  (N - 1) * ldwq + 16 * ceil(K / 32) < 2^31.
+ *   scales, lds  [N, ceil(K / group)] row-major, lds in elements; 2-byte aligned (NMM_W4_INT).
+ *   zeros, ldz   the same of bytes, or NULL.
+ *   group        a power of two >= 32; the last group may be cut short by K.
+ *   y, ldy       fp32 output, ldy >= N.
+ *   workspace    >= nmm_gemv_w4_workspace_size(M, K, N, group) bytes (0 where K is not split).
+ * Errors, determinism and empty problems as for nmm_gemv.
+ */
+typedef enum { NMM_W4_INT = 1, NMM_W4_MX = 2 } nmm_w4_format;
+
+nmm_status nmm_gemv_w4(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_w4_format format, int64_t group, const void* x,
+                       int64_t ldx, const void* Wq, int64_t ldwq, const void* scales, int64_t lds, const uint8_t* zeros,
+                       int64_t ldz, float* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+size_t nmm_gemv_w4_workspace_size(int64_t M, int64_t K, int64_t N, int64_t group);
+
+/*
  * The latent cache of a batch: rows addressed one by one (a paged pool), in one of two formats.
  *
  *   NMM_CACHE_BF16  row = kv_lora latents and rope values, bf16: the rows nmm_mla_kv_update writes

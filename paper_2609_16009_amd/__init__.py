@@ -24,6 +24,7 @@ NMM_PATH_AUTO, NMM_PATH_GEMV, NMM_PATH_MFMA = 0, 1, 2
 NMM_ROUND_EVEN, NMM_ROUND_AWAY = 0, 1
 NMM_CACHE_BF16, NMM_CACHE_E4M3 = 1, 2
 NMM_SRC_F32, NMM_SRC_BF16 = 0, 1
+NMM_W4_INT, NMM_W4_MX = 1, 2
 NMM_NOALLOC_SCRATCH_BYTES = 8 << 20   # nmm_gemv_noalloc's scratch per GPU
 
 _i64 = ctypes.c_int64
@@ -129,6 +130,9 @@ EXPORTS = {
     "nmm_mla_decode_step_workspace_size": (_sz, [ctypes.POINTER(nmm_mla_chain), ctypes.POINTER(nmm_latent_attn)]),
     "nmm_latent_attention": (ctypes.c_int, [_i64, _i64, _i64, _i64, _p, _i64, _p, _i64,
                                             ctypes.c_float, _p, _i64, _p, _sz, _p]),
+    "nmm_gemv_w4": (ctypes.c_int, [_i64, _i64, _i64, ctypes.c_int, ctypes.c_int, _i64, _p, _i64, _p, _i64, _p, _i64, _p,
+                                   _i64, _p, _i64, _p, _sz, _p]),
+    "nmm_gemv_w4_workspace_size": (_sz, [_i64, _i64, _i64, _i64]),
     "nmm_latent_cache_row_bytes": (_sz, [ctypes.c_int, _i64, _i64]),
     "nmm_latent_cache_write": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), ctypes.POINTER(nmm_cache_entries), _p]),
     "nmm_latent_cache_read": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), _i64, _p, _p, _i64, _p]),
@@ -197,7 +201,7 @@ def _stream(stream) -> int:
 
 def _ld(t: torch.Tensor) -> int:
     s = t.stride()
-    if s[-1] != 1:
+    if s[-1] != 1 and t.shape[-1] > 1:   # one column has no stride of its own
         raise ValueError("the last dimension must be contiguous")
     return s[-2] if len(s) >= 2 else t.shape[-1]
 
@@ -647,6 +651,32 @@ def _index(where: str, t: torch.Tensor, dtype: torch.dtype, n: int) -> int:
     if t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{where}: indices must be a contiguous {dtype} vector of at least {n}")
     return t.data_ptr()
+
+
+def nmm_gemv_w4(x: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, y: torch.Tensor, *, group: int,
+                zeros: torch.Tensor | None = None, K: int | None = None, workspace=None, stream=None) -> torch.Tensor:
+    """y[M,N] = x[M,K] . W[N,K]^T for 4-bit codes Wq [N, >= K / 2] (uint8, k even in the low bits) with scales
+    [N, groups] of x's type (integers, code - zero with zeros uint8 [N, groups] or 8) or uint8 (e2m1 values, a power of two per
+    32).  K is x's width unless given."""
+    _same_device("nmm_gemv_w4", x, Wq, scales, y, zeros)
+    code = _CODES.get(x.dtype)
+    if code is None or Wq.dtype != torch.uint8 or y.dtype != torch.float32:
+        raise TypeError("x must be bfloat16 or float16, Wq uint8 and y float32")
+    if scales.dtype not in (x.dtype, torch.uint8) or (zeros is not None and zeros.dtype != torch.uint8):
+        raise TypeError("scales must be of x's type or uint8, zeros uint8")
+    M, N = x.shape[0], Wq.shape[0]
+    K = x.shape[1] if K is None else K
+    groups = -(-K // group) if group > 0 else 0
+    if y.shape[0] < M or y.shape[1] < N or x.shape[1] < K or 2 * Wq.shape[1] < K or scales.shape[0] < N or \
+            scales.shape[1] < groups or (zeros is not None and (zeros.shape[0] < N or zeros.shape[1] < groups)):
+        raise ValueError("x [M, >= K], Wq [N, >= K / 2], scales and zeros [N, >= groups], y [M, N] do not fit each other")
+    fmt = NMM_W4_MX if scales.dtype == torch.uint8 else NMM_W4_INT
+    L = lib()
+    _call(L.nmm_gemv_w4, "nmm_gemv_w4", lambda: L.nmm_gemv_w4_workspace_size(M, K, N, group),
+          (M, K, N, code, fmt, group, x.data_ptr(), _ld(x), Wq.data_ptr(), _ld(Wq), scales.data_ptr(), _ld(scales),
+           zeros.data_ptr() if zeros is not None else None, _ld(zeros) if zeros is not None else 0, y.data_ptr(), _ld(y)),
+          workspace, x.device, stream)
+    return y
 
 
 def nmm_latent_cache_row_bytes(kv_lora: int, rope: int, format: int = NMM_CACHE_E4M3) -> int:
