@@ -26,6 +26,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "attention_core.h"
 #include "bf16_cast.h"
@@ -44,7 +45,6 @@ using attn::i32x4;
 using attn::lds_bf16x4;
 using attn::lds_sync;
 using attn::lds_void;
-using attn::pack_bf16;
 using attn::wave_max;
 using attn::wave_sum;
 
@@ -55,7 +55,7 @@ constexpr int kBlockElems = kChunk * 64;               // elements of one column
 constexpr int kSteps = 2 * kBlocks;                    // k-steps of 32 columns
 constexpr int kTilesW = 8;                             // 16-column output tiles per wave
 constexpr int kPPitchB = kChunk + 8;
-constexpr int kAhead = 6;                              // K fragments in flight
+constexpr int kQInAcc = 64;                            // Q fragments (of 72) of a 64-row tile in accumulation registers
 constexpr float kLazy = 8.f;
 constexpr int kMaxSlots = 64;                          // partials of a row: one lane of a wave each
 
@@ -78,8 +78,9 @@ struct BatchParams {
     float* part_o;           // [slots][rows][kv]
     float* part_ml;          // [slots][rows][2]
     int B, T, H, rows;
-    int pre_tiles, pre_spans, pre_span, pre_items, pre_wide, pre_xcd;
-    int own_tiles, own_spans, own_span;
+    int pre_tiles, pre_spans, pre_span, pre_items, pre_wide;
+    int own_tiles, own_spans, own_span, own_items;
+    int pre_grid;            // workgroups of the prefix: its items rounded up to a multiple of 8
     int direct;              // one slot: rows go straight to out
 };
 
@@ -98,17 +99,20 @@ struct Item {
 // Global memory, said so: a pointer that may also be the zero row's would otherwise be read by flat loads, which
 // count as LDS operations too.
 typedef const __attribute__((address_space(1))) uint8_t* gbytes;
-__device__ __forceinline__ uint4 load16(gbytes p) {
-    typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
-    const u32x4_t v = *(const __attribute__((address_space(1))) u32x4_t*)p;
-    return uint4{v[0], v[1], v[2], v[3]};
-}
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 load16(gbytes p) { return *(const __attribute__((address_space(1))) u32x4*)p; }
 // The zero row's address, its contents unknown to the compiler: knowing them it splits every select between
 // a cache row and this one into branches.
 __device__ __forceinline__ gbytes opaque_zero_row() {
     gbytes z = (gbytes)g_zero_row;
     asm("" : "+s"(z));
     return z;
+}
+
+// Two values rounded to bf16 (one conversion).
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
 }
 
 __device__ __forceinline__ int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
@@ -124,6 +128,8 @@ template <int HT, bool E4M3>
 __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it, uint16_t* const kv_a, uint16_t* const kv_b,
                                             uint16_t* const pbuf, float* const red, int* const flags) {
     constexpr int HB = 16 * HT;
+    // K and V fragments read ahead of their MFMAs: LDS takes about 130 cycles, a step's HT MFMAs 16 HT
+    constexpr int kAhead = HT == 4 ? (E4M3 ? 3 : 4) : HT == 2 ? 6 : 9, kAheadV = HT == 4 ? (E4M3 ? 3 : 4) : 8;
     const int tid = threadIdx.x, lane = tid & 63;
     const int pw = __builtin_amdgcn_readfirstlane(tid >> 6) & (kWavesB - 1);
     const int g = lane >> 4, j = lane & 15;
@@ -145,55 +151,57 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
         const int r = __builtin_amdgcn_ds_bpermute(row << 2, rows);
         return r < 0 ? zero_row : cache + int64_t(r) * p.ld;
     };
+    // Columns that the cache lacks read the last ones that it has: Q is zero there, and their outputs are not stored.
     // 8 rows x 128 bytes per LDS-direct load; the wave's rows are 16 pw .. 16 pw + 15
     const int c_st = (lane & 7) ^ swz(lane >> 3);
+    const uint32_t lat_last = uint32_t(2 * p.kv - 16);
+    const uint32_t rope_off = p.rope ? uint32_t(2 * p.kv + min(16 * c_st, 2 * p.rope - 16)) : 0u;
     auto stage_bf16 = [&](gbytes row_ptr, uint16_t* buf, int cb, int half) {
-        const bool has = cb < 8 ? 64 * cb + 8 * c_st < p.kv : 8 * c_st < p.rope;
-        const gbytes src = has ? row_ptr + (cb < 8 ? cb * 128 : 2 * p.kv) + c_st * 16 : zero_row;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+        const uint32_t off = cb < 8 ? min(uint32_t(cb * 128 + c_st * 16), lat_last) : rope_off;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row_ptr + off),
                                          (lds_void*)(buf + cb * kBlockElems + (16 * pw + 8 * half) * 64), 16, 0, 0);
     };
-    // 8-bit rows: a thread takes pieces 8 i + (tid & 7) of 16 codes of rows tid / 8 and tid / 8 + 32, a scale
-    // row and one piece of RoPE
-    struct Raw {
-        uint4 code[2][4], scale[2], rope[2];
+    // 8-bit rows, half a chunk at a time: a thread takes pieces 8 i + (tid & 7) of 16 codes of row tid / 8 (+ 32),
+    // the row's scales and one piece of RoPE
+    u32x4 code0, code1, code2, code3, code_scale, code_rope;
+    const int l8 = tid & 7;
+    const uint32_t rope8 = p.rope ? uint32_t(p.kv + kScaleBytes + min(16 * l8, 2 * p.rope - 16)) : 0u;
+    auto load_raw = [&](int rows, int ps) {
+        const gbytes src = ptr_of(rows, (tid >> 3) + 32 * ps);
+        const uint32_t last = uint32_t(p.kv - 16);
+        code0 = load16(src + min(uint32_t(16 * l8), last));
+        code1 = load16(src + min(uint32_t(16 * l8 + 128), last));
+        code2 = load16(src + min(uint32_t(16 * l8 + 256), last));
+        code3 = load16(src + min(uint32_t(16 * l8 + 384), last));
+        code_scale = load16(src + p.kv);
+        code_rope = load16(src + rope8);
     };
-    auto load_raw = [&](Raw& w, int rows) {
-#pragma unroll
-        for (int ps = 0; ps < 2; ++ps) {
-            const gbytes src = ptr_of(rows, (tid >> 3) + 32 * ps);
-            const int l = tid & 7;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = 16 * (l + 8 * i);
-                w.code[ps][i] = load16((c < p.kv ? src : zero_row) + c);
-            }
-            w.scale[ps] = load16(src + p.kv);
-            w.rope[ps] = load16(8 * l < p.rope ? src + p.kv + kScaleBytes + 16 * l : zero_row);
+    // part i < 4: piece l8 + 8 i, which is pieces 2 (l8 % 4) and + 1 of column block 2 i + l8 / 4; part 4: RoPE's
+    const int f8 = swz(tid >> 3), hi8 = l8 >> 2;
+    const int w8_first = (tid >> 3) * 64 + hi8 * kBlockElems + (((2 * (l8 & 3) + hi8) ^ f8) << 3);
+    const int w8_second = (tid >> 3) * 64 + hi8 * kBlockElems + (((2 * (l8 & 3) + 1 - hi8) ^ f8) << 3);
+    const int w8_rope = (tid >> 3) * 64 + 8 * kBlockElems + ((l8 ^ f8) << 3);
+    auto commit_part = [&](uint16_t* buf, int ps, auto part) {
+        constexpr int i = decltype(part)::value;
+        uint16_t* const dst = buf + 32 * 64 * ps;
+        if constexpr (i == 4) {
+            *reinterpret_cast<u32x4*>(dst + w8_rope) = code_rope;
+        } else {
+            const u32x4 q = i == 0 ? code0 : i == 1 ? code1 : i == 2 ? code2 : code3;
+            const float s = 16 * (l8 + 8 * i) < p.kv ? scale_of(code_scale[i] >> (8 * (l8 >> 1))) : 0.f;
+            const uint2 a = dequant4(q[0], s), b = dequant4(q[1], s), c = dequant4(q[2], s), d = dequant4(q[3], s);
+            const u32x4 lo{a.x, a.y, b.x, b.y}, up{c.x, c.y, d.x, d.y};
+            // lanes 4 to 7 write their upper half first: the eight lanes of a row then hit eight slots
+            *reinterpret_cast<u32x4*>(dst + 2 * i * kBlockElems + w8_first) = hi8 ? up : lo;
+            *reinterpret_cast<u32x4*>(dst + 2 * i * kBlockElems + w8_second) = hi8 ? lo : up;
         }
     };
-    auto commit_raw = [&](const Raw& w, uint16_t* buf) {
-#pragma unroll
-        for (int ps = 0; ps < 2; ++ps) {
-            const int row = (tid >> 3) + 32 * ps, l = tid & 7, f = swz(row);
-            const uint32_t sc[4] = {w.scale[ps].x, w.scale[ps].y, w.scale[ps].z, w.scale[ps].w};
-            const int hi = l >> 2;
-            uint16_t* const dst = buf + row * 64;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                // piece l + 8 i: column block 2 i + l / 4, pieces 2 (l % 4) and + 1 of it
-                const float s = scale_of(sc[i] >> (8 * (l >> 1)));
-                const uint2 a = dequant4(w.code[ps][i].x, s), b = dequant4(w.code[ps][i].y, s);
-                const uint2 c = dequant4(w.code[ps][i].z, s), d = dequant4(w.code[ps][i].w, s);
-                const uint4 lo{a.x, a.y, b.x, b.y}, up{c.x, c.y, d.x, d.y};
-                uint16_t* const blk = dst + (2 * i + hi) * kBlockElems;
-                const int c0 = 2 * (l & 3);
-                // lanes 4 to 7 write their upper half first: the eight lanes of a row then hit eight slots
-                *reinterpret_cast<uint4*>(blk + (((c0 + hi) ^ f) << 3)) = hi ? up : lo;
-                *reinterpret_cast<uint4*>(blk + (((c0 + 1 - hi) ^ f) << 3)) = hi ? lo : up;
-            }
-            *reinterpret_cast<uint4*>(dst + 8 * kBlockElems + ((l ^ f) << 3)) = w.rope[ps];
-        }
+    auto commit_at = [&](uint16_t* buf, int ps, int step) {       // step 0 .. 4, a constant where it is called
+        if (step == 0) commit_part(buf, ps, std::integral_constant<int, 0>{});
+        if (step == 1) commit_part(buf, ps, std::integral_constant<int, 1>{});
+        if (step == 2) commit_part(buf, ps, std::integral_constant<int, 2>{});
+        if (step == 3) commit_part(buf, ps, std::integral_constant<int, 3>{});
+        if (step == 4) commit_part(buf, ps, std::integral_constant<int, 4>{});
     };
 
     // ---- Q rows to buffer b, in the chunk's layout (rows past the tile's and columns past the cache's: zeros)
@@ -214,10 +222,13 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
         }
     }
     int rows_cur = row_of(it.begin);
-    Raw raw;
     if constexpr (E4M3) {
-        load_raw(raw, rows_cur);
-        commit_raw(raw, kv_a);
+#pragma unroll
+        for (int ps = 0; ps < 2; ++ps) {
+            load_raw(rows_cur, ps);
+#pragma unroll
+            for (int i = 0; i < 5; ++i) commit_at(kv_a, ps, i);
+        }
     } else {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -239,9 +250,18 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
         for (int u = 0; u < kSteps; ++u)
             qf[t][u] = *reinterpret_cast<const i32x4*>(kv_b + (u >> 1) * kBlockElems + 16 * t * 64 + (u & 1 ? fr1 : fr0));
     lds_sync();
+    // 64 rows of Q fill 288 registers: most of them in the accumulation half of the file, which MFMA operands may
+    // come from, and said so (the compiler keeps them there as spills otherwise, 288 copies a chunk)
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u)
+            if (t * kSteps + u < kQInAcc) asm("" : "+a"(qf[t][u]));
+    if constexpr (E4M3) load_raw(rows_next, 0);
 
     // positions that a row sees: those below its limit
     int limit[HT];
+    const int all_see = it.seq >= 0 ? it.len - (p.T - 1) : it.end;    // positions below it are seen by every row
 #pragma unroll
     for (int t = 0; t < HT; ++t) {
         limit[t] = it.end;
@@ -270,16 +290,12 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
 
     auto chunk = [&](const uint16_t* cur, uint16_t* nxt, int ck) {
         const int c0 = it.begin + ck * kChunk;
-        const bool stage_next = ck + 1 < nchunks;
         const uint64_t present = __builtin_amdgcn_ballot_w64(rows_cur >= 0);
+        // the next chunk (behind the last: rows of zeros, which nothing reads)
         gbytes rp[2];
-        if (stage_next) {
-            if constexpr (E4M3) {
-                load_raw(raw, rows_next);
-            } else {
-                rp[0] = ptr_of(rows_next, 16 * pw + (lane >> 3));
-                rp[1] = ptr_of(rows_next, 16 * pw + 8 + (lane >> 3));
-            }
+        if constexpr (!E4M3) {
+            rp[0] = ptr_of(rows_next, 16 * pw + (lane >> 3));
+            rp[1] = ptr_of(rows_next, 16 * pw + 8 + (lane >> 3));
         }
         const int rows_after = row_of(c0 + 2 * kChunk);
 
@@ -300,44 +316,47 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
             for (int t = 0; t < HT; ++t)
                 s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[u % kAhead]), as_bf16x8(qf[t][u]), s[t], 0, 0, 0);
             if (u + kAhead < kSteps) kf[u % kAhead] = k_frag(u + kAhead);
-            if constexpr (!E4M3) {
-                if (stage_next) stage_bf16(rp[u & 1], nxt, u >> 1, u & 1);
+            if constexpr (E4M3) {
+                // the first half of the next chunk's rows, in the MFMAs' shadow
+                if (u % 3 == 2 && u < 15) commit_at(nxt, 0, u / 3);
+                if (u == 15) load_raw(rows_next, 1);
+            } else {
+                stage_bf16(rp[u & 1], nxt, u >> 1, u & 1);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
 
-        // ---- scores in log2 units, masked, and the wave's maximum per row
+        // ---- scores in log2 units, masked where some row does not see all 64 positions, and the wave's maximum
+        // per row
         const int at = 16 * pw + 4 * g;
-        const uint32_t here = uint32_t(present >> at);
         float mx[HT];
         bool need = false;
 #pragma unroll
-        for (int t = 0; t < HT; ++t) {
-            mx[t] = -INFINITY;
+        for (int t = 0; t < HT; ++t) s[t] *= p.scale_log2;
+        if (present != ~uint64_t(0) || c0 + kChunk > all_see) {
+            const uint32_t here = uint32_t(present >> at);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool seen = ((here >> i) & 1u) && c0 + at + i < limit[t];
-                const float v = seen ? s[t][i] * p.scale_log2 : -INFINITY;
-                s[t][i] = v;
-                mx[t] = fmaxf(mx[t], v);
-            }
-            mx[t] = cols4_max(mx[t]);
+            for (int t = 0; t < HT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[t][i] = ((here >> i) & 1u) && c0 + at + i < limit[t] ? s[t][i] : -INFINITY;
+        }
+#pragma unroll
+        for (int t = 0; t < HT; ++t) {
+            mx[t] = cols4_max(fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
             need |= !(mx[t] <= m_ref[t] + kLazy);
         }
         float lc[HT];
         auto write_p = [&]() {
 #pragma unroll
             for (int t = 0; t < HT; ++t) {
+                // (a row that has seen nothing yet: 2^(-inf - 0) = 0)
+                const float m = m_ref[t] == -INFINITY ? 0.f : m_ref[t];
                 float pv[4];
-                lc[t] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float v = s[t][i];
-                    pv[i] = (v == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(v - m_ref[t]);
-                    lc[t] += pv[i];
-                }
+                for (int i = 0; i < 4; ++i) pv[i] = __builtin_amdgcn_exp2f(s[t][i] - m);
+                lc[t] = (pv[0] + pv[1]) + (pv[2] + pv[3]);
                 *reinterpret_cast<uint2*>(pbuf + (16 * t + j) * kPPitchB + at) =
-                    uint2{pack_bf16(pv[0], pv[1]), pack_bf16(pv[2], pv[3])};
+                    uint2{pack2(pv[0], pv[1]), pack2(pv[2], pv[3])};
             }
         };
         if (g == 0) {
@@ -383,36 +402,43 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
 #pragma unroll
         for (int t = 0; t < HT; ++t) l_acc[t] += lc[t];
 
-        // ---- O^T += V^T P^T over two steps of 32 positions
+        // ---- O^T += V^T P^T: step v is column tile v % 8 of positions 32 (v / 8) .. + 31
+        auto p_frag = [&](int t, int kk) {
+            return *reinterpret_cast<const i32x4*>(pbuf + (16 * t + j) * kPPitchB + 32 * kk + 8 * g);
+        };
+        auto v_frag = [&](int v) {
+            const uint16_t* base = cur + (v % kTilesW) * kBlockElems + 32 * (v / kTilesW) * 64;
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + v_lo));
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + v_hi));
+            const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
+            return i32x4{int(ulo.x), int(ulo.y), int(uhi.x), int(uhi.y)};
+        };
+        i32x4 pf[HT], vf[kAheadV];
 #pragma unroll
-        for (int kk = 0; kk < kChunk / 32; ++kk) {
-            i32x4 pf[HT];
+        for (int t = 0; t < HT; ++t) pf[t] = p_frag(t, 0);
 #pragma unroll
-            for (int t = 0; t < HT; ++t)
-                pf[t] = *reinterpret_cast<const i32x4*>(pbuf + (16 * t + j) * kPPitchB + 32 * kk + 8 * g);
-            i32x4 vf[kTilesW];
+        for (int v = 0; v < kAheadV; ++v) vf[v] = v_frag(v);
 #pragma unroll
-            for (int i = 0; i < kTilesW; ++i) {
-                const uint16_t* base = cur + i * kBlockElems + 32 * kk * 64;
-                const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + v_lo));
-                const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + v_hi));
-                const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
-                vf[i] = i32x4{int(ulo.x), int(ulo.y), int(uhi.x), int(uhi.y)};
+        for (int v = 0; v < 2 * kTilesW; ++v) {
+            const int i = v % kTilesW;
+#pragma unroll
+            for (int t = 0; t < HT; ++t) {
+                o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[v % kAheadV]), as_bf16x8(pf[t]), o[i][t], 0, 0, 0);
+                if (v == kTilesW - 1) pf[t] = p_frag(t, 1);
             }
-#pragma unroll
-            for (int i = 0; i < kTilesW; ++i)
-#pragma unroll
-                for (int t = 0; t < HT; ++t)
-                    o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[i]), as_bf16x8(pf[t]), o[i][t], 0, 0, 0);
-        }
-        if constexpr (E4M3) {
-            if (stage_next) commit_raw(raw, nxt);
+            if (v + kAheadV < 2 * kTilesW) vf[v % kAheadV] = v_frag(v + kAheadV);
+            if constexpr (E4M3) {
+                // the second half of the next chunk's rows; then the loads of the one after it
+                if (v % 3 == 2 && v < 15) commit_at(nxt, 1, v / 3);
+                if (v == 15) load_raw(rows_after, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
         rows_cur = rows_next;
         rows_next = rows_after;
         // the next chunk has landed, and every wave is done with this one and with P
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
+        if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);
+        lds_sync();
     };
     for (int ck = 0; ck < nchunks; ck += 2) {
         chunk(kv_a, kv_b, ck);
@@ -440,7 +466,7 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
             for (int i = 0; i < kTilesW; ++i) {
                 const int c = 16 * (pw + 4 * i);
                 const f32x4 v = o[i][t] * scl;
-                if (c < p.kv) *reinterpret_cast<uint2*>(dst + c) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                if (c < p.kv) *reinterpret_cast<uint2*>(dst + c) = uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
             }
         } else {
             const int64_t at = int64_t(it.slot) * p.rows + r;
@@ -455,6 +481,14 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
     }
 }
 
+// Workgroup ids go round the 8 XCDs: id b of a range of items padded to a multiple of 8 takes an item such that
+// each XCD gets a run of consecutive ones, which read the same cache rows through its L2.  -1: padding.
+__device__ __forceinline__ int xcd_run(int b, int items) {
+    const int per = (items + 7) >> 3;
+    const int v = (b & 7) * per + (b >> 3);
+    return v < items ? v : -1;
+}
+
 // HT: row tiles of an own item (and of the prefix's where its rows fit one such tile).
 template <int HT, bool E4M3>
 __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchParams p) {
@@ -465,15 +499,10 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchP
     __shared__ __attribute__((aligned(16))) int flags[4];
     const int bid = static_cast<int>(blockIdx.x);
     Item it;
-    if (bid < p.pre_items) {
-        int sp, tile;
-        if (p.pre_xcd) {     // the tiles of a span on one XCD (ids 8 apart), whose L2 serves its cache rows to all
-            sp = (bid & 7) + 8 * (bid / (8 * p.pre_tiles));
-            tile = (bid >> 3) % p.pre_tiles;
-        } else {
-            tile = bid % p.pre_tiles;
-            sp = bid / p.pre_tiles;
-        }
+    if (bid < p.pre_grid) {
+        const int v = xcd_run(bid, p.pre_items);
+        if (v < 0) return;
+        const int sp = v / p.pre_tiles, tile = v - sp * p.pre_tiles;
         const int tr = p.pre_wide ? 64 : 16 * HT;
         it.r0 = tile * tr;
         it.nrows = min(tr, p.rows - it.r0);
@@ -483,25 +512,25 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchP
         it.end = min(p.prefix_len, it.begin + p.pre_span);
         it.len = 0;
         it.slot = sp;
-        if (HT < 4 && p.pre_wide) batch_block<4, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
-        else batch_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
-        return;
+    } else {
+        const int v = xcd_run(bid - p.pre_grid, p.own_items);
+        if (v < 0) return;
+        const int unit = v / p.own_tiles, tile = v - unit * p.own_tiles;
+        const int b = unit / p.own_spans, sp = unit - b * p.own_spans;
+        const int th = p.T * p.H;
+        it.r0 = b * th + tile * 16 * HT;
+        it.nrows = min(16 * HT, th - tile * 16 * HT);
+        it.seq = b;
+        it.table = p.pages + b * p.ld_pages;
+        it.len = max(0, min(p.lens[b], p.max_len));
+        it.begin = sp * p.own_span;
+        it.end = min(it.len, it.begin + p.own_span);
+        it.slot = p.pre_spans + sp;
+        if (it.begin >= it.end && !p.direct) return;     // the merge knows how many spans a sequence has
+        it.end = max(it.end, it.begin);
     }
-    const int i = bid - p.pre_items;
-    const int unit = i / p.own_tiles, tile = i - unit * p.own_tiles;
-    const int b = unit / p.own_spans, sp = unit - b * p.own_spans;
-    const int th = p.T * p.H;
-    it.r0 = b * th + tile * 16 * HT;
-    it.nrows = min(16 * HT, th - tile * 16 * HT);
-    it.seq = b;
-    it.table = p.pages + b * p.ld_pages;
-    it.len = max(0, min(p.lens[b], p.max_len));
-    it.begin = sp * p.own_span;
-    it.end = min(it.len, it.begin + p.own_span);
-    it.slot = p.pre_spans + sp;
-    if (it.begin >= it.end && !p.direct) return;     // the merge knows how many spans a sequence has
-    it.end = max(it.end, it.begin);
-    batch_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+    if (HT < 4 && it.seq < 0 && p.pre_wide) batch_block<4, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+    else batch_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
 }
 
 // out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), the prefix's spans, then the sequence's own.  A block
@@ -544,7 +573,7 @@ __global__ __launch_bounds__(kMergeT) void attention_batch_merge_kernel(const Ba
     if (!has) return;
     const float scl = total == 0.f ? 0.f : 1.f / total;
     uint16_t* dst = p.out + row_offset(r, p.T, p.H, p.sob, p.sot, p.ldo) + c;
-    *reinterpret_cast<uint2*>(dst) = uint2{pack_bf16(acc[0] * scl, acc[1] * scl), pack_bf16(acc[2] * scl, acc[3] * scl)};
+    *reinterpret_cast<uint2*>(dst) = uint2{pack2(acc[0] * scl, acc[1] * scl), pack2(acc[2] * scl, acc[3] * scl)};
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -552,9 +581,9 @@ __global__ __launch_bounds__(kMergeT) void attention_batch_merge_kernel(const Ba
 // ---------------------------------------------------------------------------------------------
 struct BatchPlan {
     int ht = 1;                        // row tiles of an own item
-    int pre_tiles = 0, pre_spans = 0, pre_span = kChunk, pre_wide = 0, pre_xcd = 0;
+    int pre_tiles = 0, pre_spans = 0, pre_span = kChunk, pre_wide = 0;
     int own_tiles = 1, own_spans = 0, own_span = kChunk;
-    int64_t pre_items = 0, items = 0;
+    int64_t pre_items = 0, own_items = 0, grid = 0;
     size_t ws_bytes = 0;
 };
 
@@ -609,9 +638,9 @@ void plan_batch(const nmm_latent_attn_batch& a, BatchPlan* out) {
         q.own_span = static_cast<int>(cdiv(oc, best_os) * kChunk);
         q.own_spans = static_cast<int>(cdiv(a.max_len, q.own_span));
     }
-    q.pre_xcd = q.pre_spans % 8 == 0 && q.pre_spans > 0 ? 1 : 0;
     q.pre_items = int64_t(q.pre_tiles) * q.pre_spans;
-    q.items = q.pre_items + own_groups * q.own_spans;
+    q.own_items = own_groups * q.own_spans;
+    q.grid = (cdiv(q.pre_items, 8) + cdiv(q.own_items, 8)) * 8;
     const int64_t slots = q.pre_spans + q.own_spans;
     if (slots > 1) q.ws_bytes = size_t(kTicketBytes) + size_t(slots) * size_t(rows) * (size_t(a.cache.kv_lora) + 2) * 4;
     *out = q;
@@ -672,7 +701,7 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
         return NMM_ERR_ALIGN;
     BatchPlan q;
     plan_batch(a, &q);
-    if (q.items >= (int64_t(1) << 32) / kThreadsB || q.pre_items >= kLim) return NMM_ERR_SHAPE;
+    if (q.grid >= (int64_t(1) << 32) / kThreadsB) return NMM_ERR_SHAPE;
     st = validate_workspace(workspace, workspace_bytes, q.ws_bytes);
     if (st != NMM_OK) return st;
 
@@ -704,12 +733,14 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
     p.rows = static_cast<int>(rows);
     p.pre_tiles = q.pre_tiles; p.pre_spans = q.pre_spans; p.pre_span = q.pre_span;
     p.pre_items = static_cast<int>(q.pre_items);
-    p.pre_wide = q.pre_wide; p.pre_xcd = q.pre_xcd;
+    p.pre_grid = static_cast<int>(cdiv(q.pre_items, 8) * 8);
+    p.own_items = static_cast<int>(q.own_items);
+    p.pre_wide = q.pre_wide;
     p.own_tiles = q.own_tiles; p.own_spans = q.own_spans; p.own_span = q.own_span;
     p.direct = q.pre_spans + q.own_spans == 1 ? 1 : 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (q.items > 0) {
-        const dim3 grid(static_cast<uint32_t>(q.items)), block(kThreadsB);
+    if (q.grid > 0) {
+        const dim3 grid(static_cast<uint32_t>(q.grid)), block(kThreadsB);
         const bool q8 = a.cache.format == NMM_CACHE_E4M3;
         if (q.ht == 1) {
             if (q8) hipLaunchKernelGGL((attention_batch_kernel<1, true>), grid, block, 0, s, p);
