@@ -94,6 +94,7 @@ struct Item {
     int begin, end;          // positions of the span (end <= the length)
     int len;                 // own length of the sequence
     int slot;
+    int tile, tiles;         // the tile among those that read the same rows
 };
 
 // Global memory, said so: a pointer that may also be the zero row's would otherwise be read by flat loads, which
@@ -136,6 +137,15 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
     const int nchunks = (it.end - it.begin + kChunk - 1) / kChunk;
     const gbytes cache = (gbytes)p.cache;
     const gbytes zero_row = opaque_zero_row();
+
+    // Chunk ck of the walk.  The tiles that read the same rows start their walks at different chunks, so that each
+    // row comes from memory once, for one of them, and from L2 for the others.
+    const int first = nchunks ? int(uint32_t(it.tile) * uint32_t(nchunks) / uint32_t(it.tiles)) : 0;
+    auto start_of = [&](int ck) {
+        int c = ck + first;
+        c = c >= nchunks ? c - nchunks : c;
+        return ck < nchunks ? it.begin + c * kChunk : it.end;      // past the last: no positions
+    };
 
     // ---- staging.  Cache row of position c0 + lane, or -1
     auto row_of = [&](int c0) {
@@ -221,7 +231,7 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
                                              (lds_void*)(kv_b + cb * kBlockElems + 8 * grp * 64), 16, 0, 0);
         }
     }
-    int rows_cur = row_of(it.begin);
+    int rows_cur = row_of(start_of(0));
     if constexpr (E4M3) {
 #pragma unroll
         for (int ps = 0; ps < 2; ++ps) {
@@ -237,7 +247,7 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
             for (int cb = 0; cb < kBlocks; ++cb) stage_bf16(rp, kv_a, cb, half);
         }
     }
-    int rows_next = row_of(it.begin + kChunk);
+    int rows_next = row_of(start_of(1));
     __builtin_amdgcn_s_waitcnt(0);
     lds_sync();
     // fragment addresses: row j of a 16-row tile, piece 4 (u & 1) + g of column block u / 2
@@ -289,7 +299,7 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
     const int v_hi = (vrow + 4) * 64 + (((2 * pw + (b4 >> 1)) ^ swz(a4 + 4)) << 3) + 4 * (b4 & 1);
 
     auto chunk = [&](const uint16_t* cur, uint16_t* nxt, int ck) {
-        const int c0 = it.begin + ck * kChunk;
+        const int c0 = start_of(ck);
         const uint64_t present = __builtin_amdgcn_ballot_w64(rows_cur >= 0);
         // the next chunk (behind the last: rows of zeros, which nothing reads)
         gbytes rp[2];
@@ -297,7 +307,7 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
             rp[0] = ptr_of(rows_next, 16 * pw + (lane >> 3));
             rp[1] = ptr_of(rows_next, 16 * pw + 8 + (lane >> 3));
         }
-        const int rows_after = row_of(c0 + 2 * kChunk);
+        const int rows_after = row_of(start_of(ck + 2));
 
         // ---- S^T, K fragments read kAhead steps ahead, the next chunk's loads between the steps
         f32x4 s[HT];
@@ -512,6 +522,8 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchP
         it.end = min(p.prefix_len, it.begin + p.pre_span);
         it.len = 0;
         it.slot = sp;
+        it.tile = tile;
+        it.tiles = p.pre_tiles;
     } else {
         const int v = xcd_run(bid - p.pre_grid, p.own_items);
         if (v < 0) return;
@@ -526,6 +538,8 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchP
         it.begin = sp * p.own_span;
         it.end = min(it.len, it.begin + p.own_span);
         it.slot = p.pre_spans + sp;
+        it.tile = tile;
+        it.tiles = p.own_tiles;
         if (it.begin >= it.end && !p.direct) return;     // the merge knows how many spans a sequence has
         it.end = max(it.end, it.begin);
     }
