@@ -55,7 +55,6 @@ constexpr int kBlockElems = kChunk * 64;               // elements of one column
 constexpr int kSteps = 2 * kBlocks;                    // k-steps of 32 columns
 constexpr int kTilesW = 8;                             // 16-column output tiles per wave
 constexpr int kPPitchB = kChunk + 8;
-constexpr int kQInAcc = 64;                            // Q fragments (of 72) of a 64-row tile in accumulation registers
 constexpr float kLazy = 8.f;
 constexpr int kMaxSlots = 64;                          // partials of a row: one lane of a wave each
 
@@ -78,7 +77,7 @@ struct BatchParams {
     float* part_o;           // [slots][rows][kv]
     float* part_ml;          // [slots][rows][2]
     int B, T, H, rows;
-    int pre_tiles, pre_spans, pre_span, pre_items, pre_wide;
+    int pre_tiles, pre_spans, pre_span, pre_items;
     int own_tiles, own_spans, own_span, own_items;
     int pre_grid;            // workgroups of the prefix: its items rounded up to a multiple of 8
     int direct;              // one slot: rows go straight to out
@@ -116,7 +115,20 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
 }
 
-__device__ __forceinline__ int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+// The two halves of cols4_max: the maximum over rows 32 lanes apart, then 16.
+__device__ __forceinline__ float rows_max32(float x) {
+    const attn::u32x2 a = attn::swap32(__float_as_uint(x), __float_as_uint(x));
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float rows_max16(float x) {
+    const attn::u32x2 a = attn::swap16(__float_as_uint(x), __float_as_uint(x));
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// f(r), from bits 1 to 3 of the row (bit 0 picks the half of LDS's 64 banks): LDS serves 256 bytes a cycle, 16 lanes of a
+// key read (16 rows, one piece: every f differs) or 32 of a transposed value read (rows 8 g + 0 .. 3 of two g, two
+// neighbouring pieces: f differs above bit 0).
+__device__ __forceinline__ int swz(int row) { return ((row >> 1) & 4) | (row & 2) | ((row >> 2) & 1); }
 
 __device__ __forceinline__ int64_t row_offset(int r, int T, int H, int64_t sb, int64_t st, int64_t ld) {
     const int bt = r / H, h = r - bt * H;
@@ -124,13 +136,42 @@ __device__ __forceinline__ int64_t row_offset(int r, int T, int H, int64_t sb, i
     return int64_t(b) * sb + int64_t(t) * st + int64_t(h) * ld;
 }
 
+// Row 16 t + j of a tile: normalised to out, or as the span's partial (reference, sum, unnormalised output).
+template <int HT>
+__device__ __forceinline__ void store_row(const BatchParams& p, const Item& it, int row, int pw, int g, const f32x4 (&o)[kTilesW][HT],
+                                          int t, float m, float lsum) {
+    if (row >= it.nrows) return;
+    const int r = it.r0 + row;
+    if (p.direct) {
+        // a row that sees nothing is zeros
+        const float scl = lsum == 0.f ? 0.f : 1.f / lsum;
+        uint16_t* dst = p.out + row_offset(r, p.T, p.H, p.sob, p.sot, p.ldo) + 4 * g;
+#pragma unroll
+        for (int i = 0; i < kTilesW; ++i) {
+            const int c = 16 * (pw + 4 * i);
+            const f32x4 v = o[i][t] * scl;
+            if (c < p.kv) *reinterpret_cast<uint2*>(dst + c) = uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+        }
+    } else {
+        const int64_t at = int64_t(it.slot) * p.rows + r;
+        float* const dst = p.part_o + at * p.kv + 4 * g;
+#pragma unroll
+        for (int i = 0; i < kTilesW; ++i) {
+            const int c = 16 * (pw + 4 * i);
+            if (c < p.kv) __builtin_nontemporal_store(o[i][t], reinterpret_cast<f32x4*>(dst + c));
+        }
+        if (pw == 0 && g == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = float2{m, lsum};
+    }
+}
+
 // One (tile, span).  kv_a, kv_b: chunk buffers; pbuf: P [16 HT][kPPitchB]; red: [4][16 HT].
 template <int HT, bool E4M3>
-__device__ __forceinline__ void batch_block(const BatchParams& p, const Item it, uint16_t* const kv_a, uint16_t* const kv_b,
+__device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it, uint16_t* const kv_a, uint16_t* const kv_b,
                                             uint16_t* const pbuf, float* const red, int* const flags) {
     constexpr int HB = 16 * HT;
     // K and V fragments read ahead of their MFMAs: LDS takes about 130 cycles, a step's HT MFMAs 16 HT
-    constexpr int kAhead = HT == 4 ? (E4M3 ? 3 : 4) : HT == 2 ? 6 : 9, kAheadV = HT == 4 ? (E4M3 ? 3 : 4) : 8;
+    static_assert(HT == 1 || HT == 2, "16 or 32 rows");
+    constexpr int kAhead = HT == 2 ? 6 : 9, kAheadV = 8;
     const int tid = threadIdx.x, lane = tid & 63;
     const int pw = __builtin_amdgcn_readfirstlane(tid >> 6) & (kWavesB - 1);
     const int g = lane >> 4, j = lane & 15;
@@ -147,27 +188,27 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
         return ck < nchunks ? it.begin + c * kChunk : it.end;      // past the last: no positions
     };
 
-    // ---- staging.  Cache row of position c0 + lane, or -1
-    auto row_of = [&](int c0) {
+    // ---- staging.  The page of position c0 + lane (past the end, the last position's) and its cache row, or -1.
+    // Two steps: memory operations complete in order, so waiting for a page also waits for every older load, and
+    // is left until those are wanted anyway.
+    auto page_of = [&](int c0) { return it.table[min(c0 + lane, max(it.end - 1, 0)) >> p.page_shift]; };
+    auto row_at = [&](int page, int c0) {
         const int pos = c0 + lane;
-        int r = -1;
-        if (pos < it.end) {
-            const int page = it.table[pos >> p.page_shift];
-            if (page >= 0 && page < p.n_pages) r = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
-        }
-        return r;
+        const int r = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+        return pos < it.end && uint32_t(page) < uint32_t(p.n_pages) ? r : -1;
     };
+    auto row_of = [&](int c0) { return row_at(page_of(c0), c0); };
     auto ptr_of = [&](int rows, int row) {
         const int r = __builtin_amdgcn_ds_bpermute(row << 2, rows);
         return r < 0 ? zero_row : cache + int64_t(r) * p.ld;
     };
     // Columns that the cache lacks read the last ones that it has: Q is zero there, and their outputs are not stored.
     // 8 rows x 128 bytes per LDS-direct load; the wave's rows are 16 pw .. 16 pw + 15
-    const int c_st = (lane & 7) ^ swz(lane >> 3);
     const uint32_t lat_last = uint32_t(2 * p.kv - 16);
-    const uint32_t rope_off = p.rope ? uint32_t(2 * p.kv + min(16 * c_st, 2 * p.rope - 16)) : 0u;
     auto stage_bf16 = [&](gbytes row_ptr, uint16_t* buf, int cb, int half) {
-        const uint32_t off = cb < 8 ? min(uint32_t(cb * 128 + c_st * 16), lat_last) : rope_off;
+        const int c_st = (lane & 7) ^ swz(8 * half + (lane >> 3));
+        const uint32_t off = cb < 8 ? min(uint32_t(cb * 128 + c_st * 16), lat_last)
+                                    : p.rope ? uint32_t(2 * p.kv + min(16 * c_st, 2 * p.rope - 16)) : 0u;
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row_ptr + off),
                                          (lds_void*)(buf + cb * kBlockElems + (16 * pw + 8 * half) * 64), 16, 0, 0);
     };
@@ -260,13 +301,12 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
         for (int u = 0; u < kSteps; ++u)
             qf[t][u] = *reinterpret_cast<const i32x4*>(kv_b + (u >> 1) * kBlockElems + 16 * t * 64 + (u & 1 ? fr1 : fr0));
     lds_sync();
-    // 64 rows of Q fill 288 registers: most of them in the accumulation half of the file, which MFMA operands may
-    // come from, and said so (the compiler keeps them there as spills otherwise, 288 copies a chunk)
+    // Q in the accumulation half of the register file, which MFMA operands may come from
 #pragma unroll
     for (int t = 0; t < HT; ++t)
 #pragma unroll
         for (int u = 0; u < kSteps; ++u)
-            if (t * kSteps + u < kQInAcc) asm("" : "+a"(qf[t][u]));
+            asm("" : "+a"(qf[t][u]));
     if constexpr (E4M3) load_raw(rows_next, 0);
 
     // positions that a row sees: those below its limit
@@ -295,8 +335,8 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
     const int a4 = j >> 2, b4 = j & 3;
     // value fragments: rows 8 g + a4 and + 4 of a k-step, piece 2 pw + b4 / 2 of column block i
     const int vrow = 8 * g + a4;
-    const int v_lo = vrow * 64 + (((2 * pw + (b4 >> 1)) ^ swz(a4)) << 3) + 4 * (b4 & 1);
-    const int v_hi = (vrow + 4) * 64 + (((2 * pw + (b4 >> 1)) ^ swz(a4 + 4)) << 3) + 4 * (b4 & 1);
+    const int v_lo = vrow * 64 + (((2 * pw + (b4 >> 1)) ^ swz(vrow)) << 3) + 4 * (b4 & 1);
+    const int v_hi = (vrow + 4) * 64 + (((2 * pw + (b4 >> 1)) ^ swz(vrow + 4)) << 3) + 4 * (b4 & 1);
 
     auto chunk = [&](const uint16_t* cur, uint16_t* nxt, int ck) {
         const int c0 = start_of(ck);
@@ -307,7 +347,8 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
             rp[0] = ptr_of(rows_next, 16 * pw + (lane >> 3));
             rp[1] = ptr_of(rows_next, 16 * pw + 8 + (lane >> 3));
         }
-        const int rows_after = row_of(start_of(ck + 2));
+        const int page_after = page_of(start_of(ck + 2));
+        int rows_after = -1;
 
         // ---- S^T, K fragments read kAhead steps ahead, the next chunk's loads between the steps
         f32x4 s[HT];
@@ -440,14 +481,20 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
             if constexpr (E4M3) {
                 // the second half of the next chunk's rows; then the loads of the one after it
                 if (v % 3 == 2 && v < 15) commit_at(nxt, 1, v / 3);
-                if (v == 15) load_raw(rows_after, 0);
+                if (v == 15) {
+                    rows_after = row_at(page_after, start_of(ck + 2));
+                    load_raw(rows_after, 0);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        // the next chunk has landed, and every wave is done with this one and with P
+        if constexpr (!E4M3) {
+            __builtin_amdgcn_s_waitcnt(0);
+            rows_after = row_at(page_after, start_of(ck + 2));
+        }
         rows_cur = rows_next;
         rows_next = rows_after;
-        // the next chunk has landed, and every wave is done with this one and with P
-        if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);
         lds_sync();
     };
     for (int ck = 0; ck < nchunks; ck += 2) {
@@ -466,28 +513,424 @@ __device__ __forceinline__ void batch_block(const BatchParams& p, const Item it,
     for (int t = 0; t < HT; ++t) {
         const int row = 16 * t + j;
         const float lsum = ((red[row] + red[HB + row]) + red[2 * HB + row]) + red[3 * HB + row];
-        if (row >= it.nrows) continue;
-        const int r = it.r0 + row;
-        if (p.direct) {
-            // a row that sees nothing is zeros
-            const float scl = lsum == 0.f ? 0.f : 1.f / lsum;
-            uint16_t* dst = p.out + row_offset(r, p.T, p.H, p.sob, p.sot, p.ldo) + 4 * g;
-#pragma unroll
-            for (int i = 0; i < kTilesW; ++i) {
-                const int c = 16 * (pw + 4 * i);
-                const f32x4 v = o[i][t] * scl;
-                if (c < p.kv) *reinterpret_cast<uint2*>(dst + c) = uint2{pack2(v[0], v[1]), pack2(v[2], v[3])};
-            }
+        store_row<HT>(p, it, row, pw, g, o, t, m_ref[t], lsum);
+    }
+}
+
+// A tile of 64 rows over a span, in chunks of 32 positions, software-pipelined: while chunk i's scores go through
+// the softmax (vector units), the matrix cores work on chunk i + 1's, and chunk i + 3 is on its way into a ring of four
+// buffers [9 column blocks][32 rows][8 pieces].
+//  * S^T of a chunk: wave w takes positions 16 (w % 2) .. + 15 and half of the columns (9 of 18 steps), for all 64
+//    rows: half of Q in its registers (64 rows x 288 columns), every key fragment read from LDS once and used by four MFMAs.
+//    The two halves of a sum meet through LDS: each wave finishes two of the four row tiles.
+//  * Per chunk: QK(i + 1) with softmax(i), barrier (P, maxima and half sums are there), PV(i), barrier (chunk i
+//    + 2 is there, chunk i's buffer is free).
+template <bool E4M3>
+__device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, uint16_t* const b0, uint16_t* const b1,
+                                           uint16_t* const b2, uint16_t* const b3, uint16_t* const pbuf, float* const xbuf,
+                                           float* const red, int* const flags) {
+    constexpr int kPos = 32, kBlk = kPos * 64;
+    constexpr int kHalf = kSteps / 2, kAheadK = 4, kAheadV = 4, kPitch = kPos + 8;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;
+    const int pg = wave & 1, dh = wave >> 1;
+    const int g = lane >> 4, j = lane & 15;
+    const int n = (it.end - it.begin + kPos - 1) / kPos;
+    const gbytes cache = (gbytes)p.cache;
+    const gbytes zero_row = opaque_zero_row();
+
+    // the walk, as in narrow_block
+    const int first = n ? int(uint32_t(it.tile) * uint32_t(n) / uint32_t(it.tiles)) : 0;
+    auto start_of = [&](int ck) {
+        int c = ck + first;
+        c = c >= n ? c - n : c;
+        return ck < n ? it.begin + c * kPos : it.end;
+    };
+    auto page_of = [&](int c0) { return it.table[min(c0 + (lane & 31), max(it.end - 1, 0)) >> p.page_shift]; };
+    auto row_at = [&](int page, int c0) {
+        const int pos = c0 + (lane & 31);
+        const int r = (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+        return pos < it.end && uint32_t(page) < uint32_t(p.n_pages) ? r : -1;
+    };
+    auto row_of = [&](int c0) { return row_at(page_of(c0), c0); };
+    auto ptr_of = [&](int rows, int row) {
+        const int r = __builtin_amdgcn_ds_bpermute(row << 2, rows);
+        return r < 0 ? zero_row : cache + int64_t(r) * p.ld;
+    };
+    auto present_of = [&](int rows) { return uint32_t(__builtin_amdgcn_ballot_w64(rows >= 0)); };
+    // bf16 rows: wave w stages rows 8 w .. 8 w + 7, a column block a load
+    const int c_st = (lane & 7) ^ swz(8 * wave + (lane >> 3));
+    const uint32_t lat_last = uint32_t(2 * p.kv - 16);
+    const uint32_t rope_off = p.rope ? uint32_t(2 * p.kv + min(16 * c_st, 2 * p.rope - 16)) : 0u;
+    auto stage_bf16 = [&](gbytes row_ptr, uint16_t* buf, int cb) {
+        const uint32_t off = cb < 8 ? min(uint32_t(cb * 128 + (c_st ^ (cb & 1)) * 16), lat_last) : rope_off;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row_ptr + off),
+                                         (lds_void*)(buf + cb * kBlk + 8 * wave * 64), 16, 0, 0);
+    };
+    // 8-bit rows: a thread takes pieces 8 i + (tid & 7) of row tid / 8
+    u32x4 code0, code1, code2, code3, code_scale, code_rope;
+    const int l8 = tid & 7, r8 = tid >> 3, f8 = swz(r8), hi8 = l8 >> 2;
+    const uint32_t rope8 = p.rope ? uint32_t(p.kv + kScaleBytes + min(16 * l8, 2 * p.rope - 16)) : 0u;
+    auto load_raw = [&](int rows) {
+        const gbytes src = ptr_of(rows, r8);
+        const uint32_t last = uint32_t(p.kv - 16);
+        code0 = load16(src + min(uint32_t(16 * l8), last));
+        code1 = load16(src + min(uint32_t(16 * l8 + 128), last));
+        code2 = load16(src + min(uint32_t(16 * l8 + 256), last));
+        code3 = load16(src + min(uint32_t(16 * l8 + 384), last));
+        code_scale = load16(src + p.kv);
+        code_rope = load16(src + rope8);
+    };
+    // Piece l8 + 8 i is pieces 2 (l8 % 4) and + 1 of column block 2 i + l8 / 4; with the odd blocks' slots the eight
+    // lanes of a row write eight different ones.
+    const int w8_lo = r8 * 64 + hi8 * kBlk + (((2 * (l8 & 3) + hi8) ^ f8) << 3), w8_up = w8_lo ^ 8;
+    const int w8_rope = r8 * 64 + 8 * kBlk + ((l8 ^ f8) << 3);
+    float c_scale = 0.f;
+    uint2 c_a, c_b, c_c, c_d;
+    // part i, in five slices; part 4 (RoPE's) in one
+    auto commit = [&](uint16_t* dst, auto part, int slice) {
+        constexpr int i = decltype(part)::value;
+        if constexpr (i == 4) {
+            if (slice == 0) *reinterpret_cast<u32x4*>(dst + w8_rope) = code_rope;
         } else {
-            const int64_t at = int64_t(it.slot) * p.rows + r;
-            float* const dst = p.part_o + at * p.kv + 4 * g;
-#pragma unroll
-            for (int i = 0; i < kTilesW; ++i) {
-                const int c = 16 * (pw + 4 * i);
-                if (c < p.kv) __builtin_nontemporal_store(o[i][t], reinterpret_cast<f32x4*>(dst + c));
+            const u32x4 q = i == 0 ? code0 : i == 1 ? code1 : i == 2 ? code2 : code3;
+            if (slice == 0) c_scale = 16 * (l8 + 8 * i) < p.kv ? scale_of(code_scale[i] >> (8 * (l8 >> 1))) : 0.f;
+            if (slice == 1) {
+                c_a = dequant4(q[0], c_scale);
+                c_b = dequant4(q[1], c_scale);
             }
-            if (pw == 0 && g == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = float2{m_ref[t], lsum};
+            if (slice == 2) *reinterpret_cast<u32x4*>(dst + 2 * i * kBlk + w8_lo) = u32x4{c_a.x, c_a.y, c_b.x, c_b.y};
+            if (slice == 3) {
+                c_c = dequant4(q[2], c_scale);
+                c_d = dequant4(q[3], c_scale);
+            }
+            if (slice == 4) *reinterpret_cast<u32x4*>(dst + 2 * i * kBlk + w8_up) = u32x4{c_c.x, c_c.y, c_d.x, c_d.y};
         }
+    };
+    auto commit_at = [&](uint16_t* buf, int part, int slice) {       // constants where it is called
+        if (part == 0) commit(buf, std::integral_constant<int, 0>{}, slice);
+        if (part == 1) commit(buf, std::integral_constant<int, 1>{}, slice);
+        if (part == 2) commit(buf, std::integral_constant<int, 2>{}, slice);
+        if (part == 3) commit(buf, std::integral_constant<int, 3>{}, slice);
+        if (part == 4) commit(buf, std::integral_constant<int, 4>{}, slice);
+    };
+    auto stage_all = [&](int rows, uint16_t* buf) {
+        if constexpr (E4M3) {
+            load_raw(rows);
+#pragma unroll
+            for (int i = 0; i < 25; ++i) commit_at(buf, i / 5, i % 5);
+        } else {
+            const gbytes rp = ptr_of(rows, 8 * wave + (lane >> 3));
+#pragma unroll
+            for (int cb = 0; cb < kBlocks; ++cb) stage_bf16(rp, buf, cb);
+        }
+    };
+
+    // ---- chunks 0 and 1 to buffers 0 and 1; Q's rows to buffers 2 (rows 0 to 31) and 3, in the same layout
+    const int rows0 = row_of(start_of(0)), rows1 = row_of(start_of(1)), rows2 = row_of(start_of(2));
+    int page3 = page_of(start_of(3));
+    {
+        int64_t qo = -1;
+        if (lane < it.nrows) qo = row_offset(it.r0 + lane, p.T, p.H, p.sqb, p.sqt, p.ldq);
+        for (int ins = wave; ins < 8 * kBlocks; ins += kWavesB) {
+            const int cb = ins >> 3, grp = ins & 7;
+            const int row = 8 * grp + (lane >> 3);
+            const int c = (lane & 7) ^ swz(row) ^ (cb & 1);
+            const uint32_t lo = __builtin_amdgcn_ds_bpermute(row << 2, int(uint32_t(qo)));
+            const uint32_t hi = __builtin_amdgcn_ds_bpermute(row << 2, int(uint32_t(uint64_t(qo) >> 32)));
+            const int64_t o = int64_t((uint64_t(hi) << 32) | lo);
+            const bool ok = o >= 0 && (cb < 8 ? 64 * cb + 8 * c < p.kv : 8 * c < p.rope);
+            const gbytes src = ok ? (gbytes)(p.q + o + (cb < 8 ? 64 * cb : p.kv) + 8 * c) : zero_row;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             (lds_void*)((grp < 4 ? b2 : b3) + cb * kBlk + 8 * (grp & 3) * 64), 16, 0, 0);
+        }
+    }
+    stage_all(rows0, b0);
+    stage_all(rows1, b1);
+    uint32_t here0 = present_of(rows0), here1 = present_of(rows1), here2 = present_of(rows2), here3 = 0;
+    __builtin_amdgcn_s_waitcnt(0);
+    lds_sync();
+    // The wave's k-steps are 9 dh + u: row j of a 16-row tile, piece 4 (step % 2) + g of column block step / 2, which is
+    // (u / 2) + (0 or, with dh, 4 for even u and 5 for odd); odd blocks have the other slots.
+    const int fj = swz(j);
+    const int fr0 = j * 64 + ((g ^ fj) << 3), fr1 = j * 64 + (((4 + g) ^ fj) << 3);
+    const int fr_even = dh ? fr1 + 4 * kBlk : fr0, fr_odd = dh ? (fr0 ^ 8) + 5 * kBlk : fr1;
+    auto frag = [&](const uint16_t* rows16, int u) {
+        const int at = u & 1 ? fr_odd : fr_even;
+        return *reinterpret_cast<const i32x4*>(rows16 + ((u >> 1) & 1 ? at ^ 8 : at) + (u >> 1) * kBlk);
+    };
+    i32x4 qf[4][kHalf];
+    // local tile t is row tile (t + 2 dh) % 4: the wave finishes its local tiles 0 and 1
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < kHalf; ++u) qf[t][u] = frag(((t < 2) == (dh == 0) ? b2 : b3) + 1024 * (t & 1), u);
+    lds_sync();
+    // Q in the accumulation half of the register file, which MFMA operands may come from (said so: the compiler
+    // keeps it there as spills otherwise, with a copy before every use)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < kHalf; ++u) asm("" : "+a"(qf[t][u]));
+    stage_all(rows2, b2);
+    if constexpr (E4M3) {
+        const int rows3 = row_at(page3, start_of(3));
+        here3 = present_of(rows3);
+        load_raw(rows3);
+    }
+
+    const int all_see = it.seq >= 0 ? it.len - (p.T - 1) : it.end;    // positions below it are seen by every row
+    int limit[2];                                                     // of the wave's own two row tiles
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        limit[k] = it.end;
+        if (it.seq >= 0 && p.T > 1) {
+            const int tok = (it.r0 + 32 * dh + 16 * k + j - it.seq * p.T * p.H) / p.H;
+            limit[k] = min(it.end, it.len - (p.T - 1 - tok));
+        }
+    }
+
+    f32x4 o[kTilesW][4];      // O^T: lane (g, j) holds columns 16 (wave + 4 i) + 4 g .. + 3 of row 16 t + j
+#pragma unroll
+    for (int i = 0; i < kTilesW; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_ref[4], l_acc[2] = {0.f, 0.f};     // references of every row tile, sums of the wave's own
+#pragma unroll
+    for (int t = 0; t < 4; ++t) m_ref[t] = -INFINITY;
+    const int a4 = j >> 2, b4 = j & 3;
+    const int vrow = 8 * g + a4;
+    const int v_lo = vrow * 64 + (((2 * wave + (b4 >> 1)) ^ swz(vrow)) << 3) + 4 * (b4 & 1);
+    const int v_hi = (vrow + 4) * 64 + (((2 * wave + (b4 >> 1)) ^ swz(vrow + 4)) << 3) + 4 * (b4 & 1);
+    float* const x_mine = xbuf + (wave * 2 * 64 + lane) * 4;
+    const float* const x_other = xbuf + ((wave ^ 2) * 2 * 64 + lane) * 4;
+
+    f32x4 sp[4], s[2];
+    // QK of a chunk: one step of the wave's nine
+    auto k_frag = [&](const uint16_t* buf, int u) { return frag(buf + 1024 * pg, u); };
+    auto qk_mfma = [&](const i32x4 (&kf)[kAheadK], int u, int t) {
+        sp[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[u % kAheadK]), as_bf16x8(qf[t][u]),
+                                                        u ? sp[t] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+    };
+    auto x_write = [&]() {
+        *reinterpret_cast<f32x4*>(x_mine) = sp[2];
+        *reinterpret_cast<f32x4*>(x_mine + 256) = sp[3];
+    };
+    // The finished scores of the wave's own two tiles in log2 units, masked where some row does not see every position.
+    auto x_load = [&](f32x4 (&x)[2]) {
+        // local tiles 0 and 1 of this wave are tiles 2 and 3 of the other
+        x[0] = *reinterpret_cast<const f32x4*>(x_other);
+        x[1] = *reinterpret_cast<const f32x4*>(x_other + 256);
+    };
+    const int at = 16 * pg + 4 * g;
+    auto finish = [&](const f32x4 (&x)[2], uint32_t here, int c0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) s[k] = (sp[k] + x[k]) * p.scale_log2;
+        if (here != ~0u || c0 + kPos > all_see) {
+            const uint32_t bits = here >> at;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[k][e] = ((bits >> e) & 1u) && c0 + at + e < limit[k] ? s[k][e] : -INFINITY;
+        }
+    };
+    if (n > 0) {
+        i32x4 kf[kAheadK];
+#pragma unroll
+        for (int u = 0; u < kAheadK; ++u) kf[u] = k_frag(b0, u);
+#pragma unroll
+        for (int u = 0; u < kHalf; ++u) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) qk_mfma(kf, u, t);
+            if (u + kAheadK < kHalf) kf[u % kAheadK] = k_frag(b0, u + kAheadK);
+        }
+        x_write();
+        lds_sync();
+        f32x4 x[2];
+        x_load(x);
+        finish(x, here0, start_of(0));
+        if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);     // (chunk 2)
+        lds_sync();
+    }
+
+    // chunk i lies in cur, i + 1 in next; fill, chunk i - 1's, takes chunk i + 3
+    auto step = [&](auto last_c, int i, const uint16_t* const cur, const uint16_t* const next, uint16_t* const fill) {
+        constexpr bool LAST = decltype(last_c)::value;
+        gbytes rp = zero_row;
+        if constexpr (!E4M3) {
+            const int rows3 = row_at(page3, start_of(i + 3));
+            here3 = present_of(rows3);
+            rp = ptr_of(rows3, 8 * wave + (lane >> 3));
+        }
+        const int page4 = page_of(start_of(i + 4));
+        uint32_t here4 = 0;
+        auto v_frag = [&](int v) {
+            const uint16_t* base = cur + v * kBlk;
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + (v & 1 ? v_lo ^ 8 : v_lo)));
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(base + (v & 1 ? v_hi ^ 8 : v_hi)));
+            const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
+            return i32x4{int(ulo.x), int(ulo.y), int(uhi.x), int(uhi.y)};
+        };
+        auto p_frag = [&](int t) { return *reinterpret_cast<const i32x4*>(pbuf + (16 * t + j) * kPitch + 8 * g); };
+
+        // ---- softmax(i) beside QK(i + 1).  An MFMA takes the matrix core 16 cycles, three vector instructions' time,
+        // and a wave issues in order: the softmax is cut into slices, one after each MFMA, kept there by scheduling
+        // barriers (left to itself the compiler runs one after the other).
+        float mx[2], mr[2], lc[2], pv[2][4];
+        bool need = false;
+        auto soft_max = [&](int k, int slice) {
+            if (slice == 0) mx[k] = fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3]));
+            if (slice == 1) mx[k] = rows_max32(mx[k]);
+            if (slice == 2) mx[k] = rows_max16(mx[k]);
+        };
+        auto reference = [&](int k) {
+            const float m = dh ? m_ref[2 + k] : m_ref[k];
+            need |= !(mx[k] <= m + kLazy);
+            mr[k] = m == -INFINITY ? 0.f : m;      // (a row that has seen nothing: 2^(-inf - 0) = 0)
+        };
+        auto put_p = [&](int k) {
+            *reinterpret_cast<uint2*>(pbuf + (32 * dh + 16 * k + j) * kPitch + at) =
+                uint2{pack2(pv[k][0], pv[k][1]), pack2(pv[k][2], pv[k][3])};
+        };
+        i32x4 pf[4], vf[kAheadV];
+        auto soft = [&](int m) {
+            if (m < 2) reference(m);
+            if (m >= 2 && m < 10) pv[(m - 2) / 4][(m - 2) % 4] = __builtin_amdgcn_exp2f(s[(m - 2) / 4][(m - 2) % 4] - mr[(m - 2) / 4]);
+            if (m == 10 || m == 12) lc[(m - 10) / 2] = (pv[(m - 10) / 2][0] + pv[(m - 10) / 2][1]) + (pv[(m - 10) / 2][2] + pv[(m - 10) / 2][3]);
+            if (m == 11 || m == 13) put_p((m - 11) / 2);
+            // (every lane of a row writes the same maximum, every lane of a wave the same flag: no branch)
+            if (m == 14 || m == 15) red[pg * 64 + 32 * dh + 16 * (m - 14) + j] = mx[m - 14];
+            if (m == 16) flags[wave] = __builtin_amdgcn_ballot_w64(need) != 0 ? 1 : 0;
+            if (m >= 28 && m % 2 == 0 && (m - 28) / 2 < kAheadV) vf[(m - 28) / 2] = v_frag((m - 28) / 2);
+        };
+        i32x4 kf[kAheadK];
+        if constexpr (!LAST) {
+#pragma unroll
+            for (int u = 0; u < kAheadK; ++u) kf[u] = k_frag(next, u);
+        }
+#pragma unroll
+        for (int q = 0; q < 6; ++q) soft_max(q & 1, q >> 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int m = 0; m < 4 * kHalf; ++m) {
+            const int u = m / 4, t = m % 4;
+            if constexpr (!LAST) {
+                qk_mfma(kf, u, t);
+                if (t == 3 && u + kAheadK < kHalf) kf[u % kAheadK] = k_frag(next, u + kAheadK);
+                if constexpr (!E4M3) {
+                    if (m % 8 == 3) stage_bf16(rp, fill, m / 8);
+                }
+            }
+            soft(m);
+            if constexpr (!LAST) __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!LAST) x_write();
+        lds_sync();
+        const i32x4 f0 = *reinterpret_cast<const i32x4*>(flags);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) pf[t] = p_frag(t);
+        f32x4 x[2];
+        if constexpr (!LAST) x_load(x);
+        if ((f0[0] | f0[1] | f0[2] | f0[3]) != 0) {
+            // a reference moves (every wave reads the same maxima): the output rescaled, P written again
+            float alpha[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float mc = fmaxf(red[16 * t + j], red[64 + 16 * t + j]);
+                alpha[t] = 1.f;
+                if (mc > m_ref[t] + kLazy) {
+                    alpha[t] = (m_ref[t] == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m_ref[t] - mc);
+                    m_ref[t] = mc;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) l_acc[k] *= dh ? alpha[2 + k] : alpha[k];
+#pragma unroll
+            for (int q = 0; q < kTilesW; ++q)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) o[q][t] *= alpha[t];
+            lds_sync();                  // (every wave has read the P that is written again)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                reference(k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pv[k][e] = __builtin_amdgcn_exp2f(s[k][e] - mr[k]);
+                lc[k] = (pv[k][0] + pv[k][1]) + (pv[k][2] + pv[k][3]);
+                put_p(k);
+            }
+            lds_sync();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) pf[t] = p_frag(t);
+        }
+        l_acc[0] += lc[0];
+        l_acc[1] += lc[1];
+
+        // ---- PV(i), and (the rest of) the staging of chunk i + 3 in slices beside it
+#pragma unroll
+        for (int m = 0; m < 4 * kTilesW; ++m) {
+            const int v = m / 4, t = m % 4;
+            if constexpr (!LAST && E4M3) {
+                // (the first slices before the first MFMA, which waits for P)
+                if (m == 0) {
+                    commit_at(fill, 0, 0);
+                    commit_at(fill, 0, 1);
+                    commit_at(fill, 0, 2);
+                    commit_at(fill, 0, 3);
+                }
+            }
+            o[v][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[v % kAheadV]), as_bf16x8(pf[t]), o[v][t], 0, 0, 0);
+            if (t == 3 && v + kAheadV < kTilesW) vf[v % kAheadV] = v_frag(v + kAheadV);
+            if constexpr (!LAST) {
+                if constexpr (E4M3) {
+                    if (m == 0) commit_at(fill, 0, 4);
+                    if (m >= 2 && m < 17) commit_at(fill, 1 + (m - 2) / 5, (m - 2) % 5);
+                    if (m == 17) commit_at(fill, 4, 0);
+                    if (m == 18) {
+                        const int rows4 = row_at(page4, start_of(i + 4));
+                        here4 = present_of(rows4);
+                        load_raw(rows4);
+                    }
+                } else if (m % 7 == 4) {
+                    stage_bf16(rp, fill, 5 + m / 7);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!LAST) finish(x, here1, start_of(i + 1));
+        here0 = here1;
+        here1 = here2;
+        here2 = here3;
+        here3 = here4;
+        page3 = page4;
+        if constexpr (!LAST) {
+            // chunk i + 2 has landed (chunk i + 3's nine loads may be on their way), and every wave is done with chunk i
+            if constexpr (!E4M3) attn::wait_vm<kBlocks>();
+            lds_sync();
+        }
+    };
+    // (four buffers by name, so that the compiler sees which of them a staging load writes)
+    for (int i = 0; i + 1 < n; i += 4) {
+        step(std::false_type{}, i, b0, b1, b3);
+        if (i + 2 < n) step(std::false_type{}, i + 1, b1, b2, b0);
+        if (i + 3 < n) step(std::false_type{}, i + 2, b2, b3, b1);
+        if (i + 4 < n) step(std::false_type{}, i + 3, b3, b0, b2);
+    }
+    if (n > 0) {
+        const int last = (n - 1) & 3;
+        step(std::true_type{}, n - 1, last == 0 ? b0 : last == 1 ? b1 : last == 2 ? b2 : b3, nullptr, nullptr);
+    }
+
+    // ---- the rows' sums: a wave's four lanes of a row, then the two position groups
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float lw = cols4_sum(l_acc[k]);
+        if (g == 0) red[128 + pg * 64 + 32 * dh + 16 * k + j] = lw;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int row = 16 * t + j;
+        store_row<4>(p, it, row, wave, g, o, t, m_ref[t], red[128 + row] + red[192 + row]);
     }
 }
 
@@ -499,23 +942,17 @@ __device__ __forceinline__ int xcd_run(int b, int items) {
     return v < items ? v : -1;
 }
 
-// HT: row tiles of an own item (and of the prefix's where its rows fit one such tile).
-template <int HT, bool E4M3>
-__global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchParams p) {
-    __shared__ __attribute__((aligned(128))) uint16_t kv_a[kBlocks * kBlockElems];
-    __shared__ __attribute__((aligned(128))) uint16_t kv_b[kBlocks * kBlockElems];
-    __shared__ __attribute__((aligned(16))) uint16_t pbuf[kChunk * kPPitchB];
-    __shared__ __attribute__((aligned(16))) float red[kWavesB * kChunk];
-    __shared__ __attribute__((aligned(16))) int flags[4];
+// The item of a workgroup, in tiles of TR rows; false: none.
+template <int TR>
+__device__ __forceinline__ bool item_of(const BatchParams& p, Item* out) {
     const int bid = static_cast<int>(blockIdx.x);
     Item it;
     if (bid < p.pre_grid) {
         const int v = xcd_run(bid, p.pre_items);
-        if (v < 0) return;
+        if (v < 0) return false;
         const int sp = v / p.pre_tiles, tile = v - sp * p.pre_tiles;
-        const int tr = p.pre_wide ? 64 : 16 * HT;
-        it.r0 = tile * tr;
-        it.nrows = min(tr, p.rows - it.r0);
+        it.r0 = tile * TR;
+        it.nrows = min(TR, p.rows - it.r0);
         it.seq = -1;
         it.table = p.prefix_pages;
         it.begin = sp * p.pre_span;
@@ -526,12 +963,12 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchP
         it.tiles = p.pre_tiles;
     } else {
         const int v = xcd_run(bid - p.pre_grid, p.own_items);
-        if (v < 0) return;
+        if (v < 0) return false;
         const int unit = v / p.own_tiles, tile = v - unit * p.own_tiles;
         const int b = unit / p.own_spans, sp = unit - b * p.own_spans;
         const int th = p.T * p.H;
-        it.r0 = b * th + tile * 16 * HT;
-        it.nrows = min(16 * HT, th - tile * 16 * HT);
+        it.r0 = b * th + tile * TR;
+        it.nrows = min(TR, th - tile * TR);
         it.seq = b;
         it.table = p.pages + b * p.ld_pages;
         it.len = max(0, min(p.lens[b], p.max_len));
@@ -540,11 +977,37 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchP
         it.slot = p.pre_spans + sp;
         it.tile = tile;
         it.tiles = p.own_tiles;
-        if (it.begin >= it.end && !p.direct) return;     // the merge knows how many spans a sequence has
+        if (it.begin >= it.end && !p.direct) return false;     // the merge knows how many spans a sequence has
         it.end = max(it.end, it.begin);
     }
-    if (HT < 4 && it.seq < 0 && p.pre_wide) batch_block<4, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
-    else batch_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+    *out = it;
+    return true;
+}
+
+template <int HT, bool E4M3>
+__global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchParams p) {
+    __shared__ __attribute__((aligned(128))) uint16_t kv_a[kBlocks * kBlockElems];
+    __shared__ __attribute__((aligned(128))) uint16_t kv_b[kBlocks * kBlockElems];
+    __shared__ __attribute__((aligned(16))) uint16_t pbuf[16 * HT * kPPitchB];
+    __shared__ __attribute__((aligned(16))) float red[kWavesB * 16 * HT];
+    __shared__ __attribute__((aligned(16))) int flags[4];
+    Item it;
+    if (item_of<16 * HT>(p, &it)) narrow_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+}
+
+template <bool E4M3>
+__global__ __launch_bounds__(kThreadsB) void attention_batch_wide_kernel(const BatchParams p) {
+    constexpr int kElems = kBlocks * 32 * 64;
+    __shared__ __attribute__((aligned(128))) uint16_t b0[kElems];
+    __shared__ __attribute__((aligned(128))) uint16_t b1[kElems];
+    __shared__ __attribute__((aligned(128))) uint16_t b2[kElems];
+    __shared__ __attribute__((aligned(128))) uint16_t b3[kElems];
+    __shared__ __attribute__((aligned(16))) uint16_t pbuf[64 * (32 + 8)];
+    __shared__ __attribute__((aligned(16))) float xbuf[4 * 2 * 64 * 4];
+    __shared__ __attribute__((aligned(16))) float red[256];
+    __shared__ __attribute__((aligned(16))) int flags[4];
+    Item it;
+    if (item_of<64>(p, &it)) wide_block<E4M3>(p, it, b0, b1, b2, b3, pbuf, xbuf, red, flags);
 }
 
 // out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), the prefix's spans, then the sequence's own.  A block
@@ -594,8 +1057,8 @@ __global__ __launch_bounds__(kMergeT) void attention_batch_merge_kernel(const Ba
 // The partition.
 // ---------------------------------------------------------------------------------------------
 struct BatchPlan {
-    int ht = 1;                        // row tiles of an own item
-    int pre_tiles = 0, pre_spans = 0, pre_span = kChunk, pre_wide = 0;
+    int ht = 1;                        // 16-row tiles per workgroup: 1, 2 or 4
+    int pre_tiles = 0, pre_spans = 0, pre_span = kChunk;
     int own_tiles = 1, own_spans = 0, own_span = kChunk;
     int64_t pre_items = 0, own_items = 0, grid = 0;
     size_t ws_bytes = 0;
@@ -606,18 +1069,17 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Time of a chunk in a tile of 16 ht rows, relative to 16 rows.
 int chunk_cost(int ht) { return ht == 4 ? 16 : ht == 2 ? 11 : 10; }
 
-void plan_batch(const nmm_latent_attn_batch& a, BatchPlan* out) {
+// The partition in tiles of 16 ht rows, and an estimate of its time.
+int64_t plan_tiles(const nmm_latent_attn_batch& a, int ht, BatchPlan* out) {
     constexpr int64_t kCus = 256;
     BatchPlan q;
+    q.ht = ht;
     const int64_t th = a.tokens * a.heads, rows = a.batch * th;
-    q.ht = th <= 16 ? 1 : th <= 32 ? 2 : 4;
-    q.own_tiles = static_cast<int>(cdiv(th, 16 * q.ht));
+    q.own_tiles = static_cast<int>(cdiv(th, 16 * ht));
     const int64_t pc = cdiv(a.prefix_len, kChunk), oc = cdiv(a.max_len, kChunk);
-    q.pre_wide = rows > 16 * q.ht ? 1 : 0;
-    const int pre_ht = q.pre_wide ? 4 : q.ht;
-    q.pre_tiles = pc ? static_cast<int>(cdiv(rows, 16 * pre_ht)) : 0;
+    q.pre_tiles = pc ? static_cast<int>(cdiv(rows, 16 * ht)) : 0;
     const int64_t own_groups = oc ? a.batch * q.own_tiles : 0;
-    const int cp = chunk_cost(pre_ht), co = chunk_cost(q.ht);
+    const int cost = chunk_cost(ht);
     // For each number of prefix spans, own spans of about the same time; the pair with the least estimated
     // time: the longest item where one round of the CUs holds all, else the CUs' share and a last item, and
     // the merge's reads.
@@ -628,12 +1090,12 @@ void plan_batch(const nmm_latent_attn_batch& a, BatchPlan* out) {
         int64_t ps = 0, os = 0;
         if (pc) {
             ps = cdiv(pc, cdiv(pc, i));
-            if (oc) os = std::min<int64_t>({oc, kMaxSlots - ps, cdiv(oc * co, cdiv(pc, ps) * cp)});
+            if (oc) os = std::min<int64_t>({oc, kMaxSlots - ps, cdiv(oc, cdiv(pc, ps))});
         } else {
             os = i;
         }
         if (os) os = cdiv(oc, cdiv(oc, os));
-        const int64_t ip = ps ? cdiv(pc, ps) * cp : 0, io = os ? cdiv(oc, os) * co : 0;
+        const int64_t ip = ps ? cdiv(pc, ps) * cost : 0, io = os ? cdiv(oc, os) * cost : 0;
         const int64_t items = ps * q.pre_tiles + os * own_groups;
         const int64_t work = ps * q.pre_tiles * ip + os * own_groups * io;
         int64_t t = items <= kCus ? std::max(ip, io) : work / kCus + std::max(ip, io);
@@ -658,6 +1120,18 @@ void plan_batch(const nmm_latent_attn_batch& a, BatchPlan* out) {
     const int64_t slots = q.pre_spans + q.own_spans;
     if (slots > 1) q.ws_bytes = size_t(kTicketBytes) + size_t(slots) * size_t(rows) * (size_t(a.cache.kv_lora) + 2) * 4;
     *out = q;
+    return best;
+}
+
+// A sequence's own positions take the smallest tile that holds its rows; with a prefix, whose rows are all
+// sequences', tiles of 64 for both where that is estimated to be faster.
+void plan_batch(const nmm_latent_attn_batch& a, BatchPlan* out) {
+    const int64_t th = a.tokens * a.heads;
+    const int ht = th <= 16 ? 1 : th <= 32 ? 2 : 4;
+    const int64_t t = plan_tiles(a, ht, out);
+    if (ht == 4 || a.prefix_len == 0 || a.batch * th <= 16 * ht) return;
+    BatchPlan wide;
+    if (plan_tiles(a, 4, &wide) < t) *out = wide;
 }
 
 constexpr int64_t kLim = int64_t(1) << 31;
@@ -749,7 +1223,6 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
     p.pre_items = static_cast<int>(q.pre_items);
     p.pre_grid = static_cast<int>(cdiv(q.pre_items, 8) * 8);
     p.own_items = static_cast<int>(q.own_items);
-    p.pre_wide = q.pre_wide;
     p.own_tiles = q.own_tiles; p.own_spans = q.own_spans; p.own_span = q.own_span;
     p.direct = q.pre_spans + q.own_spans == 1 ? 1 : 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -763,8 +1236,8 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
             if (q8) hipLaunchKernelGGL((attention_batch_kernel<2, true>), grid, block, 0, s, p);
             else hipLaunchKernelGGL((attention_batch_kernel<2, false>), grid, block, 0, s, p);
         } else {
-            if (q8) hipLaunchKernelGGL((attention_batch_kernel<4, true>), grid, block, 0, s, p);
-            else hipLaunchKernelGGL((attention_batch_kernel<4, false>), grid, block, 0, s, p);
+            if (q8) hipLaunchKernelGGL((attention_batch_wide_kernel<true>), grid, block, 0, s, p);
+            else hipLaunchKernelGGL((attention_batch_wide_kernel<false>), grid, block, 0, s, p);
         }
     }
     // no position anywhere: the merge of no slots writes the zeros
