@@ -523,8 +523,8 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
 //  * S^T of a chunk: wave w takes positions 16 (w % 2) .. + 15 and half of the columns (9 of 18 steps), for all 64
 //    rows: half of Q in its registers (64 rows x 288 columns), every key fragment read from LDS once and used by four MFMAs.
 //    The two halves of a sum meet through LDS: each wave finishes two of the four row tiles.
-//  * Per chunk: QK(i + 1) with softmax(i), barrier (P, maxima and half sums are there), PV(i), barrier (chunk i
-//    + 2 is there, chunk i's buffer is free).
+//  * Per chunk: QK(i + 1) with softmax(i), barrier (P, maxima, half sums and chunk i + 2 are there), PV(i),
+//    barrier (chunk i's buffer is free).
 template <bool E4M3>
 __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, uint16_t* const b0, uint16_t* const b1,
                                            uint16_t* const b2, uint16_t* const b3, uint16_t* const pbuf, float* const xbuf,
@@ -571,15 +571,19 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
     u32x4 code0, code1, code2, code3, code_scale, code_rope;
     const int l8 = tid & 7, r8 = tid >> 3, f8 = swz(r8), hi8 = l8 >> 2;
     const uint32_t rope8 = p.rope ? uint32_t(p.kv + kScaleBytes + min(16 * l8, 2 * p.rope - 16)) : 0u;
+    auto load_part = [&](gbytes src, int i) {
+        const uint32_t last = uint32_t(p.kv - 16);
+        if (i == 0) code0 = load16(src + min(uint32_t(16 * l8), last));
+        if (i == 1) code1 = load16(src + min(uint32_t(16 * l8 + 128), last));
+        if (i == 2) code2 = load16(src + min(uint32_t(16 * l8 + 256), last));
+        if (i == 3) code3 = load16(src + min(uint32_t(16 * l8 + 384), last));
+        if (i == 4) code_scale = load16(src + p.kv);
+        if (i == 5) code_rope = load16(src + rope8);
+    };
     auto load_raw = [&](int rows) {
         const gbytes src = ptr_of(rows, r8);
-        const uint32_t last = uint32_t(p.kv - 16);
-        code0 = load16(src + min(uint32_t(16 * l8), last));
-        code1 = load16(src + min(uint32_t(16 * l8 + 128), last));
-        code2 = load16(src + min(uint32_t(16 * l8 + 256), last));
-        code3 = load16(src + min(uint32_t(16 * l8 + 384), last));
-        code_scale = load16(src + p.kv);
-        code_rope = load16(src + rope8);
+#pragma unroll
+        for (int i = 0; i < 6; ++i) load_part(src, i);
     };
     // Piece l8 + 8 i is pieces 2 (l8 % 4) and + 1 of column block 2 i + l8 / 4; with the odd blocks' slots the eight
     // lanes of a row write eight different ones.
@@ -723,9 +727,8 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
         x[1] = *reinterpret_cast<const f32x4*>(x_other + 256);
     };
     const int at = 16 * pg + 4 * g;
-    auto finish = [&](const f32x4 (&x)[2], uint32_t here, int c0) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) s[k] = (sp[k] + x[k]) * p.scale_log2;
+    auto scale_scores = [&](const f32x4 (&x)[2], int k) { s[k] = (sp[k] + x[k]) * p.scale_log2; };
+    auto mask_scores = [&](uint32_t here, int c0) {
         if (here != ~0u || c0 + kPos > all_see) {
             const uint32_t bits = here >> at;
 #pragma unroll
@@ -734,8 +737,8 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
                 for (int e = 0; e < 4; ++e) s[k][e] = ((bits >> e) & 1u) && c0 + at + e < limit[k] ? s[k][e] : -INFINITY;
         }
     };
+    i32x4 kf[kAheadK];        // the next chunk's first key fragments
     if (n > 0) {
-        i32x4 kf[kAheadK];
 #pragma unroll
         for (int u = 0; u < kAheadK; ++u) kf[u] = k_frag(b0, u);
 #pragma unroll
@@ -748,13 +751,18 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
         lds_sync();
         f32x4 x[2];
         x_load(x);
-        finish(x, here0, start_of(0));
+        scale_scores(x, 0);
+        scale_scores(x, 1);
+        mask_scores(here0, start_of(0));
+#pragma unroll
+        for (int u = 0; u < kAheadK; ++u) kf[u] = k_frag(b1, u);
         if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);     // (chunk 2)
         lds_sync();
     }
 
-    // chunk i lies in cur, i + 1 in next; fill, chunk i - 1's, takes chunk i + 3
-    auto step = [&](auto last_c, int i, const uint16_t* const cur, const uint16_t* const next, uint16_t* const fill) {
+    // chunk i lies in cur, i + 1 in next, i + 2 in after; fill, chunk i - 1's, takes chunk i + 3
+    auto step = [&](auto last_c, int i, const uint16_t* const cur, const uint16_t* const next, const uint16_t* const after,
+                    uint16_t* const fill) {
         constexpr bool LAST = decltype(last_c)::value;
         gbytes rp = zero_row;
         if constexpr (!E4M3) {
@@ -794,29 +802,23 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
         };
         i32x4 pf[4], vf[kAheadV];
         auto soft = [&](int m) {
-            if (m < 2) reference(m);
-            if (m >= 2 && m < 10) pv[(m - 2) / 4][(m - 2) % 4] = __builtin_amdgcn_exp2f(s[(m - 2) / 4][(m - 2) % 4] - mr[(m - 2) / 4]);
-            if (m == 10 || m == 12) lc[(m - 10) / 2] = (pv[(m - 10) / 2][0] + pv[(m - 10) / 2][1]) + (pv[(m - 10) / 2][2] + pv[(m - 10) / 2][3]);
-            if (m == 11 || m == 13) put_p((m - 11) / 2);
+            if (m < 6) soft_max(m & 1, m >> 1);
+            if (m == 6 || m == 7) reference(m - 6);
+            if (m >= 8 && m < 16) pv[(m - 8) / 4][m % 4] = __builtin_amdgcn_exp2f(s[(m - 8) / 4][m % 4] - mr[(m - 8) / 4]);
+            if (m == 16 || m == 18) lc[(m - 16) / 2] = (pv[(m - 16) / 2][0] + pv[(m - 16) / 2][1]) + (pv[(m - 16) / 2][2] + pv[(m - 16) / 2][3]);
+            if (m == 17 || m == 19) put_p((m - 17) / 2);
             // (every lane of a row writes the same maximum, every lane of a wave the same flag: no branch)
-            if (m == 14 || m == 15) red[pg * 64 + 32 * dh + 16 * (m - 14) + j] = mx[m - 14];
-            if (m == 16) flags[wave] = __builtin_amdgcn_ballot_w64(need) != 0 ? 1 : 0;
+            if (m == 20 || m == 21) red[pg * 64 + 32 * dh + 16 * (m - 20) + j] = mx[m - 20];
+            if (m == 22) flags[wave] = __builtin_amdgcn_ballot_w64(need) != 0 ? 1 : 0;
             if (m >= 28 && m % 2 == 0 && (m - 28) / 2 < kAheadV) vf[(m - 28) / 2] = v_frag((m - 28) / 2);
         };
-        i32x4 kf[kAheadK];
-        if constexpr (!LAST) {
-#pragma unroll
-            for (int u = 0; u < kAheadK; ++u) kf[u] = k_frag(next, u);
-        }
-#pragma unroll
-        for (int q = 0; q < 6; ++q) soft_max(q & 1, q >> 1);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 4 * kHalf; ++m) {
-            const int u = m / 4, t = m % 4;
+            // (the other wave's tiles first: they go to LDS behind the last step)
+            const int u = m / 4, t = (m + 2) % 4;
             if constexpr (!LAST) {
                 qk_mfma(kf, u, t);
-                if (t == 3 && u + kAheadK < kHalf) kf[u % kAheadK] = k_frag(next, u + kAheadK);
+                if (m % 4 == 3 && u + kAheadK < kHalf) kf[u % kAheadK] = k_frag(next, u + kAheadK);
                 if constexpr (!E4M3) {
                     if (m % 8 == 3) stage_bf16(rp, fill, m / 8);
                 }
@@ -824,7 +826,11 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
             soft(m);
             if constexpr (!LAST) __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (!LAST) x_write();
+        if constexpr (!LAST) {
+            x_write();
+            // chunk i + 2 has landed once at most this phase's loads are on their way
+            if constexpr (!E4M3) attn::wait_vm<(4 * kHalf + 4) / 8>();
+        }
         lds_sync();
         const i32x4 f0 = *reinterpret_cast<const i32x4*>(flags);
 #pragma unroll
@@ -881,43 +887,44 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
             o[v][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[v % kAheadV]), as_bf16x8(pf[t]), o[v][t], 0, 0, 0);
             if (t == 3 && v + kAheadV < kTilesW) vf[v % kAheadV] = v_frag(v + kAheadV);
             if constexpr (!LAST) {
+                if (m >= 22 && m < 30 && m % 2 == 0) kf[(m - 22) / 2] = k_frag(after, (m - 22) / 2);
+                if (m == 29 || m == 30) scale_scores(x, m - 29);
                 if constexpr (E4M3) {
                     if (m == 0) commit_at(fill, 0, 4);
                     if (m >= 2 && m < 17) commit_at(fill, 1 + (m - 2) / 5, (m - 2) % 5);
                     if (m == 17) commit_at(fill, 4, 0);
-                    if (m == 18) {
+                    // chunk i + 4's loads, as chunk i + 3's registers come free
+                    if (m == 6) {
                         const int rows4 = row_at(page4, start_of(i + 4));
                         here4 = present_of(rows4);
-                        load_raw(rows4);
+                        rp = ptr_of(rows4, r8);
                     }
+                    if (m == 9 || m == 13) load_part(rp, (m - 9) / 4);
+                    if (m == 18 || m == 21 || m == 24 || m == 27) load_part(rp, 2 + (m - 18) / 3);
                 } else if (m % 7 == 4) {
                     stage_bf16(rp, fill, 5 + m / 7);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (!LAST) finish(x, here1, start_of(i + 1));
+        if constexpr (!LAST) mask_scores(here1, start_of(i + 1));
         here0 = here1;
         here1 = here2;
         here2 = here3;
         here3 = here4;
         page3 = page4;
-        if constexpr (!LAST) {
-            // chunk i + 2 has landed (chunk i + 3's nine loads may be on their way), and every wave is done with chunk i
-            if constexpr (!E4M3) attn::wait_vm<kBlocks>();
-            lds_sync();
-        }
+        if constexpr (!LAST) lds_sync();      // every wave is done with chunk i, and its part of chunk i + 3 is written
     };
     // (four buffers by name, so that the compiler sees which of them a staging load writes)
     for (int i = 0; i + 1 < n; i += 4) {
-        step(std::false_type{}, i, b0, b1, b3);
-        if (i + 2 < n) step(std::false_type{}, i + 1, b1, b2, b0);
-        if (i + 3 < n) step(std::false_type{}, i + 2, b2, b3, b1);
-        if (i + 4 < n) step(std::false_type{}, i + 3, b3, b0, b2);
+        step(std::false_type{}, i, b0, b1, b2, b3);
+        if (i + 2 < n) step(std::false_type{}, i + 1, b1, b2, b3, b0);
+        if (i + 3 < n) step(std::false_type{}, i + 2, b2, b3, b0, b1);
+        if (i + 4 < n) step(std::false_type{}, i + 3, b3, b0, b1, b2);
     }
     if (n > 0) {
         const int last = (n - 1) & 3;
-        step(std::true_type{}, n - 1, last == 0 ? b0 : last == 1 ? b1 : last == 2 ? b2 : b3, nullptr, nullptr);
+        step(std::true_type{}, n - 1, last == 0 ? b0 : last == 1 ? b1 : last == 2 ? b2 : b3, nullptr, nullptr, nullptr);
     }
 
     // ---- the rows' sums: a wave's four lanes of a row, then the two position groups
