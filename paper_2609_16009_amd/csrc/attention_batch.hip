@@ -81,6 +81,7 @@ struct BatchParams {
     int own_tiles, own_spans, own_span, own_items;
     int pre_grid;            // workgroups of the prefix: its items rounded up to a multiple of 8
     int direct;              // one slot: rows go straight to out
+    uint32_t extent;         // bytes of a pool under 2 GB
 };
 
 // Cache rows that do not exist read zeros here.
@@ -136,6 +137,42 @@ __device__ __forceinline__ int64_t row_offset(int r, int T, int H, int64_t sb, i
     return int64_t(b) * sb + int64_t(t) * st + int64_t(h) * ld;
 }
 
+// LDS-direct loads of 16-byte pieces of cache rows, a row per lane: with 32-bit offsets into the pool, a row that does
+// not exist out of its range (zeros), or, for a pool of 2 GB and more, with 64-bit addresses and the zero row (the
+// compiler takes those loads to count as LDS operations too, and so waits for every LDS read at once: 10 % slower).
+template <bool BIG>
+struct StageRows;
+template <>
+struct StageRows<false> {
+    typedef uint32_t Row;
+    __amdgpu_buffer_rsrc_t rsrc;
+    uint32_t ld;
+    __device__ __forceinline__ explicit StageRows(const BatchParams& p)
+        : rsrc(attn::make_rsrc(p.cache, p.extent)), ld(static_cast<uint32_t>(p.ld)) {}
+    __device__ __forceinline__ Row row(int rows, int lane_of) const {
+        const int r = __builtin_amdgcn_ds_bpermute(lane_of << 2, rows);
+        return r < 0 ? attn::kOutOfRange : uint32_t(r) * ld;
+    }
+    __device__ __forceinline__ void load(Row row, uint32_t off, uint16_t* dst) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)dst, 16, row + off, 0, 0, 0);
+    }
+};
+template <>
+struct StageRows<true> {
+    typedef gbytes Row;
+    gbytes cache, zero_row;
+    int64_t ld;
+    __device__ __forceinline__ explicit StageRows(const BatchParams& p)
+        : cache((gbytes)p.cache), zero_row(opaque_zero_row()), ld(p.ld) {}
+    __device__ __forceinline__ Row row(int rows, int lane_of) const {
+        const int r = __builtin_amdgcn_ds_bpermute(lane_of << 2, rows);
+        return r < 0 ? zero_row : cache + int64_t(r) * ld;
+    }
+    __device__ __forceinline__ void load(Row row, uint32_t off, uint16_t* dst) const {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row + off), (lds_void*)dst, 16, 0, 0);
+    }
+};
+
 // Row 16 t + j of a tile: normalised to out, or as the span's partial (reference, sum, unnormalised output).
 template <int HT>
 __device__ __forceinline__ void store_row(const BatchParams& p, const Item& it, int row, int pw, int g, const f32x4 (&o)[kTilesW][HT],
@@ -165,7 +202,7 @@ __device__ __forceinline__ void store_row(const BatchParams& p, const Item& it, 
 }
 
 // One (tile, span).  kv_a, kv_b: chunk buffers; pbuf: P [16 HT][kPPitchB]; red: [4][16 HT].
-template <int HT, bool E4M3>
+template <int HT, bool E4M3, bool BIG>
 __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it, uint16_t* const kv_a, uint16_t* const kv_b,
                                             uint16_t* const pbuf, float* const red, int* const flags) {
     constexpr int HB = 16 * HT;
@@ -205,12 +242,12 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
     // Columns that the cache lacks read the last ones that it has: Q is zero there, and their outputs are not stored.
     // 8 rows x 128 bytes per LDS-direct load; the wave's rows are 16 pw .. 16 pw + 15
     const uint32_t lat_last = uint32_t(2 * p.kv - 16);
-    auto stage_bf16 = [&](gbytes row_ptr, uint16_t* buf, int cb, int half) {
+    const StageRows<BIG> stage(p);
+    auto stage_bf16 = [&](const typename StageRows<BIG>::Row& row, uint16_t* buf, int cb, int half) {
         const int c_st = (lane & 7) ^ swz(8 * half + (lane >> 3));
         const uint32_t off = cb < 8 ? min(uint32_t(cb * 128 + c_st * 16), lat_last)
                                     : p.rope ? uint32_t(2 * p.kv + min(16 * c_st, 2 * p.rope - 16)) : 0u;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row_ptr + off),
-                                         (lds_void*)(buf + cb * kBlockElems + (16 * pw + 8 * half) * 64), 16, 0, 0);
+        stage.load(row, off, buf + cb * kBlockElems + (16 * pw + 8 * half) * 64);
     };
     // 8-bit rows, half a chunk at a time: a thread takes pieces 8 i + (tid & 7) of 16 codes of row tid / 8 (+ 32),
     // the row's scales and one piece of RoPE
@@ -283,7 +320,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
     } else {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const gbytes rp = ptr_of(rows_cur, 16 * pw + 8 * half + (lane >> 3));
+            const auto rp = stage.row(rows_cur, 16 * pw + 8 * half + (lane >> 3));
 #pragma unroll
             for (int cb = 0; cb < kBlocks; ++cb) stage_bf16(rp, kv_a, cb, half);
         }
@@ -342,10 +379,10 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
         const int c0 = start_of(ck);
         const uint64_t present = __builtin_amdgcn_ballot_w64(rows_cur >= 0);
         // the next chunk (behind the last: rows of zeros, which nothing reads)
-        gbytes rp[2];
+        typename StageRows<BIG>::Row rp[2];
         if constexpr (!E4M3) {
-            rp[0] = ptr_of(rows_next, 16 * pw + (lane >> 3));
-            rp[1] = ptr_of(rows_next, 16 * pw + 8 + (lane >> 3));
+            rp[0] = stage.row(rows_next, 16 * pw + (lane >> 3));
+            rp[1] = stage.row(rows_next, 16 * pw + 8 + (lane >> 3));
         }
         const int page_after = page_of(start_of(ck + 2));
         int rows_after = -1;
@@ -525,7 +562,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
 //    The two halves of a sum meet through LDS: each wave finishes two of the four row tiles.
 //  * Per chunk: QK(i + 1) with softmax(i), barrier (P, maxima, half sums and chunk i + 2 are there), PV(i),
 //    barrier (chunk i's buffer is free).
-template <bool E4M3>
+template <bool E4M3, bool BIG>
 __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, uint16_t* const b0, uint16_t* const b1,
                                            uint16_t* const b2, uint16_t* const b3, uint16_t* const pbuf, float* const xbuf,
                                            float* const red, int* const flags) {
@@ -562,10 +599,10 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
     const int c_st = (lane & 7) ^ swz(8 * wave + (lane >> 3));
     const uint32_t lat_last = uint32_t(2 * p.kv - 16);
     const uint32_t rope_off = p.rope ? uint32_t(2 * p.kv + min(16 * c_st, 2 * p.rope - 16)) : 0u;
-    auto stage_bf16 = [&](gbytes row_ptr, uint16_t* buf, int cb) {
+    const StageRows<BIG> stage(p);
+    auto stage_bf16 = [&](const typename StageRows<BIG>::Row& row, uint16_t* buf, int cb) {
         const uint32_t off = cb < 8 ? min(uint32_t(cb * 128 + (c_st ^ (cb & 1)) * 16), lat_last) : rope_off;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row_ptr + off),
-                                         (lds_void*)(buf + cb * kBlk + 8 * wave * 64), 16, 0, 0);
+        stage.load(row, off, buf + cb * kBlk + 8 * wave * 64);
     };
     // 8-bit rows: a thread takes pieces 8 i + (tid & 7) of row tid / 8
     u32x4 code0, code1, code2, code3, code_scale, code_rope;
@@ -624,7 +661,7 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
 #pragma unroll
             for (int i = 0; i < 25; ++i) commit_at(buf, i / 5, i % 5);
         } else {
-            const gbytes rp = ptr_of(rows, 8 * wave + (lane >> 3));
+            const auto rp = stage.row(rows, 8 * wave + (lane >> 3));
 #pragma unroll
             for (int cb = 0; cb < kBlocks; ++cb) stage_bf16(rp, buf, cb);
         }
@@ -765,10 +802,11 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
                     uint16_t* const fill) {
         constexpr bool LAST = decltype(last_c)::value;
         gbytes rp = zero_row;
+        typename StageRows<BIG>::Row row3{};
         if constexpr (!E4M3) {
             const int rows3 = row_at(page3, start_of(i + 3));
             here3 = present_of(rows3);
-            rp = ptr_of(rows3, 8 * wave + (lane >> 3));
+            row3 = stage.row(rows3, 8 * wave + (lane >> 3));
         }
         const int page4 = page_of(start_of(i + 4));
         uint32_t here4 = 0;
@@ -820,7 +858,7 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
                 qk_mfma(kf, u, t);
                 if (m % 4 == 3 && u + kAheadK < kHalf) kf[u % kAheadK] = k_frag(next, u + kAheadK);
                 if constexpr (!E4M3) {
-                    if (m % 8 == 3) stage_bf16(rp, fill, m / 8);
+                    if (m % 8 == 3) stage_bf16(row3, fill, m / 8);
                 }
             }
             soft(m);
@@ -902,7 +940,7 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
                     if (m == 9 || m == 13) load_part(rp, (m - 9) / 4);
                     if (m == 18 || m == 21 || m == 24 || m == 27) load_part(rp, 2 + (m - 18) / 3);
                 } else if (m % 7 == 4) {
-                    stage_bf16(rp, fill, 5 + m / 7);
+                    stage_bf16(row3, fill, 5 + m / 7);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -991,7 +1029,7 @@ __device__ __forceinline__ bool item_of(const BatchParams& p, Item* out) {
     return true;
 }
 
-template <int HT, bool E4M3>
+template <int HT, bool E4M3, bool BIG>
 __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchParams p) {
     __shared__ __attribute__((aligned(128))) uint16_t kv_a[kBlocks * kBlockElems];
     __shared__ __attribute__((aligned(128))) uint16_t kv_b[kBlocks * kBlockElems];
@@ -999,10 +1037,10 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchP
     __shared__ __attribute__((aligned(16))) float red[kWavesB * 16 * HT];
     __shared__ __attribute__((aligned(16))) int flags[4];
     Item it;
-    if (item_of<16 * HT>(p, &it)) narrow_block<HT, E4M3>(p, it, kv_a, kv_b, pbuf, red, flags);
+    if (item_of<16 * HT>(p, &it)) narrow_block<HT, E4M3, BIG>(p, it, kv_a, kv_b, pbuf, red, flags);
 }
 
-template <bool E4M3>
+template <bool E4M3, bool BIG>
 __global__ __launch_bounds__(kThreadsB) void attention_batch_wide_kernel(const BatchParams p) {
     constexpr int kElems = kBlocks * 32 * 64;
     __shared__ __attribute__((aligned(128))) uint16_t b0[kElems];
@@ -1014,7 +1052,7 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_wide_kernel(const B
     __shared__ __attribute__((aligned(16))) float red[256];
     __shared__ __attribute__((aligned(16))) int flags[4];
     Item it;
-    if (item_of<64>(p, &it)) wide_block<E4M3>(p, it, b0, b1, b2, b3, pbuf, xbuf, red, flags);
+    if (item_of<64>(p, &it)) wide_block<E4M3, BIG>(p, it, b0, b1, b2, b3, pbuf, xbuf, red, flags);
 }
 
 // out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), the prefix's spans, then the sequence's own.  A block
@@ -1158,6 +1196,13 @@ nmm_status validate_sizes(const nmm_latent_attn_batch& a) {
     return NMM_OK;
 }
 
+template <bool E4M3, bool BIG>
+void launch_tiles(int ht, const BatchParams& p, dim3 grid, dim3 block, hipStream_t s) {
+    if (ht == 1) hipLaunchKernelGGL((attention_batch_kernel<1, E4M3, BIG>), grid, block, 0, s, p);
+    else if (ht == 2) hipLaunchKernelGGL((attention_batch_kernel<2, E4M3, BIG>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((attention_batch_wide_kernel<E4M3, BIG>), grid, block, 0, s, p);
+}
+
 }  // namespace
 }  // namespace nmm
 
@@ -1232,20 +1277,15 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
     p.own_items = static_cast<int>(q.own_items);
     p.own_tiles = q.own_tiles; p.own_spans = q.own_spans; p.own_span = q.own_span;
     p.direct = q.pre_spans + q.own_spans == 1 ? 1 : 0;
+    const int64_t extent = a.cache.rows * a.cache.ld;
+    const bool big = extent >= kLim;
+    p.extent = big ? 0u : static_cast<uint32_t>(extent);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (q.grid > 0) {
         const dim3 grid(static_cast<uint32_t>(q.grid)), block(kThreadsB);
-        const bool q8 = a.cache.format == NMM_CACHE_E4M3;
-        if (q.ht == 1) {
-            if (q8) hipLaunchKernelGGL((attention_batch_kernel<1, true>), grid, block, 0, s, p);
-            else hipLaunchKernelGGL((attention_batch_kernel<1, false>), grid, block, 0, s, p);
-        } else if (q.ht == 2) {
-            if (q8) hipLaunchKernelGGL((attention_batch_kernel<2, true>), grid, block, 0, s, p);
-            else hipLaunchKernelGGL((attention_batch_kernel<2, false>), grid, block, 0, s, p);
-        } else {
-            if (q8) hipLaunchKernelGGL((attention_batch_wide_kernel<true>), grid, block, 0, s, p);
-            else hipLaunchKernelGGL((attention_batch_wide_kernel<false>), grid, block, 0, s, p);
-        }
+        if (a.cache.format == NMM_CACHE_E4M3) launch_tiles<true, false>(q.ht, p, grid, block, s);
+        else if (big) launch_tiles<false, true>(q.ht, p, grid, block, s);
+        else launch_tiles<false, false>(q.ht, p, grid, block, s);
     }
     // no position anywhere: the merge of no slots writes the zeros
     if (!p.direct) hipLaunchKernelGGL(attention_batch_merge_kernel, dim3(static_cast<uint32_t>(rows)), dim3(kMergeT), 0, s, p);
