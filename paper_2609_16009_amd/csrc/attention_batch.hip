@@ -1058,33 +1058,39 @@ __global__ __launch_bounds__(kThreadsB) void attention_batch_wide_kernel(const B
 // out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), the prefix's spans, then the sequence's own.  A block
 // takes a row, a thread four columns; lane s of each wave weighs slot s.
 constexpr int kMergeT = 128;
-constexpr int kMergeB = 8;       // slots loaded at once
+// BATCH: slots loaded at once, before the sequence's length is known; what a slot that was not written holds is dropped
+template <int BATCH>
 __global__ __launch_bounds__(kMergeT) void attention_batch_merge_kernel(const BatchParams p) {
     const int r = static_cast<int>(blockIdx.x), lane = threadIdx.x & 63;
     const int b = r / (p.T * p.H);
+    const int c = 4 * static_cast<int>(threadIdx.x);
+    const bool has = c < p.kv;
+    const int slots = p.pre_spans + p.own_spans;
+    const float* src = p.part_o + int64_t(r) * p.kv + (has ? c : 0);
+    const int64_t step = int64_t(p.rows) * p.kv;
+    f32x4 v[BATCH];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) v[u] = *reinterpret_cast<const f32x4*>(src + int64_t(min(u, slots - 1)) * step);
+    float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (int64_t(min(lane, slots - 1)) * p.rows + r) * 2);
     int n = p.pre_spans;
     if (p.own_spans) {
         const int len = max(0, min(p.lens[b], p.max_len));
         n += (len + p.own_span - 1) / p.own_span;
     }
     n = __builtin_amdgcn_readfirstlane(n);
-    float2 ml{-INFINITY, 0.f};
-    if (lane < n) ml = *reinterpret_cast<const float2*>(p.part_ml + (int64_t(lane) * p.rows + r) * 2);
-    const int c = 4 * static_cast<int>(threadIdx.x);
-    const bool has = c < p.kv;
-    const float* src = p.part_o + int64_t(r) * p.kv + (has ? c : 0);
-    const int64_t step = int64_t(p.rows) * p.kv;
+    if (lane >= n) ml = float2{-INFINITY, 0.f};
     const float top = wave_max(ml.x);
     // a NaN reference cannot occur (a maximum skips NaN); a NaN sum stays one
     const float w = (ml.x == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
     const float total = wave_sum(w * ml.y);
     f32x4 acc{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < n; s0 += kMergeB) {
-        f32x4 v[kMergeB];
+    for (int s0 = 0; s0 < n; s0 += BATCH) {
+        if (s0 > 0) {
 #pragma unroll
-        for (int u = 0; u < kMergeB; ++u) v[u] = *reinterpret_cast<const f32x4*>(src + int64_t(min(s0 + u, n - 1)) * step);
+            for (int u = 0; u < BATCH; ++u) v[u] = *reinterpret_cast<const f32x4*>(src + int64_t(min(s0 + u, slots - 1)) * step);
+        }
 #pragma unroll
-        for (int u = 0; u < kMergeB; ++u) {
+        for (int u = 0; u < BATCH; ++u) {
             if (s0 + u < n) {
                 const float wu = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s0 + u));
 #pragma unroll
@@ -1096,6 +1102,13 @@ __global__ __launch_bounds__(kMergeT) void attention_batch_merge_kernel(const Ba
     const float scl = total == 0.f ? 0.f : 1.f / total;
     uint16_t* dst = p.out + row_offset(r, p.T, p.H, p.sob, p.sot, p.ldo) + c;
     *reinterpret_cast<uint2*>(dst) = uint2{pack2(acc[0] * scl, acc[1] * scl), pack2(acc[2] * scl, acc[3] * scl)};
+}
+
+// No position anywhere: zeros.
+__global__ __launch_bounds__(kMergeT) void attention_batch_zero_kernel(const BatchParams p) {
+    const int c = 4 * static_cast<int>(threadIdx.x);
+    if (c < p.kv)
+        *reinterpret_cast<uint2*>(p.out + row_offset(static_cast<int>(blockIdx.x), p.T, p.H, p.sob, p.sot, p.ldo) + c) = uint2{0, 0};
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1287,8 +1300,12 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
         else if (big) launch_tiles<false, true>(q.ht, p, grid, block, s);
         else launch_tiles<false, false>(q.ht, p, grid, block, s);
     }
-    // no position anywhere: the merge of no slots writes the zeros
-    if (!p.direct) hipLaunchKernelGGL(attention_batch_merge_kernel, dim3(static_cast<uint32_t>(rows)), dim3(kMergeT), 0, s, p);
+    const int slots = q.pre_spans + q.own_spans;
+    const dim3 rgrid(static_cast<uint32_t>(rows)), rblock(kMergeT);
+    if (slots == 0) hipLaunchKernelGGL(attention_batch_zero_kernel, rgrid, rblock, 0, s, p);
+    else if (slots > 8) hipLaunchKernelGGL(attention_batch_merge_kernel<16>, rgrid, rblock, 0, s, p);
+    else if (slots > 4) hipLaunchKernelGGL(attention_batch_merge_kernel<8>, rgrid, rblock, 0, s, p);
+    else if (slots > 1) hipLaunchKernelGGL(attention_batch_merge_kernel<4>, rgrid, rblock, 0, s, p);
     return hipGetLastError() == hipSuccess ? NMM_OK : NMM_ERR_HIP;
 }
 
