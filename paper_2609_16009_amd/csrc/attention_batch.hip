@@ -209,6 +209,9 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
     // K and V fragments read ahead of their MFMAs: LDS takes about 130 cycles, a step's HT MFMAs 16 HT
     static_assert(HT == 1 || HT == 2, "16 or 32 rows");
     constexpr int kAhead = HT == 2 ? 6 : 9, kAheadV = 8;
+    // 16 rows: one chunk buffer (kv_b is kv_a), so that two workgroups share a CU and one's loads run beside the
+    // other's work; a chunk is staged between two others' work instead of beside it
+    constexpr bool SINGLE = HT == 1;
     const int tid = threadIdx.x, lane = tid & 63;
     const int pw = __builtin_amdgcn_readfirstlane(tid >> 6) & (kWavesB - 1);
     const int g = lane >> 4, j = lane & 15;
@@ -251,32 +254,32 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
     };
     // 8-bit rows, half a chunk at a time: a thread takes pieces 8 i + (tid & 7) of 16 codes of row tid / 8 (+ 32),
     // the row's scales and one piece of RoPE
-    u32x4 code0, code1, code2, code3, code_scale, code_rope;
+    constexpr int kHalves = SINGLE ? 2 : 1;        // halves of a chunk held in registers
+    u32x4 code[kHalves][4], code_scale[kHalves], code_rope[kHalves];
     const int l8 = tid & 7;
     const uint32_t rope8 = p.rope ? uint32_t(p.kv + kScaleBytes + min(16 * l8, 2 * p.rope - 16)) : 0u;
     auto load_raw = [&](int rows, int ps) {
         const gbytes src = ptr_of(rows, (tid >> 3) + 32 * ps);
         const uint32_t last = uint32_t(p.kv - 16);
-        code0 = load16(src + min(uint32_t(16 * l8), last));
-        code1 = load16(src + min(uint32_t(16 * l8 + 128), last));
-        code2 = load16(src + min(uint32_t(16 * l8 + 256), last));
-        code3 = load16(src + min(uint32_t(16 * l8 + 384), last));
-        code_scale = load16(src + p.kv);
-        code_rope = load16(src + rope8);
+        const int k = SINGLE ? ps : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) code[k][i] = load16(src + min(uint32_t(16 * l8 + 128 * i), last));
+        code_scale[k] = load16(src + p.kv);
+        code_rope[k] = load16(src + rope8);
     };
     // part i < 4: piece l8 + 8 i, which is pieces 2 (l8 % 4) and + 1 of column block 2 i + l8 / 4; part 4: RoPE's
     const int f8 = swz(tid >> 3), hi8 = l8 >> 2;
     const int w8_first = (tid >> 3) * 64 + hi8 * kBlockElems + (((2 * (l8 & 3) + hi8) ^ f8) << 3);
     const int w8_second = (tid >> 3) * 64 + hi8 * kBlockElems + (((2 * (l8 & 3) + 1 - hi8) ^ f8) << 3);
     const int w8_rope = (tid >> 3) * 64 + 8 * kBlockElems + ((l8 ^ f8) << 3);
-    auto commit_part = [&](uint16_t* buf, int ps, auto part) {
-        constexpr int i = decltype(part)::value;
+    auto commit_part = [&](uint16_t* buf, int ps, int i) {         // ps and i constants where it is called
         uint16_t* const dst = buf + 32 * 64 * ps;
-        if constexpr (i == 4) {
-            *reinterpret_cast<u32x4*>(dst + w8_rope) = code_rope;
+        const int k = SINGLE ? ps : 0;
+        if (i == 4) {
+            *reinterpret_cast<u32x4*>(dst + w8_rope) = code_rope[k];
         } else {
-            const u32x4 q = i == 0 ? code0 : i == 1 ? code1 : i == 2 ? code2 : code3;
-            const float s = 16 * (l8 + 8 * i) < p.kv ? scale_of(code_scale[i] >> (8 * (l8 >> 1))) : 0.f;
+            const u32x4 q = code[k][i];
+            const float s = 16 * (l8 + 8 * i) < p.kv ? scale_of(code_scale[k][i] >> (8 * (l8 >> 1))) : 0.f;
             const uint2 a = dequant4(q[0], s), b = dequant4(q[1], s), c = dequant4(q[2], s), d = dequant4(q[3], s);
             const u32x4 lo{a.x, a.y, b.x, b.y}, up{c.x, c.y, d.x, d.y};
             // lanes 4 to 7 write their upper half first: the eight lanes of a row then hit eight slots
@@ -284,13 +287,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
             *reinterpret_cast<u32x4*>(dst + 2 * i * kBlockElems + w8_second) = hi8 ? lo : up;
         }
     };
-    auto commit_at = [&](uint16_t* buf, int ps, int step) {       // step 0 .. 4, a constant where it is called
-        if (step == 0) commit_part(buf, ps, std::integral_constant<int, 0>{});
-        if (step == 1) commit_part(buf, ps, std::integral_constant<int, 1>{});
-        if (step == 2) commit_part(buf, ps, std::integral_constant<int, 2>{});
-        if (step == 3) commit_part(buf, ps, std::integral_constant<int, 3>{});
-        if (step == 4) commit_part(buf, ps, std::integral_constant<int, 4>{});
-    };
+    auto commit_at = [&](uint16_t* buf, int ps, int step) { commit_part(buf, ps, step); };
 
     // ---- Q rows to buffer b, in the chunk's layout (rows past the tile's and columns past the cache's: zeros)
     {
@@ -310,21 +307,28 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
         }
     }
     int rows_cur = row_of(start_of(0));
-    if constexpr (E4M3) {
+    auto stage_chunk = [&](int rows, uint16_t* buf) {
+        if constexpr (E4M3) {
 #pragma unroll
-        for (int ps = 0; ps < 2; ++ps) {
-            load_raw(rows_cur, ps);
+            for (int ps = 0; ps < 2; ++ps) {
+                if constexpr (!SINGLE) load_raw(rows, ps);
 #pragma unroll
-            for (int i = 0; i < 5; ++i) commit_at(kv_a, ps, i);
+                for (int i = 0; i < 5; ++i) commit_at(buf, ps, i);
+            }
+        } else {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const auto rp = stage.row(rows, 16 * pw + 8 * half + (lane >> 3));
+#pragma unroll
+                for (int cb = 0; cb < kBlocks; ++cb) stage_bf16(rp, buf, cb, half);
+            }
         }
-    } else {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const auto rp = stage.row(rows_cur, 16 * pw + 8 * half + (lane >> 3));
-#pragma unroll
-            for (int cb = 0; cb < kBlocks; ++cb) stage_bf16(rp, kv_a, cb, half);
-        }
+    };
+    if constexpr (E4M3 && SINGLE) {
+        load_raw(rows_cur, 0);
+        load_raw(rows_cur, 1);
     }
+    if constexpr (!SINGLE) stage_chunk(rows_cur, kv_a);
     int rows_next = row_of(start_of(1));
     __builtin_amdgcn_s_waitcnt(0);
     lds_sync();
@@ -344,7 +348,13 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
 #pragma unroll
         for (int u = 0; u < kSteps; ++u)
             asm("" : "+a"(qf[t][u]));
-    if constexpr (E4M3) load_raw(rows_next, 0);
+    if constexpr (SINGLE) {
+        stage_chunk(rows_cur, kv_a);
+        if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);
+        lds_sync();
+    } else if constexpr (E4M3) {
+        load_raw(rows_next, 0);
+    }
 
     // positions that a row sees: those below its limit
     int limit[HT];
@@ -380,7 +390,11 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
         const uint64_t present = __builtin_amdgcn_ballot_w64(rows_cur >= 0);
         // the next chunk (behind the last: rows of zeros, which nothing reads)
         typename StageRows<BIG>::Row rp[2];
-        if constexpr (!E4M3) {
+        if constexpr (E4M3 && SINGLE) {
+            load_raw(rows_next, 0);
+            load_raw(rows_next, 1);
+        }
+        if constexpr (!E4M3 && !SINGLE) {
             rp[0] = stage.row(rows_next, 16 * pw + (lane >> 3));
             rp[1] = stage.row(rows_next, 16 * pw + 8 + (lane >> 3));
         }
@@ -404,7 +418,8 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
             for (int t = 0; t < HT; ++t)
                 s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[u % kAhead]), as_bf16x8(qf[t][u]), s[t], 0, 0, 0);
             if (u + kAhead < kSteps) kf[u % kAhead] = k_frag(u + kAhead);
-            if constexpr (E4M3) {
+            if constexpr (SINGLE) {
+            } else if constexpr (E4M3) {
                 // the first half of the next chunk's rows, in the MFMAs' shadow
                 if (u % 3 == 2 && u < 15) commit_at(nxt, 0, u / 3);
                 if (u == 15) load_raw(rows_next, 1);
@@ -515,7 +530,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
                 if (v == kTilesW - 1) pf[t] = p_frag(t, 1);
             }
             if (v + kAheadV < 2 * kTilesW) vf[v % kAheadV] = v_frag(v + kAheadV);
-            if constexpr (E4M3) {
+            if constexpr (E4M3 && !SINGLE) {
                 // the second half of the next chunk's rows; then the loads of the one after it
                 if (v % 3 == 2 && v < 15) commit_at(nxt, 1, v / 3);
                 if (v == 15) {
@@ -525,11 +540,14 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        // the next chunk has landed, and every wave is done with this one and with P
-        if constexpr (!E4M3) {
-            __builtin_amdgcn_s_waitcnt(0);
-            rows_after = row_at(page_after, start_of(ck + 2));
+        if constexpr (SINGLE) {
+            // every wave is done with this chunk: the next one takes its place
+            lds_sync();
+            stage_chunk(rows_next, nxt);
         }
+        // the next chunk has landed, and every wave is done with this one and with P
+        if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);
+        if constexpr (!E4M3 || SINGLE) rows_after = row_at(page_after, start_of(ck + 2));
         rows_cur = rows_next;
         rows_next = rows_after;
         lds_sync();
@@ -1030,14 +1048,14 @@ __device__ __forceinline__ bool item_of(const BatchParams& p, Item* out) {
 }
 
 template <int HT, bool E4M3, bool BIG>
-__global__ __launch_bounds__(kThreadsB) void attention_batch_kernel(const BatchParams p) {
+__global__ __launch_bounds__(kThreadsB, HT == 1 ? 2 : 1) void attention_batch_kernel(const BatchParams p) {
     __shared__ __attribute__((aligned(128))) uint16_t kv_a[kBlocks * kBlockElems];
-    __shared__ __attribute__((aligned(128))) uint16_t kv_b[kBlocks * kBlockElems];
+    __shared__ __attribute__((aligned(128))) uint16_t kv_b[HT == 1 ? 64 : kBlocks * kBlockElems];
     __shared__ __attribute__((aligned(16))) uint16_t pbuf[16 * HT * kPPitchB];
     __shared__ __attribute__((aligned(16))) float red[kWavesB * 16 * HT];
     __shared__ __attribute__((aligned(16))) int flags[4];
     Item it;
-    if (item_of<16 * HT>(p, &it)) narrow_block<HT, E4M3, BIG>(p, it, kv_a, kv_b, pbuf, red, flags);
+    if (item_of<16 * HT>(p, &it)) narrow_block<HT, E4M3, BIG>(p, it, kv_a, HT == 1 ? kv_a : kv_b, pbuf, red, flags);
 }
 
 template <bool E4M3, bool BIG>
@@ -1129,7 +1147,7 @@ int chunk_cost(int ht) { return ht == 4 ? 16 : ht == 2 ? 11 : 10; }
 
 // The partition in tiles of 16 ht rows, and an estimate of its time.
 int64_t plan_tiles(const nmm_latent_attn_batch& a, int ht, BatchPlan* out) {
-    constexpr int64_t kCus = 256;
+    const int64_t kCus = ht == 1 ? 512 : 256;      // workgroups that run at once
     BatchPlan q;
     q.ht = ht;
     const int64_t th = a.tokens * a.heads, rows = a.batch * th;
