@@ -43,10 +43,10 @@ constexpr int kSlotK = 256;                 // k of a slot
 constexpr int kSteps = kSlotK / 32;
 constexpr int kMaxGroups = 64;              // groups of a K-slice (their scales lie in LDS)
 constexpr int kMaxRows = 32;                // rows of x per block
-constexpr int kWaves4 = 4;
-// Slots of a K-slice at most: what x's rows of it may take of LDS (8 KB a row of x up to 4 rows, 32 KB in all up to 16
-// rows, 64 KB for 32).
-constexpr int max_slots(int xr) { return xr <= 4 ? 16 : xr == 8 ? 8 : 4; }
+constexpr int kFewRows = 8;                 // up to so many: w4_few_kernel
+constexpr int kFewSlots = 16;               // its slots of a K-slice at most (x's rows of them lie in LDS, 8 KB a row)
+constexpr int kFewDepth = 4, kRowsDepth = 4;
+constexpr int kMaxWaves = 8;
 
 struct W4Params {
     const uint16_t* x;
@@ -57,11 +57,12 @@ struct W4Params {
     int64_t lds, ldz;         // groups per row
     float* y;
     int64_t ldy;
-    float* part;              // [tile][slice][rows of x][16 NT]
+    float* part;              // [tile][slice][rows of x][rows of the weight]
     unsigned* tickets;
     uint32_t row_bytes, w_extent;
     int M, K, N, groups, lg_group;
     int row_blocks, mblocks, ks, slots_per_slice, slots;
+    int waves;
 };
 
 template <int DT>
@@ -119,279 +120,373 @@ __device__ __forceinline__ float scale_value(const uint8_t* s) {
     }
 }
 
-// XR: rows of x staged (1, 2, 4, 8, 16, 32); NT: 16-row tiles of the weight per wave; D: slots in flight (2 to 4); GS:
-// steps of a group within a slot (1, 2, 4, or 8 for groups of 256 k and more).
-template <int DT, bool MX, int XR, int NT, int D, int GS>
-__global__ __launch_bounds__(64 * kWaves4) void w4_kernel(const W4Params p) {
-    constexpr int NW = kWaves4;
-    constexpr int MT = XR > 16 ? 2 : 1;
-    constexpr int kWLoads = 2 * NT, kSlotBytes = kWLoads * 1024;
-    static_assert((D - 1) * kWLoads < 64, "vmcnt holds 6 bits");
-    constexpr int kScaleSize = MX ? 1 : 2;
-    constexpr int kRows = 16 * NT * NW;
-    __shared__ __attribute__((aligned(256))) uint8_t xs_buf[XR * max_slots(XR) * kSlotK * 2];
-    __shared__ __attribute__((aligned(128))) uint8_t ring0[NW * kSlotBytes];
-    __shared__ __attribute__((aligned(128))) uint8_t ring1[NW * kSlotBytes];
-    __shared__ __attribute__((aligned(128))) uint8_t ring2[D > 2 ? NW * kSlotBytes : 16];
-    __shared__ __attribute__((aligned(128))) uint8_t ring3[D > 3 ? NW * kSlotBytes : 16];
-    // a row's scales, padded to an odd number of dwords so that 16 rows of one group lie in 16 banks
-    constexpr int kScalePitch = kMaxGroups * kScaleSize + 4, kZeroPitch = MX ? 4 : kMaxGroups + 4;
-    __shared__ __attribute__((aligned(16))) uint8_t sc[kRows * kScalePitch];
-    __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : kRows * kZeroPitch];
-    __shared__ int s_last;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & (NW - 1);
-    const int g = lane >> 4, j = lane & 15;
+// What a workgroup works on.
+struct W4Tile {
+    int rows, n0, m0, mrows, rb, mb, slice, slot0, slot1, group0, n_groups;
+};
 
+__device__ __forceinline__ bool tile_of(const W4Params& p, int xr, int waves, W4Tile* t) {
     // the row blocks of x over one block of weight rows sit 8 workgroup ids apart, on one XCD
     const int per_rb = p.mblocks * p.ks;
     const int bid = static_cast<int>(blockIdx.x);
-    const int rb = (bid & 7) + 8 * (bid / (8 * per_rb));
+    t->rb = (bid & 7) + 8 * (bid / (8 * per_rb));
     const int rest = (bid >> 3) % per_rb;
-    const int slice = rest / p.mblocks, mb = rest - slice * p.mblocks;
-    if (rb >= p.row_blocks) return;
-    const int n0 = rb * kRows, nw = n0 + wave * 16 * NT, m0 = mb * XR;
-    const int mrows = min(XR, p.M - m0);
-    const int slot0 = slice * p.slots_per_slice, slot1 = min(p.slots, slot0 + p.slots_per_slice);
-    const int n_slots = slot1 - slot0;
-    const int k_begin = slot0 * kSlotK;
-    const int group0 = k_begin >> p.lg_group;
+    t->slice = rest / p.mblocks;
+    t->mb = rest - t->slice * p.mblocks;
+    t->rows = 16 * waves;
+    t->n0 = t->rb * t->rows;
+    t->m0 = t->mb * xr;
+    t->mrows = min(xr, p.M - t->m0);
+    t->slot0 = t->slice * p.slots_per_slice;
+    t->slot1 = min(p.slots, t->slot0 + p.slots_per_slice);
+    t->group0 = (t->slot0 * kSlotK) >> p.lg_group;
+    t->n_groups = min(p.groups - t->group0, ((t->slot1 * kSlotK - 1) >> p.lg_group) - t->group0 + 1);
+    return t->rb < p.row_blocks;
+}
 
-    const __amdgpu_buffer_rsrc_t wr =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.w), (short)0, (int)p.w_extent, kRsrcWord3);
-    const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint16_t*>(p.x + int64_t(m0) * p.ldx), (short)0,
-        int(uint32_t((int64_t(mrows - 1) * p.ldx + (p.K + 7) / 8 * 8) * 2)), kRsrcWord3);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t weight_resource(const W4Params& p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.w), (short)0, (int)p.w_extent, kRsrcWord3);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t x_resource(const W4Params& p, const W4Tile& w) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p.x + int64_t(w.m0) * p.ldx), (short)0,
+                                             int(uint32_t((int64_t(w.mrows - 1) * p.ldx + (p.K + 7) / 8 * 8) * 2)), kRsrcWord3);
+}
 
-    // Weight load q of a slot: rows 8 q + lane / 8, slot lane % 8 of the row holds its chunk (lane % 8) ^ (row / 2 % 8).
-    uint32_t woff[kWLoads];
-    int wk[2];                                   // the chunk's first k: rows 8 q, q even and odd
+__device__ __forceinline__ void load_x(const __amdgpu_buffer_rsrc_t xr, uint32_t off, uint8_t* dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_void*)dst, 16, off, 0, 0, 0);
+}
+
+// A wave's 16 rows of the weight, two loads a slot: load q takes rows 8 q + lane / 8, slot lane % 8 of a row holds its
+// chunk (lane % 8) ^ (row / 2 % 8).
+struct WaveRows {
+    uint32_t off[2];
+    int k[2];                                    // the chunk's first k
+    __device__ __forceinline__ void init(const W4Params& p, int nw, int lane) {
 #pragma unroll
-    for (int q = 0; q < kWLoads; ++q) {
-        const int r = 8 * q + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
-        if (q < 2) wk[q] = 32 * c;
-        woff[q] = nw + r < p.N ? uint32_t(nw + r) * p.row_bytes + 16u * c : kOutOfRange;
+        for (int q = 0; q < 2; ++q) {
+            const int r = 8 * q + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+            k[q] = 32 * c;
+            off[q] = nw + r < p.N ? uint32_t(nw + r) * p.row_bytes + 16u * c : kOutOfRange;
+        }
     }
-    auto load_slot = [&](int slot, uint8_t* ring) {
-        uint8_t* const dst = ring + wave * kSlotBytes;
-        const int k0 = slot * kSlotK;
-        const int left = slot < slot1 ? p.K - k0 : 0;        // a slot past the slice loads nothing
+    // (left: what of K there is from k0 on; none for a slot past the slice)
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t wr, int k0, int left, uint8_t* dst) const {
 #pragma unroll
-        for (int q = 0; q < kWLoads; ++q) {
-            const uint32_t o = wk[q & 1] < left ? woff[q] + uint32_t(k0 / 2) : kOutOfRange;
+        for (int q = 0; q < 2; ++q) {
+            const uint32_t o = k[q] < left ? off[q] + uint32_t(k0 / 2) : kOutOfRange;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void*)(dst + q * 1024), 16, o, 0, 0, kLoadNT);
         }
-    };
-    // The slice's scales and zero points (rows past N: the last one's; without zero points all are 8) are loaded first, to
-    // registers, then x and the ring's first slots, so that all of it is in flight at once.
-    constexpr int kPer = 64 * NW / kRows, kTimes = kMaxGroups / kPer;         // threads per row, groups per thread
-    const int n_groups = min(p.groups - group0, ((slot1 * kSlotK - 1) >> p.lg_group) - group0 + 1);
-    const int sr = tid / kPer, sg = tid % kPer;
-    uint32_t sreg[kTimes], zreg[kTimes];
-    {
-        const int64_t n = min(n0 + sr, p.N - 1);
-        const uint8_t* const s8 = p.scales + (n * p.lds + group0) * kScaleSize;
-        const uint8_t* const z8 = MX || !p.zeros ? s8 : p.zeros + n * p.ldz + group0;
+    }
+};
+
+// The slice's scales and zero points, four threads a row (rows past N: the last one's; without zero points all are 8).
+constexpr int kScaleTimes = kMaxGroups / 4;
+template <bool MX>
+struct Scales {
+    static constexpr int kSize = MX ? 1 : 2;
+    // a row's scales, padded to an odd number of dwords so that 16 rows of one group lie in 16 banks
+    static constexpr int kPitch = kMaxGroups * kSize + 4, kZeroPitch = MX ? 0 : kMaxGroups + 4;
+    uint32_t s[kScaleTimes], z[kScaleTimes];
+    __device__ __forceinline__ void load(const W4Params& p, const W4Tile& w, int tid) {
+        const int64_t n = min(w.n0 + (tid >> 2), p.N - 1);
+        const uint8_t* const s8 = p.scales + (n * p.lds + w.group0) * kSize;
+        const uint8_t* const z8 = MX || !p.zeros ? s8 : p.zeros + n * p.ldz + w.group0;
 #pragma unroll
-        for (int i = 0; i < kTimes; ++i) {
-            if (i * kPer >= n_groups) break;
-            const int gr = min(i * kPer + sg, n_groups - 1);
+        for (int i = 0; i < kScaleTimes; ++i) {
+            if (i * 4 >= w.n_groups) break;
+            const int gr = min(i * 4 + (tid & 3), w.n_groups - 1);
             if constexpr (MX) {
-                sreg[i] = s8[gr];
+                s[i] = s8[gr];
             } else {
-                sreg[i] = reinterpret_cast<const uint16_t*>(s8)[gr];
-                if (p.zeros) zreg[i] = z8[gr];
+                s[i] = reinterpret_cast<const uint16_t*>(s8)[gr];
+                if (p.zeros) z[i] = z8[gr];
             }
         }
     }
-    // x: half a row's slot (32 chunks of 8 k) in half a load: unit u is slot u % n_slots of row u / n_slots; slot c of
-    // row r holds chunk c ^ (r % 16), so that 16 rows of one chunk lie in 16 columns of LDS.
-    const int units = XR * n_slots;
-    for (int u0 = 2 * wave; u0 < units; u0 += 2 * NW) {
-        const int u = u0 + (lane >> 5);
-        const int r = u / n_slots, sl = u - r * n_slots;
-        const int k = (slot0 + sl) * kSlotK + 8 * ((lane & 31) ^ (r & 15));
-        const uint32_t o = u < units && r < mrows && k < p.K ? uint32_t((int64_t(r) * p.ldx + k) * 2) : kOutOfRange;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_void*)(xs_buf + u0 * 512), 16, o, 0, 0, 0);
-    }
-    load_slot(slot0, ring0);
-    load_slot(slot0 + 1, ring1);
-    if constexpr (D > 2) load_slot(slot0 + 2, ring2);
-    if constexpr (D > 3) load_slot(slot0 + 3, ring3);
+    __device__ __forceinline__ void store(const W4Params& p, const W4Tile& w, int tid, uint8_t* sc, uint8_t* zp) const {
+        const int r = tid >> 2;
 #pragma unroll
-    for (int i = 0; i < kTimes; ++i) {
-        if (i * kPer >= n_groups) break;
-        const int gr = i * kPer + sg;
-        if constexpr (MX) {
-            sc[sr * kScalePitch + gr] = uint8_t(sreg[i]);
-        } else {
-            *reinterpret_cast<uint16_t*>(sc + sr * kScalePitch + 2 * gr) = uint16_t(sreg[i]);
-            zp[sr * kZeroPitch + gr] = p.zeros ? uint8_t(zreg[i]) : uint8_t(8);
+        for (int i = 0; i < kScaleTimes; ++i) {
+            if (i * 4 >= w.n_groups) break;
+            const int gr = i * 4 + (tid & 3);
+            if constexpr (MX) {
+                sc[r * kPitch + gr] = uint8_t(s[i]);
+            } else {
+                *reinterpret_cast<uint16_t*>(sc + r * kPitch + 2 * gr) = uint16_t(s[i]);
+                zp[r * kZeroPitch + gr] = p.zeros ? uint8_t(z[i]) : uint8_t(8);
+            }
         }
     }
-    // (x has landed once at most the weight's loads are outstanding; those stay in flight)
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(D * kWLoads) : "memory");
-    // what a chunk that K ends in holds past K is cleared
-    if (p.K % 8 && p.K > k_begin && p.K <= slot1 * kSlotK) {
-        const int c = (p.K - k_begin) / 8;
-        for (int i = tid; i < XR * 8; i += 64 * NW) {
-            const int r = i / 8, e = i % 8;
-            if (e >= p.K % 8)
-                *reinterpret_cast<uint16_t*>(xs_buf + (r * n_slots + c / 32) * 512 + (((c % 32) ^ (r & 15)) << 4) + 2 * e) = 0;
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // (the weight's loads stay in flight)
-    }
+};
 
-    f32x4 sum[NT][MT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sum[t][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int jx = XR < 16 ? (j & (XR - 1)) : j;
+// A slot of a wave's 16 rows (src) times MT x 16 rows of x (xb, `pitch` apart; chunk c of row r at slot c ^ (r % 16)), added
+// to sum: lane (g, j) has rows 4 g + e of x and row j of the weight.
+template <int DT, bool MX, int MT, int GS>
+__device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* src, const uint8_t* xb, int pitch, int jx,
+                                              const uint8_t* sc_row, const uint8_t* zp_row, int k0, int gr0, int lane,
+                                              f32x4 (&sum)[MT]) {
+    const int g = lane >> 4, j = lane & 15;
     const i32x4 ones = DT == NMM_BF16 ? i32x4{0x3F803F80, 0x3F803F80, 0x3F803F80, 0x3F803F80}
                                       : i32x4{0x3C003C00, 0x3C003C00, 0x3C003C00, 0x3C003C00};
-    const uint8_t* const sc_row = sc + (wave * 16 * NT + j) * kScalePitch;
-    const uint8_t* const zp_row = zp + (MX ? 0 : (wave * 16 * NT + j) * kZeroPitch);
-
-    auto consume = [&](const uint8_t* ring, int sl) {
-        // the slot has landed once at most the younger slots' loads are outstanding (loads complete in order)
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * kWLoads) : "memory");
-        const uint8_t* const src = ring + wave * kSlotBytes;
-        const int k0 = (slot0 + sl) * kSlotK;
-        const int gr0 = (k0 >> p.lg_group) - group0;
-        // all that the slot's steps read, first
-        i32x4 xf[kSteps][MT];
-        uint32_t q[kSteps][NT];
-        float sv[kSteps / GS][NT], zv[kSteps / GS][NT];
+    // all that the slot's steps read, first
+    i32x4 xf[kSteps][MT];
+    uint32_t q[kSteps];
+    float sv[kSteps / GS], zv[kSteps / GS];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < kSteps; ++i) {
+        q[i] = *reinterpret_cast<const uint32_t*>(src + j * 128 + ((i ^ ((j >> 1) & 7)) << 4) + 4 * g);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                q[i][t] = *reinterpret_cast<const uint32_t*>(src + (16 * t + j) * 128 + ((i ^ ((j >> 1) & 7)) << 4) + 4 * g);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const int r = 16 * mt + jx;
-                xf[i][mt] = *reinterpret_cast<const i32x4*>(xs_buf + (r * n_slots + sl) * 512 + (((4 * i + g) ^ (r & 15)) << 4));
-            }
-            if (i % GS == GS - 1) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int gr = gr0 + i / GS;
-                    sv[i / GS][t] = scale_value<DT, MX>(sc_row + 16 * t * kScalePitch + gr * kScaleSize);
-                    if constexpr (!MX) zv[i / GS][t] = float(zp_row[16 * t * kZeroPitch + gr]);
-                }
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 acc[NT][MT], xs[MT];
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            if (i % GS == 0) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    xs[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-                }
-            }
-            if constexpr (!MX) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) xs[mt] = mfma<DT>(xf[i][mt], ones, xs[mt]);
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const i32x4 wf = widen<DT, MX>(q[i][t]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) acc[t][mt] = mfma<DT>(xf[i][mt], wf, acc[t][mt]);
-            }
-            if (i % GS == GS - 1) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    // (a group that starts past K has no scale)
-                    const float s = k0 + 32 * (i / GS * GS) < p.K ? sv[i / GS][t] : 0.f;
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float a = MX ? acc[t][mt][e] : __builtin_fmaf(-zv[i / GS][t], xs[mt][e], acc[t][mt][e]);
-                            sum[t][mt][e] = __builtin_fmaf(s, a, sum[t][mt][e]);
-                        }
-                }
-            }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (read before the ring is loaded again)
-    };
-    for (int sl = 0; sl < n_slots; sl += D) {
-        consume(ring0, sl);
-        load_slot(slot0 + sl + D, ring0);
-        if (sl + 1 < n_slots) consume(ring1, sl + 1);
-        load_slot(slot0 + sl + D + 1, ring1);
-        if constexpr (D > 2) {
-            if (sl + 2 < n_slots) consume(ring2, sl + 2);
-            load_slot(slot0 + sl + D + 2, ring2);
-        }
-        if constexpr (D > 3) {
-            if (sl + 3 < n_slots) consume(ring3, sl + 3);
-            load_slot(slot0 + sl + D + 3, ring3);
+        for (int mt = 0; mt < MT; ++mt)
+            xf[i][mt] = *reinterpret_cast<const i32x4*>(xb + (16 * mt + jx) * pitch + (((4 * i + g) ^ jx) << 4));
+        if (i % GS == GS - 1) {
+            const int gr = gr0 + i / GS;
+            sv[i / GS] = scale_value<DT, MX>(sc_row + gr * Scales<MX>::kSize);
+            if constexpr (!MX) zv[i / GS] = float(zp_row[gr]);
         }
     }
-    __builtin_amdgcn_s_waitcnt(0);        // (no load may write LDS after the workgroup has left)
-
-    // lane (g, j) holds m = 4 g + e, n = j of each tile
-    const int64_t tile = int64_t(rb) * p.mblocks + mb;
-    constexpr int kPart = XR * kRows;
-    if (p.ks == 1) {
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 acc[MT], xs[MT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+    for (int i = 0; i < kSteps; ++i) {
+        if (i % GS == 0) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) acc[mt] = xs[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if constexpr (!MX) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) xs[mt] = mfma<DT>(xf[i][mt], ones, xs[mt]);
+        }
+        const i32x4 wf = widen<DT, MX>(q[i]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[mt] = mfma<DT>(xf[i][mt], wf, acc[mt]);
+        if (i % GS == GS - 1) {
+            // (a group that starts past K has no scale)
+            const float s = k0 + 32 * (i / GS * GS) < p.K ? sv[i / GS] : 0.f;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int m = 16 * mt + 4 * g + e, n = nw + 16 * t + j;
-                    if (m < mrows && n < p.N) p.y[int64_t(m0 + m) * p.ldy + n] = sum[t][mt][e];
+                    const float a = MX ? acc[mt][e] : __builtin_fmaf(-zv[i / GS], xs[mt][e], acc[mt][e]);
+                    sum[mt][e] = __builtin_fmaf(s, a, sum[mt][e]);
                 }
-        return;
+        }
     }
-    const __amdgpu_buffer_rsrc_t pr = __builtin_amdgcn_make_buffer_rsrc(p.part + tile * p.ks * kPart, (short)0,
-                                                                        int(uint32_t(p.ks) * kPart * 4u), kRsrcWord3);
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (read before the ring is loaded again)
+}
+
+// y, or the slice's part of it and, for the workgroup that comes last, the sum of the parts.
+template <int XR, int MT>
+__device__ __forceinline__ void finish(const W4Params& p, const W4Tile& w, int tid, int threads, const f32x4 (&sum)[MT]) {
+    __shared__ int s_last;
+    const int lane = tid & 63, g = lane >> 4, col = (tid >> 6) * 16 + (lane & 15);
+    if (p.ks == 1) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int m = 16 * mt + 4 * g + e;
-                if (m < mrows)
-                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum[t][mt][e]), pr,
-                                                          uint32_t(slice * kPart + m * kRows + (wave * NT + t) * 16 + j) * 4u, 0, kDevice);
+                const int m = 16 * mt + 4 * g + e, n = w.n0 + col;
+                if (m < w.mrows && n < p.N) p.y[int64_t(w.m0 + m) * p.ldy + n] = sum[mt][e];
             }
+        return;
+    }
+    const int64_t tile = int64_t(w.rb) * p.mblocks + w.mb;
+    const int part = XR * w.rows;
+    const __amdgpu_buffer_rsrc_t pr =
+        __builtin_amdgcn_make_buffer_rsrc(p.part + tile * p.ks * part, (short)0, int(uint32_t(p.ks * part) * 4u), kRsrcWord3);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int m = 16 * mt + 4 * g + e;
+            if (m < w.mrows)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum[mt][e]), pr,
+                                                      uint32_t(w.slice * part + m * w.rows + col) * 4u, 0, kDevice);
+        }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (tid == 0) s_last = arrive(p.tickets + tile, unsigned(p.ks));
     __syncthreads();
     if (!s_last) return;
     constexpr int kBatch = 8;
-    for (int o = tid; o < kRows * mrows; o += 64 * NW) {
+    for (int o = tid; o < w.rows * w.mrows; o += threads) {
         float v = 0.f;
         for (int q0 = 0; q0 < p.ks; q0 += kBatch) {
             float u[kBatch];
 #pragma unroll
             for (int q = 0; q < kBatch; ++q)
                 u[q] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
-                    pr, q0 + q < p.ks ? uint32_t((q0 + q) * kPart + o) * 4u : kOutOfRange, 0, kDevice));
+                    pr, q0 + q < p.ks ? uint32_t((q0 + q) * part + o) * 4u : kOutOfRange, 0, kDevice));
 #pragma unroll
             for (int q = 0; q < kBatch; ++q) v += u[q];
         }
-        const int m = o / kRows, n = n0 + o - m * kRows;
-        if (n < p.N) p.y[int64_t(m0 + m) * p.ldy + n] = v;
+        const int m = o / w.rows, n = w.n0 + o - m * w.rows;
+        if (n < p.N) p.y[int64_t(w.m0 + m) * p.ldy + n] = v;
     }
+}
+
+// Up to 8 rows of x.  XR: rows of x staged (1, 2, 4, 8); GS: steps of a group within a slot (1, 2, 4, or 8 for groups of
+// 256 k and more).
+template <int DT, bool MX, int XR, int GS>
+__global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p) {
+    constexpr int D = kFewDepth;
+    constexpr int kSlotBytes = 2048;                     // of a wave
+    __shared__ __attribute__((aligned(256))) uint8_t xs_buf[XR * kFewSlots * kSlotK * 2];
+    __shared__ __attribute__((aligned(128))) uint8_t ring0[kMaxWaves * kSlotBytes];
+    __shared__ __attribute__((aligned(128))) uint8_t ring1[kMaxWaves * kSlotBytes];
+    __shared__ __attribute__((aligned(128))) uint8_t ring2[kMaxWaves * kSlotBytes];
+    __shared__ __attribute__((aligned(128))) uint8_t ring3[kMaxWaves * kSlotBytes];
+    static_assert(D == 4, "four rings");
+    __shared__ __attribute__((aligned(16))) uint8_t sc[16 * kMaxWaves * Scales<MX>::kPitch];
+    __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : 16 * kMaxWaves * Scales<MX>::kZeroPitch];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    W4Tile w;
+    if (!tile_of(p, XR, p.waves, &w)) return;
+    const int n_slots = w.slot1 - w.slot0;
+    const __amdgpu_buffer_rsrc_t wr = weight_resource(p), xr = x_resource(p, w);
+    WaveRows rows;
+    rows.init(p, w.n0 + 16 * wave, lane);
+    auto load_slot = [&](int sl, uint8_t* ring) {
+        const int k0 = (w.slot0 + sl) * kSlotK;
+        rows.load(wr, k0, sl < n_slots ? p.K - k0 : 0, ring + wave * kSlotBytes);
+    };
+    // the scales are loaded first, to registers, then x and the ring's first slots: all of it is in flight at once
+    Scales<MX> scales;
+    scales.load(p, w, tid);
+    // x: half a row's slot (32 chunks of 8 k) in half a load: unit u is slot u % n_slots of row u / n_slots
+    const int units = XR * n_slots;
+    for (int u0 = 2 * wave; u0 < units; u0 += 2 * p.waves) {
+        const int u = u0 + (lane >> 5);
+        const int r = u / n_slots, sl = u - r * n_slots;
+        const int k = (w.slot0 + sl) * kSlotK + 8 * ((lane & 31) ^ r);
+        const uint32_t o = u < units && r < w.mrows && k < p.K ? uint32_t((int64_t(r) * p.ldx + k) * 2) : kOutOfRange;
+        load_x(xr, o, xs_buf + u0 * 512);
+    }
+    load_slot(0, ring0);
+    load_slot(1, ring1);
+    load_slot(2, ring2);
+    load_slot(3, ring3);
+    scales.store(p, w, tid, sc, zp);
+    // (x has landed once at most the weight's loads are outstanding; those stay in flight)
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * D) : "memory");
+    // what a chunk that K ends in holds past K is cleared
+    if (p.K % 8 && p.K > w.slot0 * kSlotK && p.K <= w.slot1 * kSlotK) {
+        const int c = (p.K - w.slot0 * kSlotK) / 8;
+        if (tid < XR * 8 && tid % 8 >= p.K % 8) {
+            const int r = tid / 8;
+            *reinterpret_cast<uint16_t*>(xs_buf + (r * n_slots + c / 32) * 512 + (((c % 32) ^ r) << 4) + 2 * (tid % 8)) = 0;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+
+    f32x4 sum[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
+    const int jx = lane & (XR - 1);
+    const int row = 16 * wave + (lane & 15);
+    auto consume = [&](const uint8_t* ring, int sl) {
+        // the slot has landed once at most the younger slots' loads are outstanding (loads complete in order)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (D - 1)) : "memory");
+        const int k0 = (w.slot0 + sl) * kSlotK;
+        slot_products<DT, MX, 1, GS>(p, ring + wave * kSlotBytes, xs_buf + sl * 512, n_slots * 512, jx,
+                                     sc + row * Scales<MX>::kPitch, zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0,
+                                     (k0 >> p.lg_group) - w.group0, lane, sum);
+    };
+    for (int sl = 0; sl < n_slots; sl += D) {
+        consume(ring0, sl);
+        load_slot(sl + D, ring0);
+        if (sl + 1 < n_slots) consume(ring1, sl + 1);
+        load_slot(sl + D + 1, ring1);
+        if (sl + 2 < n_slots) consume(ring2, sl + 2);
+        load_slot(sl + D + 2, ring2);
+        if (sl + 3 < n_slots) consume(ring3, sl + 3);
+        load_slot(sl + D + 3, ring3);
+    }
+    __builtin_amdgcn_s_waitcnt(0);        // (no load may write LDS after the workgroup has left)
+    finish<XR, 1>(p, w, tid, 64 * p.waves, sum);
+}
+
+// More rows of x: XR = 16 MT of them, a slot of which lies in the ring beside the weight's, shared by the 8 waves.
+template <int DT, bool MX, int MT, int GS>
+__global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params p) {
+    constexpr int XR = 16 * MT, D = kRowsDepth;
+    constexpr int kSlotBytes = 2048, kWeightBytes = kMaxWaves * kSlotBytes, kRingBytes = kWeightBytes + XR * 512;
+    constexpr int kLoads = 2 + MT;                       // of a wave, a slot
+    __shared__ __attribute__((aligned(256))) uint8_t ring0[kRingBytes];
+    __shared__ __attribute__((aligned(256))) uint8_t ring1[kRingBytes];
+    __shared__ __attribute__((aligned(256))) uint8_t ring2[kRingBytes];
+    __shared__ __attribute__((aligned(256))) uint8_t ring3[kRingBytes];
+    static_assert(D == 4, "four rings");
+    __shared__ __attribute__((aligned(16))) uint8_t sc[16 * kMaxWaves * Scales<MX>::kPitch];
+    __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : 16 * kMaxWaves * Scales<MX>::kZeroPitch];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    W4Tile w;
+    if (!tile_of(p, XR, kMaxWaves, &w)) return;
+    const int n_slots = w.slot1 - w.slot0;
+    const __amdgpu_buffer_rsrc_t wr = weight_resource(p), xr = x_resource(p, w);
+    WaveRows rows;
+    rows.init(p, w.n0 + 16 * wave, lane);
+    // x: two rows' slots a load
+    uint32_t xoff[MT];
+    int xk[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int r = 2 * (wave * MT + i) + (lane >> 5);
+        xk[i] = 8 * ((lane & 31) ^ (r & 15));
+        xoff[i] = r < w.mrows ? uint32_t((int64_t(r) * p.ldx + xk[i]) * 2) : kOutOfRange;
+    }
+    auto load_slot = [&](int sl, uint8_t* ring) {
+        const int k0 = (w.slot0 + sl) * kSlotK;
+        const int left = sl < n_slots ? p.K - k0 : 0;
+        rows.load(wr, k0, left, ring + wave * kSlotBytes);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            load_x(xr, xk[i] < left ? xoff[i] + uint32_t(k0) * 2u : kOutOfRange,
+                   ring + kWeightBytes + (wave * MT + i) * 1024);
+    };
+    Scales<MX> scales;
+    scales.load(p, w, tid);
+    load_slot(0, ring0);
+    load_slot(1, ring1);
+    load_slot(2, ring2);
+    scales.store(p, w, tid, sc, zp);
+
+    f32x4 sum[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) sum[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = 16 * wave + (lane & 15);
+    // the slot has landed, for every wave, and every wave has read the slot before, whose ring is loaded again
+    auto step = [&](uint8_t* ring, uint8_t* before, int sl) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * kLoads) : "memory");
+        load_slot(sl + D - 1, before);
+        const int k0 = (w.slot0 + sl) * kSlotK;
+        // what a chunk that K ends in holds past K is cleared
+        if (p.K % 8 && p.K - k0 < kSlotK && p.K > k0) {
+            const int c = (p.K - k0) / 8;
+            if (tid < XR * 8 && tid % 8 >= p.K % 8) {
+                const int r = tid / 8;
+                *reinterpret_cast<uint16_t*>(ring + kWeightBytes + r * 512 + ((c ^ (r & 15)) << 4) + 2 * (tid % 8)) = 0;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+        slot_products<DT, MX, MT, GS>(p, ring + wave * kSlotBytes, ring + kWeightBytes, 512, lane & 15,
+                                      sc + row * Scales<MX>::kPitch, zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0,
+                                      (k0 >> p.lg_group) - w.group0, lane, sum);
+    };
+    for (int sl = 0; sl < n_slots; sl += D) {
+        step(ring0, ring3, sl);
+        if (sl + 1 < n_slots) step(ring1, ring0, sl + 1);
+        if (sl + 2 < n_slots) step(ring2, ring1, sl + 2);
+        if (sl + 3 < n_slots) step(ring3, ring2, sl + 3);
+    }
+    __builtin_amdgcn_s_waitcnt(0);        // (no load may write LDS after the workgroup has left)
+    finish<XR, MT>(p, w, tid, 64 * kMaxWaves, sum);
 }
 
 // ---------------------------------------------------------------------------------------------
 // The partition.
 // ---------------------------------------------------------------------------------------------
 struct W4Plan {
-    int xr = 1, nt = 1;
+    int xr = 1, waves = 4;
     int row_blocks = 1, mblocks = 1, ks = 1, slots = 1, slots_per_slice = 1;
     int64_t grid = 0;
     size_t ws_bytes = 0;
@@ -399,7 +494,8 @@ struct W4Plan {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kLim = int64_t(1) << 31;
-constexpr int kTargetGrid = 512;
+constexpr int64_t kCus = 256;
+constexpr int64_t kStartCost = 28, kSplitCost = 20;
 
 nmm_status plan_w4(int64_t M, int64_t K, int64_t N, int64_t group, W4Plan* out) {
     W4Plan q;
@@ -409,54 +505,62 @@ nmm_status plan_w4(int64_t M, int64_t K, int64_t N, int64_t group, W4Plan* out) 
     }
     q.xr = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : M <= 8 ? 8 : M <= 16 ? 16 : 32;
     q.mblocks = static_cast<int>(cdiv(M, q.xr));
-    q.nt = 1;
-    const int rows = 16 * kWaves4 * q.nt;
-    q.row_blocks = static_cast<int>(cdiv(N, rows));
     q.slots = static_cast<int>(cdiv(K, kSlotK));
-    // slices: enough workgroups, but at least four slots each, and no more of K than LDS holds x's rows and the scales of
-    const int64_t tiles = int64_t(q.row_blocks) * q.mblocks;
-    const int64_t most = std::min<int64_t>(max_slots(q.xr), std::max<int64_t>(1, kMaxGroups * group / kSlotK));
-    int64_t ks = std::max<int64_t>(1, std::min<int64_t>(kTargetGrid / std::max<int64_t>(1, tiles), q.slots / 4));
-    ks = std::max(ks, cdiv(q.slots, most));
-    const int64_t per = cdiv(q.slots, ks);
-    q.slots_per_slice = static_cast<int>(per);
-    q.ks = static_cast<int>(cdiv(q.slots, per));
-    q.grid = cdiv(q.row_blocks, 8) * 8 * q.mblocks * q.ks;
-    if (q.grid >= (int64_t(1) << 32) / (64 * kWaves4)) return NMM_ERR_SHAPE;
-    if (q.ks > 1) {
-        if (tiles > kMaxTickets) return NMM_ERR_SHAPE;
-        q.ws_bytes = size_t(kTicketBytes) + size_t(tiles) * q.ks * q.xr * rows * 4;
+    const bool few = q.xr <= kFewRows;
+    const int64_t most = std::min<int64_t>(few ? kFewSlots : 64, std::max<int64_t>(1, kMaxGroups * group / kSlotK));
+    int64_t best = INT64_MAX;
+    for (int waves = kMaxWaves; waves >= (few ? 4 : kMaxWaves); --waves) {
+        const int64_t tiles = cdiv(N, 16 * waves) * q.mblocks;
+        for (int64_t per = std::min<int64_t>(most, q.slots); per >= 1; --per) {
+            const int64_t ks = cdiv(q.slots, per);
+            if (ks > 1 && tiles > kMaxTickets) break;
+            const int64_t cost = cdiv(tiles * ks, kCus) * (per * waves + kStartCost) + (ks > 1 ? kSplitCost : 0);
+            if (cost >= best) continue;
+            best = cost;
+            q.waves = waves;
+            q.row_blocks = static_cast<int>(cdiv(N, 16 * waves));
+            q.ks = static_cast<int>(ks);
+            q.slots_per_slice = static_cast<int>(per);
+        }
     }
+    if (best == INT64_MAX) return NMM_ERR_SHAPE;
+    q.grid = cdiv(q.row_blocks, 8) * 8 * q.mblocks * q.ks;
+    if (q.grid >= (int64_t(1) << 32) / (64 * kMaxWaves)) return NMM_ERR_SHAPE;
+    if (q.ks > 1)
+        q.ws_bytes = size_t(kTicketBytes) + size_t(q.row_blocks) * q.mblocks * q.ks * q.xr * 16 * q.waves * 4;
     *out = q;
     return NMM_OK;
 }
 
+// Rows of x per launch: more row blocks than there are tickets (handoff.h) are split over launches, which follow each other on
+// the stream and may use one workspace.  (N of 2^21 and more has K < 2048 and is never split.)
+int64_t launch_rows(int64_t M, int64_t N) {
+    return std::min<int64_t>(M, kMaxRows * std::max<int64_t>(1, kMaxTickets / cdiv(N, 16 * kMaxWaves)));
+}
+
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-template <int DT, bool MX, int XR, int NT, int D>
-void launch_gs(const W4Params& p, const W4Plan& q, hipStream_t s) {
-    const dim3 grid(static_cast<uint32_t>(q.grid)), block(64 * kWaves4);
-    if constexpr (MX) {
-        hipLaunchKernelGGL((w4_kernel<DT, true, XR, NT, D, 1>), grid, block, 0, s, p);
-    } else {
-        switch (p.lg_group) {
-            case 5: hipLaunchKernelGGL((w4_kernel<DT, false, XR, NT, D, 1>), grid, block, 0, s, p); break;
-            case 6: hipLaunchKernelGGL((w4_kernel<DT, false, XR, NT, D, 2>), grid, block, 0, s, p); break;
-            case 7: hipLaunchKernelGGL((w4_kernel<DT, false, XR, NT, D, 4>), grid, block, 0, s, p); break;
-            default: hipLaunchKernelGGL((w4_kernel<DT, false, XR, NT, D, 8>), grid, block, 0, s, p); break;
-        }
+template <int DT, bool MX, int GS>
+void launch_xr(const W4Params& p, const W4Plan& q, hipStream_t s) {
+    const dim3 grid(static_cast<uint32_t>(q.grid)), block(64 * q.waves);
+    switch (q.xr) {
+        case 1: hipLaunchKernelGGL((w4_few_kernel<DT, MX, 1, GS>), grid, block, 0, s, p); break;
+        case 2: hipLaunchKernelGGL((w4_few_kernel<DT, MX, 2, GS>), grid, block, 0, s, p); break;
+        case 4: hipLaunchKernelGGL((w4_few_kernel<DT, MX, 4, GS>), grid, block, 0, s, p); break;
+        case 8: hipLaunchKernelGGL((w4_few_kernel<DT, MX, 8, GS>), grid, block, 0, s, p); break;
+        case 16: hipLaunchKernelGGL((w4_rows_kernel<DT, MX, 1, GS>), grid, block, 0, s, p); break;
+        default: hipLaunchKernelGGL((w4_rows_kernel<DT, MX, 2, GS>), grid, block, 0, s, p); break;
     }
 }
 
-template <int DT, bool MX>
-void launch_xr(const W4Params& p, const W4Plan& q, hipStream_t s) {
-    switch (q.xr) {
-        case 1: launch_gs<DT, MX, 1, 1, 4>(p, q, s); break;
-        case 2: launch_gs<DT, MX, 2, 1, 4>(p, q, s); break;
-        case 4: launch_gs<DT, MX, 4, 1, 4>(p, q, s); break;
-        case 8: launch_gs<DT, MX, 8, 1, 3>(p, q, s); break;
-        case 16: launch_gs<DT, MX, 16, 1, 3>(p, q, s); break;
-        default: launch_gs<DT, MX, 32, 1, 3>(p, q, s); break;
+template <int DT>
+void launch(const W4Params& p, const W4Plan& q, bool mx, hipStream_t s) {
+    if (mx) return launch_xr<DT, true, 1>(p, q, s);
+    switch (p.lg_group) {
+        case 5: return launch_xr<DT, false, 1>(p, q, s);
+        case 6: return launch_xr<DT, false, 2>(p, q, s);
+        case 7: return launch_xr<DT, false, 4>(p, q, s);
+        default: return launch_xr<DT, false, 8>(p, q, s);
     }
 }
 
@@ -468,9 +572,12 @@ using namespace nmm;
 extern "C" {
 
 size_t nmm_gemv_w4_workspace_size(int64_t M, int64_t K, int64_t N, int64_t group) {
-    if (M < 0 || K < 0 || N < 0 || M >= kLim || K >= kLim || N >= kLim || group < 32 || (group & (group - 1))) return 0;
-    W4Plan q;
-    return plan_w4(M, K, N, group, &q) == NMM_OK ? q.ws_bytes : 0;
+    if (M <= 0 || K <= 0 || N <= 0 || M >= kLim || K >= kLim || N >= kLim || group < 32 || (group & (group - 1))) return 0;
+    const int64_t step = launch_rows(M, N);
+    W4Plan first, last;
+    if (plan_w4(step, K, N, group, &first) != NMM_OK) return 0;
+    if (plan_w4(M % step ? M % step : step, K, N, group, &last) != NMM_OK) return 0;
+    return std::max(first.ws_bytes, last.ws_bytes);
 }
 
 nmm_status nmm_gemv_w4(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_w4_format format, int64_t group, const void* x,
@@ -499,41 +606,45 @@ nmm_status nmm_gemv_w4(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_w4_for
     const int64_t w_extent = (N - 1) * ldwq + cdiv(K, 32) * 16;
     if (w_extent >= kLim) return NMM_ERR_SHAPE;
     if (((std::min<int64_t>(M, kMaxRows) - 1) * ldx + cdiv(K, 8) * 8) * 2 >= kLim) return NMM_ERR_SHAPE;
-    W4Plan q;
-    nmm_status st = plan_w4(M, K, N, group, &q);
+    const int64_t step = launch_rows(M, N);
+    W4Plan first, last;
+    nmm_status st = plan_w4(step, K, N, group, &first);
+    if (st == NMM_OK) st = plan_w4(M % step ? M % step : step, K, N, group, &last);
     if (st != NMM_OK) return st;
-    st = validate_workspace(workspace, workspace_bytes, q.ws_bytes);
+    st = validate_workspace(workspace, workspace_bytes, std::max(first.ws_bytes, last.ws_bytes));
     if (st != NMM_OK) return st;
     W4Params p{};
-    p.x = static_cast<const uint16_t*>(x);
     p.ldx = ldx;
     p.w = static_cast<const uint8_t*>(Wq);
     p.scales = static_cast<const uint8_t*>(scales);
     p.zeros = zeros;
     p.lds = lds;
     p.ldz = ldz;
-    p.y = y;
     p.ldy = ldy;
-    if (q.ks > 1) {
+    if (workspace) {
         p.tickets = static_cast<unsigned*>(workspace);
         p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kTicketBytes);
     }
     p.row_bytes = static_cast<uint32_t>(ldwq);
     p.w_extent = static_cast<uint32_t>(w_extent);
-    p.M = static_cast<int>(M);
     p.K = static_cast<int>(K);
     p.N = static_cast<int>(N);
     p.groups = static_cast<int>(groups);
     while ((int64_t(1) << p.lg_group) < group) ++p.lg_group;
-    p.row_blocks = q.row_blocks;
-    p.mblocks = q.mblocks;
-    p.ks = q.ks;
-    p.slots_per_slice = q.slots_per_slice;
-    p.slots = q.slots;
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool mx = format == NMM_W4_MX;
-    if (dt == NMM_BF16) mx ? launch_xr<NMM_BF16, true>(p, q, s) : launch_xr<NMM_BF16, false>(p, q, s);
-    else mx ? launch_xr<NMM_F16, true>(p, q, s) : launch_xr<NMM_F16, false>(p, q, s);
+    for (int64_t m = 0; m < M; m += step) {
+        const W4Plan& q = M - m >= step ? first : last;
+        p.x = static_cast<const uint16_t*>(x) + m * ldx;
+        p.y = y + m * ldy;
+        p.M = static_cast<int>(std::min(step, M - m));
+        p.row_blocks = q.row_blocks;
+        p.mblocks = q.mblocks;
+        p.ks = q.ks;
+        p.slots_per_slice = q.slots_per_slice;
+        p.slots = q.slots;
+        p.waves = q.waves;
+        if (dt == NMM_BF16) launch<NMM_BF16>(p, q, format == NMM_W4_MX, static_cast<hipStream_t>(stream));
+        else launch<NMM_F16>(p, q, format == NMM_W4_MX, static_cast<hipStream_t>(stream));
+    }
     return hipGetLastError() == hipSuccess ? NMM_OK : NMM_ERR_HIP;
 }
 
