@@ -73,8 +73,8 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// The values of 8 codes, k ascending.
-template <int DT, bool MX>
+// The values of 8 codes, k ascending, or (EVEN_ODD, two instructions fewer) k = 0, 2, 4, 6, 1, 3, 5, 7.
+template <int DT, bool MX, bool EVEN_ODD>
 __device__ __forceinline__ i32x4 widen(uint32_t q) {
     i32x4 r;
     if constexpr (MX) {
@@ -91,7 +91,8 @@ __device__ __forceinline__ i32x4 widen(uint32_t q) {
         }
     } else {
         const uint32_t even = q & 0x0F0F0F0Fu, odd = (q >> 4) & 0x0F0F0F0Fu;
-        const uint32_t lo = __builtin_amdgcn_perm(odd, even, 0x05010400u), hi = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+        const uint32_t lo = EVEN_ODD ? even : __builtin_amdgcn_perm(odd, even, 0x05010400u);
+        const uint32_t hi = EVEN_ODD ? odd : __builtin_amdgcn_perm(odd, even, 0x07030602u);
         if constexpr (DT == NMM_BF16) {
             r[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, false));
             r[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.0f, true));
@@ -107,17 +108,26 @@ __device__ __forceinline__ i32x4 widen(uint32_t q) {
     return r;
 }
 
+template <int DT>
+__device__ __forceinline__ float value(uint32_t bits) {
+    if constexpr (DT == NMM_BF16) return __uint_as_float(bits << 16);
+    else return float(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits)));
+}
+
 template <int DT, bool MX>
 __device__ __forceinline__ float scale_value(const uint8_t* s) {
     if constexpr (MX) {
         // 2^(b - 127): b = 0 is a subnormal fp32, 255 NaN
         const uint32_t b = *s;
         return b == 255u ? __uint_as_float(0x7FC00000u) : b == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(b << 23);
-    } else if constexpr (DT == NMM_BF16) {
-        return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(s)) << 16);
     } else {
-        return float(*reinterpret_cast<const _Float16*>(s));
+        return value<DT>(*reinterpret_cast<const uint16_t*>(s));
     }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
 
 // What a workgroup works on.
@@ -221,14 +231,15 @@ struct Scales {
 
 // A slot of a wave's 16 rows (src) times MT x 16 rows of x (xb, `pitch` apart; chunk c of row r at slot c ^ (r % 16)), added
 // to sum: lane (g, j) has rows 4 g + e of x and row j of the weight.
-template <int DT, bool MX, int MT, int GS>
+// STAGED: x lies in the order of widen's EVEN_ODD, and its sums over the groups were taken before (x_sums, those of the
+// lane's rows; otherwise by one more MFMA a step).
+template <int DT, bool MX, int MT, int GS, bool STAGED>
 __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* src, const uint8_t* xb, int pitch, int jx,
                                               const uint8_t* sc_row, const uint8_t* zp_row, int k0, int gr0, int lane,
-                                              f32x4 (&sum)[MT]) {
+                                              f32x4 (&x_sums)[kSteps / GS], f32x4 (&sum)[MT]) {
     const int g = lane >> 4, j = lane & 15;
     const i32x4 ones = DT == NMM_BF16 ? i32x4{0x3F803F80, 0x3F803F80, 0x3F803F80, 0x3F803F80}
                                       : i32x4{0x3C003C00, 0x3C003C00, 0x3C003C00, 0x3C003C00};
-    // all that the slot's steps read, first
     i32x4 xf[kSteps][MT];
     uint32_t q[kSteps];
     float sv[kSteps / GS], zv[kSteps / GS];
@@ -244,7 +255,6 @@ __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* 
             if constexpr (!MX) zv[i / GS] = float(zp_row[gr]);
         }
     }
-    __builtin_amdgcn_sched_barrier(0);
     f32x4 acc[MT], xs[MT];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
@@ -252,11 +262,11 @@ __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* 
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[mt] = xs[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        if constexpr (!MX) {
+        if constexpr (!MX && !STAGED) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) xs[mt] = mfma<DT>(xf[i][mt], ones, xs[mt]);
         }
-        const i32x4 wf = widen<DT, MX>(q[i]);
+        const i32x4 wf = widen<DT, MX, STAGED>(q[i]);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) acc[mt] = mfma<DT>(xf[i][mt], wf, acc[mt]);
         if (i % GS == GS - 1) {
@@ -266,7 +276,8 @@ __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* 
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float a = MX ? acc[mt][e] : __builtin_fmaf(-zv[i / GS], xs[mt][e], acc[mt][e]);
+                    const float xe = STAGED ? x_sums[i / GS][e] : xs[mt][e];
+                    const float a = MX ? acc[mt][e] : __builtin_fmaf(-zv[i / GS], xe, acc[mt][e]);
                     sum[mt][e] = __builtin_fmaf(s, a, sum[mt][e]);
                 }
         }
@@ -336,6 +347,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
     __shared__ __attribute__((aligned(128))) uint8_t ring2[kMaxWaves * kSlotBytes];
     __shared__ __attribute__((aligned(128))) uint8_t ring3[kMaxWaves * kSlotBytes];
     static_assert(D == 4, "four rings");
+    __shared__ __attribute__((aligned(16))) float x_sum[MX ? 4 : kFewSlots * (kSteps / GS) * XR];
     __shared__ __attribute__((aligned(16))) uint8_t sc[16 * kMaxWaves * Scales<MX>::kPitch];
     __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : 16 * kMaxWaves * Scales<MX>::kZeroPitch];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -353,11 +365,11 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
     // the scales are loaded first, to registers, then x and the ring's first slots: all of it is in flight at once
     Scales<MX> scales;
     scales.load(p, w, tid);
-    // x: half a row's slot (32 chunks of 8 k) in half a load: unit u is slot u % n_slots of row u / n_slots
+    // x: half a row's slot (32 chunks of 8 k) in half a load: unit u is slot u / XR of row u % XR
     const int units = XR * n_slots;
     for (int u0 = 2 * wave; u0 < units; u0 += 2 * p.waves) {
         const int u = u0 + (lane >> 5);
-        const int r = u / n_slots, sl = u - r * n_slots;
+        const int r = u & (XR - 1), sl = u / XR;
         const int k = (w.slot0 + sl) * kSlotK + 8 * ((lane & 31) ^ r);
         const uint32_t o = u < units && r < w.mrows && k < p.K ? uint32_t((int64_t(r) * p.ldx + k) * 2) : kOutOfRange;
         load_x(xr, o, xs_buf + u0 * 512);
@@ -369,12 +381,33 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
     scales.store(p, w, tid, sc, zp);
     // (x has landed once at most the weight's loads are outstanding; those stay in flight)
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * D) : "memory");
-    // what a chunk that K ends in holds past K is cleared
-    if (p.K % 8 && p.K > w.slot0 * kSlotK && p.K <= w.slot1 * kSlotK) {
-        const int c = (p.K - w.slot0 * kSlotK) / 8;
-        if (tid < XR * 8 && tid % 8 >= p.K % 8) {
-            const int r = tid / 8;
-            *reinterpret_cast<uint16_t*>(xs_buf + (r * n_slots + c / 32) * 512 + (((c % 32) ^ r) << 4) + 2 * (tid % 8)) = 0;
+    // What a chunk that K ends in holds past K is cleared; beside zero points, the chunks are put into widen's order and
+    // their sums taken, 4 GS chunks a group.
+    constexpr int kGroups = kSteps / GS;                 // groups of a slot
+    if (!MX || p.K % 8) {
+        for (int c = tid; c < XR * n_slots * 32; c += 64 * p.waves) {
+            const int u = c >> 5, r = u & (XR - 1), sl = u / XR;
+            i32x4* const at = reinterpret_cast<i32x4*>(xs_buf + u * 512 + (((c & 31) ^ r) << 4));
+            i32x4 v = *at;
+            const int left = p.K - ((w.slot0 + sl) * kSlotK + 8 * (c & 31));
+            if (left < 8) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = left > 2 * e + 1 ? v[e] : left > 2 * e ? v[e] & 0xFFFF : 0;
+            }
+            if constexpr (!MX) {
+                float t = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t += value<DT>(uint32_t(v[e]) & 0xFFFFu) + value<DT>(uint32_t(v[e]) >> 16);
+                t += dpp<0xB1>(t);                                   // lane ^ 1
+                t += dpp<0x4E>(t);                                   // lane ^ 2
+                if constexpr (GS > 1) t += dpp<0x141>(t);            // the mirrored lane of 8
+                if constexpr (GS > 2) t += dpp<0x140>(t);            // of 16
+                if constexpr (GS > 4) t += __shfl_xor(t, 16);
+                if ((c & (4 * GS - 1)) == 0) x_sum[(sl * kGroups + (c & 31) / (4 * GS)) * XR + r] = t;
+                v = i32x4{int(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u)), int(__builtin_amdgcn_perm(v[3], v[2], 0x05040100u)),
+                          int(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u)), int(__builtin_amdgcn_perm(v[3], v[2], 0x07060302u))};
+            }
+            *at = v;
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
@@ -386,9 +419,19 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
         // the slot has landed once at most the younger slots' loads are outstanding (loads complete in order)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (D - 1)) : "memory");
         const int k0 = (w.slot0 + sl) * kSlotK;
-        slot_products<DT, MX, 1, GS>(p, ring + wave * kSlotBytes, xs_buf + sl * 512, n_slots * 512, jx,
+        // rows 4 g + e of x, of XR
+        f32x4 x_sums[kGroups];
+        if constexpr (!MX) {
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                const float* const t = x_sum + (sl * kGroups + i) * XR + (XR == 8 ? 4 * ((lane >> 4) & 1) : 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x_sums[i][e] = t[e & (XR - 1)];
+            }
+        }
+        slot_products<DT, MX, 1, GS, true>(p, ring + wave * kSlotBytes, xs_buf + sl * XR * 512, 512, jx,
                                      sc + row * Scales<MX>::kPitch, zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0,
-                                     (k0 >> p.lg_group) - w.group0, lane, sum);
+                                     (k0 >> p.lg_group) - w.group0, lane, x_sums, sum);
     };
     for (int sl = 0; sl < n_slots; sl += D) {
         consume(ring0, sl);
@@ -468,9 +511,10 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params 
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
-        slot_products<DT, MX, MT, GS>(p, ring + wave * kSlotBytes, ring + kWeightBytes, 512, lane & 15,
+        f32x4 none[kSteps / GS];
+        slot_products<DT, MX, MT, GS, false>(p, ring + wave * kSlotBytes, ring + kWeightBytes, 512, lane & 15,
                                       sc + row * Scales<MX>::kPitch, zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0,
-                                      (k0 >> p.lg_group) - w.group0, lane, sum);
+                                      (k0 >> p.lg_group) - w.group0, lane, none, sum);
     };
     for (int sl = 0; sl < n_slots; sl += D) {
         step(ring0, ring3, sl);
