@@ -47,6 +47,10 @@ constexpr int kFewRows = 8;                 // up to so many: w4_few_kernel
 constexpr int kFewSlots = 16;               // its slots of a K-slice at most (x's rows of them lie in LDS, 8 KB a row)
 constexpr int kFewDepth = 4, kRowsDepth = 4;
 constexpr int kMaxWaves = 8;
+// 16 rows of the weight, a slot of them, in w4_rows_kernel's ring.  (Not 2048 apart: the compiler then reads two tiles by one
+// instruction, loses track of which loads that has to wait for and waits for all, 35.3 instead of 28.3 us at
+// 32 x 16384 x 7168; the order of the reads is fixed for the same reason.)
+constexpr int kTileBytes = 2048 + 16;
 
 struct W4Params {
     const uint16_t* x;
@@ -229,67 +233,83 @@ struct Scales {
     }
 };
 
-// A slot of a wave's 16 rows (src) times MT x 16 rows of x (xb, `pitch` apart; chunk c of row r at slot c ^ (r % 16)), added
-// to sum: lane (g, j) has rows 4 g + e of x and row j of the weight.
+// STEPS steps of a slot, from i0 on, of NT x 16 rows of the weight (src, 16 rows 2 KB) times MT x 16 rows of x (xb; chunk c
+// of row r at slot c ^ (r % 16)), added to sum: lane (g, j) has rows 4 g + e of x and row j of the weight.
 // STAGED: x lies in the order of widen's EVEN_ODD, and its sums over the groups were taken before (x_sums, those of the
 // lane's rows; otherwise by one more MFMA a step).
-template <int DT, bool MX, int MT, int GS, bool STAGED>
-__device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* src, const uint8_t* xb, int pitch, int jx,
+template <int DT, bool MX, int MT, int NT, int STEPS, int GS, bool STAGED>
+__device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* src, const uint8_t* xb, int jx, int i0,
                                               const uint8_t* sc_row, const uint8_t* zp_row, int k0, int gr0, int lane,
-                                              f32x4 (&x_sums)[kSteps / GS], f32x4 (&sum)[MT]) {
+                                              const f32x4 (&x_sums)[STEPS / GS], f32x4 (&sum)[NT][MT]) {
     const int g = lane >> 4, j = lane & 15;
     const i32x4 ones = DT == NMM_BF16 ? i32x4{0x3F803F80, 0x3F803F80, 0x3F803F80, 0x3F803F80}
                                       : i32x4{0x3C003C00, 0x3C003C00, 0x3C003C00, 0x3C003C00};
-    i32x4 xf[kSteps][MT];
-    uint32_t q[kSteps];
-    float sv[kSteps / GS], zv[kSteps / GS];
+    i32x4 xf[STEPS][MT];
+    uint32_t q[STEPS][NT];
+    float sv[STEPS / GS][NT], zv[STEPS / GS][NT];
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        q[i] = *reinterpret_cast<const uint32_t*>(src + j * 128 + ((i ^ ((j >> 1) & 7)) << 4) + 4 * g);
+    for (int i = 0; i < STEPS; ++i) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            q[i][t] = *reinterpret_cast<const uint32_t*>(src + (t * kTileBytes + j * 128 + (((i0 + i) ^ ((j >> 1) & 7)) << 4) + 4 * g));
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
-            xf[i][mt] = *reinterpret_cast<const i32x4*>(xb + (16 * mt + jx) * pitch + (((4 * i + g) ^ jx) << 4));
+            xf[i][mt] = *reinterpret_cast<const i32x4*>(xb + (16 * mt + jx) * 512 + (((4 * (i0 + i) + g) ^ jx) << 4));
+        if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);      // (as read here: see kTileBytes)
         if (i % GS == GS - 1) {
-            const int gr = gr0 + i / GS;
-            sv[i / GS] = scale_value<DT, MX>(sc_row + gr * Scales<MX>::kSize);
-            if constexpr (!MX) zv[i / GS] = float(zp_row[gr]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int gr = gr0 + i / GS;
+                sv[i / GS][t] = scale_value<DT, MX>(sc_row + 16 * t * Scales<MX>::kPitch + gr * Scales<MX>::kSize);
+                if constexpr (!MX) zv[i / GS][t] = float(zp_row[16 * t * Scales<MX>::kZeroPitch + gr]);
+            }
         }
     }
-    f32x4 acc[MT], xs[MT];
+    f32x4 acc[NT][MT], xs[MT];
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < STEPS; ++i) {
         if (i % GS == 0) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) acc[mt] = xs[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int mt = 0; mt < MT; ++mt) {
+                xs[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
         }
         if constexpr (!MX && !STAGED) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) xs[mt] = mfma<DT>(xf[i][mt], ones, xs[mt]);
         }
-        const i32x4 wf = widen<DT, MX, STAGED>(q[i]);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[mt] = mfma<DT>(xf[i][mt], wf, acc[mt]);
+        for (int t = 0; t < NT; ++t) {
+            const i32x4 wf = widen<DT, MX, STAGED>(q[i][t]);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) acc[t][mt] = mfma<DT>(xf[i][mt], wf, acc[t][mt]);
+        }
         if (i % GS == GS - 1) {
-            // (a group that starts past K has no scale)
-            const float s = k0 + 32 * (i / GS * GS) < p.K ? sv[i / GS] : 0.f;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int t = 0; t < NT; ++t) {
+                // (a group that starts past K has no scale)
+                const float s = k0 + 32 * (i / GS * GS) < p.K ? sv[i / GS][t] : 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float xe = STAGED ? x_sums[i / GS][e] : xs[mt][e];
-                    const float a = MX ? acc[mt][e] : __builtin_fmaf(-zv[i / GS], xe, acc[mt][e]);
-                    sum[mt][e] = __builtin_fmaf(s, a, sum[mt][e]);
-                }
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float xe = STAGED ? x_sums[i / GS][e] : xs[mt][e];
+                        const float a = MX ? acc[t][mt][e] : __builtin_fmaf(-zv[i / GS][t], xe, acc[t][mt][e]);
+                        sum[t][mt][e] = __builtin_fmaf(s, a, sum[t][mt][e]);
+                    }
+            }
         }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (read before the ring is loaded again)
 }
 
-// y, or the slice's part of it and, for the workgroup that comes last, the sum of the parts.
+// y (the wave has the weight's 16 rows `tile16`), or the slice's part of it and, for the workgroup that comes last, the sum of the parts.
 template <int XR, int MT>
-__device__ __forceinline__ void finish(const W4Params& p, const W4Tile& w, int tid, int threads, const f32x4 (&sum)[MT]) {
+__device__ __forceinline__ void finish(const W4Params& p, const W4Tile& w, int tid, int threads, int tile16, const f32x4 (&sum)[MT]) {
     __shared__ int s_last;
-    const int lane = tid & 63, g = lane >> 4, col = (tid >> 6) * 16 + (lane & 15);
+    const int lane = tid & 63, g = lane >> 4, col = tile16 * 16 + (lane & 15);
     if (p.ks == 1) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -412,7 +432,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
 
-    f32x4 sum[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
+    f32x4 sum[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
     const int jx = lane & (XR - 1);
     const int row = 16 * wave + (lane & 15);
     auto consume = [&](const uint8_t* ring, int sl) {
@@ -429,9 +449,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
                 for (int e = 0; e < 4; ++e) x_sums[i][e] = t[e & (XR - 1)];
             }
         }
-        slot_products<DT, MX, 1, GS, true>(p, ring + wave * kSlotBytes, xs_buf + sl * XR * 512, 512, jx,
-                                     sc + row * Scales<MX>::kPitch, zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0,
-                                     (k0 >> p.lg_group) - w.group0, lane, x_sums, sum);
+        slot_products<DT, MX, 1, 1, kSteps, GS, true>(
+            p, ring + wave * kSlotBytes, xs_buf + sl * XR * 512, jx, 0, sc + row * Scales<MX>::kPitch,
+            zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0, (k0 >> p.lg_group) - w.group0, lane, x_sums, sum);
     };
     for (int sl = 0; sl < n_slots; sl += D) {
         consume(ring0, sl);
@@ -444,14 +464,15 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
         load_slot(sl + D + 3, ring3);
     }
     __builtin_amdgcn_s_waitcnt(0);        // (no load may write LDS after the workgroup has left)
-    finish<XR, 1>(p, w, tid, 64 * p.waves, sum);
+    finish<XR, 1>(p, w, tid, 64 * p.waves, wave, sum[0]);
 }
 
-// More rows of x: XR = 16 MT of them, a slot of which lies in the ring beside the weight's, shared by the 8 waves.
+// More rows of x: XR = 16 MT of them, a slot of which lies in the ring beside the weight's, shared by the 8 waves: wave
+// w multiplies 32 rows of the weight, w % 4, and half of a slot's steps, w / 4.
 template <int DT, bool MX, int MT, int GS>
 __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params p) {
     constexpr int XR = 16 * MT, D = kRowsDepth;
-    constexpr int kSlotBytes = 2048, kWeightBytes = kMaxWaves * kSlotBytes, kRingBytes = kWeightBytes + XR * 512;
+    constexpr int kWeightBytes = kMaxWaves * kTileBytes, kRingBytes = kWeightBytes + XR * 512;
     constexpr int kLoads = 2 + MT;                       // of a wave, a slot
     __shared__ __attribute__((aligned(256))) uint8_t ring0[kRingBytes];
     __shared__ __attribute__((aligned(256))) uint8_t ring1[kRingBytes];
@@ -480,7 +501,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params 
     auto load_slot = [&](int sl, uint8_t* ring) {
         const int k0 = (w.slot0 + sl) * kSlotK;
         const int left = sl < n_slots ? p.K - k0 : 0;
-        rows.load(wr, k0, left, ring + wave * kSlotBytes);
+        rows.load(wr, k0, left, ring + wave * kTileBytes);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
             load_x(xr, xk[i] < left ? xoff[i] + uint32_t(k0) * 2u : kOutOfRange,
@@ -493,10 +514,12 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params 
     load_slot(2, ring2);
     scales.store(p, w, tid, sc, zp);
 
-    f32x4 sum[MT];
+    constexpr int kHalf = kSteps / 2, kGS = GS < kHalf ? GS : kHalf;
+    const int pair = wave & 3, half = wave >> 2;
+    f32x4 sum[2][MT];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) sum[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int row = 16 * wave + (lane & 15);
+    for (int mt = 0; mt < MT; ++mt) sum[0][mt] = sum[1][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = 32 * pair + (lane & 15);
     // the slot has landed, for every wave, and every wave has read the slot before, whose ring is loaded again
     auto step = [&](uint8_t* ring, uint8_t* before, int sl) {
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * kLoads) : "memory");
@@ -511,19 +534,39 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params 
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
-        f32x4 none[kSteps / GS];
-        slot_products<DT, MX, MT, GS, false>(p, ring + wave * kSlotBytes, ring + kWeightBytes, 512, lane & 15,
-                                      sc + row * Scales<MX>::kPitch, zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0,
-                                      (k0 >> p.lg_group) - w.group0, lane, none, sum);
+        f32x4 none[kHalf / kGS];
+        const int kh = k0 + half * kHalf * 32;
+        slot_products<DT, MX, MT, 2, kHalf, kGS, false>(
+            p, ring + pair * 2 * kTileBytes, ring + kWeightBytes, lane & 15, half * kHalf, sc + row * Scales<MX>::kPitch,
+            zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), kh, (kh >> p.lg_group) - w.group0, lane, none, sum);
     };
     for (int sl = 0; sl < n_slots; sl += D) {
         step(ring0, ring3, sl);
-        if (sl + 1 < n_slots) step(ring1, ring0, sl + 1);
-        if (sl + 2 < n_slots) step(ring2, ring1, sl + 2);
-        if (sl + 3 < n_slots) step(ring3, ring2, sl + 3);
+        if (sl + 1 >= n_slots) break;
+        step(ring1, ring0, sl + 1);
+        if (sl + 2 >= n_slots) break;
+        step(ring2, ring1, sl + 2);
+        if (sl + 3 >= n_slots) break;
+        step(ring3, ring2, sl + 3);
     }
     __builtin_amdgcn_s_waitcnt(0);        // (no load may write LDS after the workgroup has left)
-    finish<XR, MT>(p, w, tid, 64 * kMaxWaves, sum);
+    // each wave of a pair hands the other half's sums of one tile over and keeps the other tile
+    __syncthreads();
+    f32x4* const xchg = reinterpret_cast<f32x4*>(ring0);                   // [wave][MT][lane]
+    f32x4 mine[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        mine[mt] = half ? sum[1][mt] : sum[0][mt];
+        xchg[(wave * MT + mt) * 64 + lane] = half ? sum[0][mt] : sum[1][mt];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const f32x4 other = xchg[((wave ^ 4) * MT + mt) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[mt][e] += other[e];
+    }
+    finish<XR, MT>(p, w, tid, 64 * kMaxWaves, 2 * pair + half, mine);
 }
 
 // ---------------------------------------------------------------------------------------------
