@@ -41,7 +41,8 @@ constexpr int kDevice = 16;                 // sc1: device scope (handoff.h)
 constexpr uint32_t kOutOfRange = 0x80000000u;
 constexpr int kSlotK = 256;                 // k of a slot
 constexpr int kSteps = kSlotK / 32;
-constexpr int kMaxGroups = 64;              // groups of a K-slice (their scales lie in LDS)
+// Groups of a K-slice at most (their scales lie in LDS).
+constexpr int max_groups(bool mx) { return mx ? 128 : 64; }
 constexpr int kMaxRows = 32;                // rows of x per block
 constexpr int kFewRows = 8;                 // up to so many: w4_few_kernel
 constexpr int kFewSlots = 16;               // its slots of a K-slice at most (x's rows of them lie in LDS, 8 KB a row)
@@ -119,13 +120,27 @@ __device__ __forceinline__ float value(uint32_t bits) {
 }
 
 template <int DT, bool MX>
-__device__ __forceinline__ float scale_value(const uint8_t* s) {
-    if constexpr (MX) {
-        // 2^(b - 127): b = 0 is a subnormal fp32, 255 NaN
-        const uint32_t b = *s;
-        return b == 255u ? __uint_as_float(0x7FC00000u) : b == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(b << 23);
+__device__ __forceinline__ float scale_value(uint32_t bits) {
+    if constexpr (MX) return bits == 255u ? __uint_as_float(0x7FC00000u) : ldexpf(0x1p-127f, int(bits));      // 2^(b - 127)
+    else return value<DT>(bits);
+}
+
+// COUNT values of BYTES bytes each, in words where they fill some (the caller's address is a multiple of COUNT * BYTES, or of 4
+// where that is more).
+template <int COUNT, int BYTES>
+__device__ __forceinline__ void read_small(const uint8_t* at, uint32_t (&v)[COUNT]) {
+    static_assert(BYTES == 1 || BYTES == 2, "scales and zero points");
+    if constexpr (COUNT * BYTES >= 4) {
+        constexpr int kPer = 4 / BYTES;
+#pragma unroll
+        for (int w = 0; w < COUNT / kPer; ++w) {
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(at + 4 * w);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) v[w * kPer + i] = (u >> (8 * BYTES * i)) & (BYTES == 1 ? 0xFFu : 0xFFFFu);
+        }
     } else {
-        return value<DT>(*reinterpret_cast<const uint16_t*>(s));
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = BYTES == 1 ? *(at + i) : *reinterpret_cast<const uint16_t*>(at + 2 * i);
     }
 }
 
@@ -194,19 +209,19 @@ struct WaveRows {
 };
 
 // The slice's scales and zero points, four threads a row (rows past N: the last one's; without zero points all are 8).
-constexpr int kScaleTimes = kMaxGroups / 4;
 template <bool MX>
 struct Scales {
+    static constexpr int kMaxGroups = max_groups(MX), kTimes = kMaxGroups / 4;
     static constexpr int kSize = MX ? 1 : 2;
     // a row's scales, padded to an odd number of dwords so that 16 rows of one group lie in 16 banks
     static constexpr int kPitch = kMaxGroups * kSize + 4, kZeroPitch = MX ? 0 : kMaxGroups + 4;
-    uint32_t s[kScaleTimes], z[kScaleTimes];
+    uint32_t s[kTimes], z[kTimes];
     __device__ __forceinline__ void load(const W4Params& p, const W4Tile& w, int tid) {
         const int64_t n = min(w.n0 + (tid >> 2), p.N - 1);
         const uint8_t* const s8 = p.scales + (n * p.lds + w.group0) * kSize;
         const uint8_t* const z8 = MX || !p.zeros ? s8 : p.zeros + n * p.ldz + w.group0;
 #pragma unroll
-        for (int i = 0; i < kScaleTimes; ++i) {
+        for (int i = 0; i < kTimes; ++i) {
             if (i * 4 >= w.n_groups) break;
             const int gr = min(i * 4 + (tid & 3), w.n_groups - 1);
             if constexpr (MX) {
@@ -220,7 +235,7 @@ struct Scales {
     __device__ __forceinline__ void store(const W4Params& p, const W4Tile& w, int tid, uint8_t* sc, uint8_t* zp) const {
         const int r = tid >> 2;
 #pragma unroll
-        for (int i = 0; i < kScaleTimes; ++i) {
+        for (int i = 0; i < kTimes; ++i) {
             if (i * 4 >= w.n_groups) break;
             const int gr = i * 4 + (tid & 3);
             if constexpr (MX) {
@@ -246,7 +261,7 @@ __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* 
                                       : i32x4{0x3C003C00, 0x3C003C00, 0x3C003C00, 0x3C003C00};
     i32x4 xf[STEPS][MT];
     uint32_t q[STEPS][NT];
-    float sv[STEPS / GS][NT], zv[STEPS / GS][NT];
+    uint32_t sv[NT][STEPS / GS], zv[NT][STEPS / GS];
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
 #pragma unroll
@@ -256,14 +271,12 @@ __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* 
         for (int mt = 0; mt < MT; ++mt)
             xf[i][mt] = *reinterpret_cast<const i32x4*>(xb + (16 * mt + jx) * 512 + (((4 * (i0 + i) + g) ^ jx) << 4));
         if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);      // (as read here: see kTileBytes)
-        if (i % GS == GS - 1) {
+    }
+    // (gr0 is a multiple of STEPS / GS: a slice starts with a group, or GS = STEPS)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int gr = gr0 + i / GS;
-                sv[i / GS][t] = scale_value<DT, MX>(sc_row + 16 * t * Scales<MX>::kPitch + gr * Scales<MX>::kSize);
-                if constexpr (!MX) zv[i / GS][t] = float(zp_row[16 * t * Scales<MX>::kZeroPitch + gr]);
-            }
-        }
+    for (int t = 0; t < NT; ++t) {
+        read_small<STEPS / GS, Scales<MX>::kSize>(sc_row + 16 * t * Scales<MX>::kPitch + gr0 * Scales<MX>::kSize, sv[t]);
+        if constexpr (!MX) read_small<STEPS / GS, 1>(zp_row + 16 * t * Scales<MX>::kZeroPitch + gr0, zv[t]);
     }
     f32x4 acc[NT][MT], xs[MT];
 #pragma unroll
@@ -290,13 +303,13 @@ __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* 
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 // (a group that starts past K has no scale)
-                const float s = k0 + 32 * (i / GS * GS) < p.K ? sv[i / GS][t] : 0.f;
+                const float s = k0 + 32 * (i / GS * GS) < p.K ? scale_value<DT, MX>(sv[t][i / GS]) : 0.f;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float xe = STAGED ? x_sums[i / GS][e] : xs[mt][e];
-                        const float a = MX ? acc[t][mt][e] : __builtin_fmaf(-zv[i / GS][t], xe, acc[t][mt][e]);
+                        const float a = MX ? acc[t][mt][e] : __builtin_fmaf(-float(zv[t][i / GS]), xe, acc[t][mt][e]);
                         sum[t][mt][e] = __builtin_fmaf(s, a, sum[t][mt][e]);
                     }
             }
@@ -584,7 +597,7 @@ constexpr int64_t kLim = int64_t(1) << 31;
 constexpr int64_t kCus = 256;
 constexpr int64_t kStartCost = 28, kSplitCost = 20;
 
-nmm_status plan_w4(int64_t M, int64_t K, int64_t N, int64_t group, W4Plan* out) {
+nmm_status plan_w4(int64_t M, int64_t K, int64_t N, bool mx, int64_t group, W4Plan* out) {
     W4Plan q;
     if (M <= 0 || K <= 0 || N <= 0) {
         *out = q;
@@ -594,7 +607,7 @@ nmm_status plan_w4(int64_t M, int64_t K, int64_t N, int64_t group, W4Plan* out) 
     q.mblocks = static_cast<int>(cdiv(M, q.xr));
     q.slots = static_cast<int>(cdiv(K, kSlotK));
     const bool few = q.xr <= kFewRows;
-    const int64_t most = std::min<int64_t>(few ? kFewSlots : 64, std::max<int64_t>(1, kMaxGroups * group / kSlotK));
+    const int64_t most = std::min<int64_t>(few ? kFewSlots : 64, std::max<int64_t>(1, max_groups(mx) * group / kSlotK));
     int64_t best = INT64_MAX;
     for (int waves = kMaxWaves; waves >= (few ? 4 : kMaxWaves); --waves) {
         const int64_t tiles = cdiv(N, 16 * waves) * q.mblocks;
@@ -661,10 +674,16 @@ extern "C" {
 size_t nmm_gemv_w4_workspace_size(int64_t M, int64_t K, int64_t N, int64_t group) {
     if (M <= 0 || K <= 0 || N <= 0 || M >= kLim || K >= kLim || N >= kLim || group < 32 || (group & (group - 1))) return 0;
     const int64_t step = launch_rows(M, N);
-    W4Plan first, last;
-    if (plan_w4(step, K, N, group, &first) != NMM_OK) return 0;
-    if (plan_w4(M % step ? M % step : step, K, N, group, &last) != NMM_OK) return 0;
-    return std::max(first.ws_bytes, last.ws_bytes);
+    size_t most = 0;
+    for (const bool mx : {false, true}) {
+        if (mx && group != 32) continue;
+        for (const int64_t rows : {step, M % step ? M % step : step}) {
+            W4Plan q;
+            if (plan_w4(rows, K, N, mx, group, &q) != NMM_OK) return 0;
+            most = std::max(most, q.ws_bytes);
+        }
+    }
+    return most;
 }
 
 nmm_status nmm_gemv_w4(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_w4_format format, int64_t group, const void* x,
@@ -695,8 +714,9 @@ nmm_status nmm_gemv_w4(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_w4_for
     if (((std::min<int64_t>(M, kMaxRows) - 1) * ldx + cdiv(K, 8) * 8) * 2 >= kLim) return NMM_ERR_SHAPE;
     const int64_t step = launch_rows(M, N);
     W4Plan first, last;
-    nmm_status st = plan_w4(step, K, N, group, &first);
-    if (st == NMM_OK) st = plan_w4(M % step ? M % step : step, K, N, group, &last);
+    const bool mx = format == NMM_W4_MX;
+    nmm_status st = plan_w4(step, K, N, mx, group, &first);
+    if (st == NMM_OK) st = plan_w4(M % step ? M % step : step, K, N, mx, group, &last);
     if (st != NMM_OK) return st;
     st = validate_workspace(workspace, workspace_bytes, std::max(first.ws_bytes, last.ws_bytes));
     if (st != NMM_OK) return st;
@@ -729,8 +749,8 @@ nmm_status nmm_gemv_w4(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_w4_for
         p.slots_per_slice = q.slots_per_slice;
         p.slots = q.slots;
         p.waves = q.waves;
-        if (dt == NMM_BF16) launch<NMM_BF16>(p, q, format == NMM_W4_MX, static_cast<hipStream_t>(stream));
-        else launch<NMM_F16>(p, q, format == NMM_W4_MX, static_cast<hipStream_t>(stream));
+        if (dt == NMM_BF16) launch<NMM_BF16>(p, q, mx, static_cast<hipStream_t>(stream));
+        else launch<NMM_F16>(p, q, mx, static_cast<hipStream_t>(stream));
     }
     return hipGetLastError() == hipSuccess ? NMM_OK : NMM_ERR_HIP;
 }
