@@ -41,8 +41,8 @@ constexpr int kDevice = 16;                 // sc1: device scope (handoff.h)
 constexpr uint32_t kOutOfRange = 0x80000000u;
 constexpr int kSlotK = 256;                 // k of a slot
 constexpr int kSteps = kSlotK / 32;
-// Groups of a K-slice at most (their scales lie in LDS).
-constexpr int max_groups(bool mx) { return mx ? 128 : 64; }
+// Groups of a K-slice at most: their scales lie in LDS, a byte or three each, beside the x rows.
+constexpr int max_groups(bool mx, int xr) { return mx || xr <= 4 ? 128 : 64; }
 constexpr int kMaxRows = 32;                // rows of x per block
 constexpr int kFewRows = 8;                 // up to so many: w4_few_kernel
 constexpr int kFewSlots = 16;               // its slots of a K-slice at most (x's rows of them lie in LDS, 8 KB a row)
@@ -209,9 +209,9 @@ struct WaveRows {
 };
 
 // The slice's scales and zero points, four threads a row (rows past N: the last one's; without zero points all are 8).
-template <bool MX>
+template <bool MX, int XR>
 struct Scales {
-    static constexpr int kMaxGroups = max_groups(MX), kTimes = kMaxGroups / 4;
+    static constexpr int kMaxGroups = max_groups(MX, XR), kTimes = kMaxGroups / 4;
     static constexpr int kSize = MX ? 1 : 2;
     // a row's scales, padded to an odd number of dwords so that 16 rows of one group lie in 16 banks
     static constexpr int kPitch = kMaxGroups * kSize + 4, kZeroPitch = MX ? 0 : kMaxGroups + 4;
@@ -252,7 +252,7 @@ struct Scales {
 // of row r at slot c ^ (r % 16)), added to sum: lane (g, j) has rows 4 g + e of x and row j of the weight.
 // STAGED: x lies in the order of widen's EVEN_ODD, and its sums over the groups were taken before (x_sums, those of the
 // lane's rows; otherwise by one more MFMA a step).
-template <int DT, bool MX, int MT, int NT, int STEPS, int GS, bool STAGED>
+template <int DT, bool MX, int XR, int MT, int NT, int STEPS, int GS, bool STAGED>
 __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* src, const uint8_t* xb, int jx, int i0,
                                               const uint8_t* sc_row, const uint8_t* zp_row, int k0, int gr0, int lane,
                                               const f32x4 (&x_sums)[STEPS / GS], f32x4 (&sum)[NT][MT]) {
@@ -275,8 +275,8 @@ __device__ __forceinline__ void slot_products(const W4Params& p, const uint8_t* 
     // (gr0 is a multiple of STEPS / GS: a slice starts with a group, or GS = STEPS)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        read_small<STEPS / GS, Scales<MX>::kSize>(sc_row + 16 * t * Scales<MX>::kPitch + gr0 * Scales<MX>::kSize, sv[t]);
-        if constexpr (!MX) read_small<STEPS / GS, 1>(zp_row + 16 * t * Scales<MX>::kZeroPitch + gr0, zv[t]);
+        read_small<STEPS / GS, Scales<MX, XR>::kSize>(sc_row + 16 * t * Scales<MX, XR>::kPitch + gr0 * Scales<MX, XR>::kSize, sv[t]);
+        if constexpr (!MX) read_small<STEPS / GS, 1>(zp_row + 16 * t * Scales<MX, XR>::kZeroPitch + gr0, zv[t]);
     }
     f32x4 acc[NT][MT], xs[MT];
 #pragma unroll
@@ -381,8 +381,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
     __shared__ __attribute__((aligned(128))) uint8_t ring3[kMaxWaves * kSlotBytes];
     static_assert(D == 4, "four rings");
     __shared__ __attribute__((aligned(16))) float x_sum[MX ? 4 : kFewSlots * (kSteps / GS) * XR];
-    __shared__ __attribute__((aligned(16))) uint8_t sc[16 * kMaxWaves * Scales<MX>::kPitch];
-    __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : 16 * kMaxWaves * Scales<MX>::kZeroPitch];
+    __shared__ __attribute__((aligned(16))) uint8_t sc[16 * kMaxWaves * Scales<MX, XR>::kPitch];
+    __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : 16 * kMaxWaves * Scales<MX, XR>::kZeroPitch];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     W4Tile w;
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
         rows.load(wr, k0, sl < n_slots ? p.K - k0 : 0, ring + wave * kSlotBytes);
     };
     // the scales are loaded first, to registers, then x and the ring's first slots: all of it is in flight at once
-    Scales<MX> scales;
+    Scales<MX, XR> scales;
     scales.load(p, w, tid);
     // x: half a row's slot (32 chunks of 8 k) in half a load: unit u is slot u / XR of row u % XR
     const int units = XR * n_slots;
@@ -462,9 +462,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_few_kernel(const W4Params p
                 for (int e = 0; e < 4; ++e) x_sums[i][e] = t[e & (XR - 1)];
             }
         }
-        slot_products<DT, MX, 1, 1, kSteps, GS, true>(
-            p, ring + wave * kSlotBytes, xs_buf + sl * XR * 512, jx, 0, sc + row * Scales<MX>::kPitch,
-            zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), k0, (k0 >> p.lg_group) - w.group0, lane, x_sums, sum);
+        slot_products<DT, MX, XR, 1, 1, kSteps, GS, true>(
+            p, ring + wave * kSlotBytes, xs_buf + sl * XR * 512, jx, 0, sc + row * Scales<MX, XR>::kPitch,
+            zp + (MX ? 0 : row * Scales<MX, XR>::kZeroPitch), k0, (k0 >> p.lg_group) - w.group0, lane, x_sums, sum);
     };
     for (int sl = 0; sl < n_slots; sl += D) {
         consume(ring0, sl);
@@ -492,8 +492,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params 
     __shared__ __attribute__((aligned(256))) uint8_t ring2[kRingBytes];
     __shared__ __attribute__((aligned(256))) uint8_t ring3[kRingBytes];
     static_assert(D == 4, "four rings");
-    __shared__ __attribute__((aligned(16))) uint8_t sc[16 * kMaxWaves * Scales<MX>::kPitch];
-    __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : 16 * kMaxWaves * Scales<MX>::kZeroPitch];
+    __shared__ __attribute__((aligned(16))) uint8_t sc[16 * kMaxWaves * Scales<MX, XR>::kPitch];
+    __shared__ __attribute__((aligned(16))) uint8_t zp[MX ? 16 : 16 * kMaxWaves * Scales<MX, XR>::kZeroPitch];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     W4Tile w;
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params 
             load_x(xr, xk[i] < left ? xoff[i] + uint32_t(k0) * 2u : kOutOfRange,
                    ring + kWeightBytes + (wave * MT + i) * 1024);
     };
-    Scales<MX> scales;
+    Scales<MX, XR> scales;
     scales.load(p, w, tid);
     load_slot(0, ring0);
     load_slot(1, ring1);
@@ -549,9 +549,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void w4_rows_kernel(const W4Params 
         }
         f32x4 none[kHalf / kGS];
         const int kh = k0 + half * kHalf * 32;
-        slot_products<DT, MX, MT, 2, kHalf, kGS, false>(
-            p, ring + pair * 2 * kTileBytes, ring + kWeightBytes, lane & 15, half * kHalf, sc + row * Scales<MX>::kPitch,
-            zp + (MX ? 0 : row * Scales<MX>::kZeroPitch), kh, (kh >> p.lg_group) - w.group0, lane, none, sum);
+        slot_products<DT, MX, XR, MT, 2, kHalf, kGS, false>(
+            p, ring + pair * 2 * kTileBytes, ring + kWeightBytes, lane & 15, half * kHalf, sc + row * Scales<MX, XR>::kPitch,
+            zp + (MX ? 0 : row * Scales<MX, XR>::kZeroPitch), kh, (kh >> p.lg_group) - w.group0, lane, none, sum);
     };
     for (int sl = 0; sl < n_slots; sl += D) {
         step(ring0, ring3, sl);
@@ -607,7 +607,7 @@ nmm_status plan_w4(int64_t M, int64_t K, int64_t N, bool mx, int64_t group, W4Pl
     q.mblocks = static_cast<int>(cdiv(M, q.xr));
     q.slots = static_cast<int>(cdiv(K, kSlotK));
     const bool few = q.xr <= kFewRows;
-    const int64_t most = std::min<int64_t>(few ? kFewSlots : 64, std::max<int64_t>(1, max_groups(mx) * group / kSlotK));
+    const int64_t most = std::min<int64_t>(few ? kFewSlots : 64, std::max<int64_t>(1, max_groups(mx, q.xr) * group / kSlotK));
     int64_t best = INT64_MAX;
     for (int waves = kMaxWaves; waves >= (few ? 4 : kMaxWaves); --waves) {
         const int64_t tiles = cdiv(N, 16 * waves) * q.mblocks;
