@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const WriteP
     const int t = static_cast<int>(blockIdx.x) * kTokensPerGroup + (threadIdx.x >> 6);
     if (t >= p.tokens) return;
     const int64_t slot = p.slots[t];
-    if (slot < 0 || slot >= p.rows) return;
+    const int64_t pos = p.positions ? p.positions[t] : 0;
     const int c = 8 * lane;
     const bool has = c < p.kv;
     const bool pair = lane < p.rope / 2;
@@ -117,11 +117,12 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const WriteP
             v[2 * i + 1] = v[2 * i + 1] * inv * bf16_up(w[i] >> 16);
         }
     }
+    if (slot < 0 || slot >= p.rows) return;        // (checked here, so that the row is loaded beside its slot)
     uint8_t* const row = p.data + slot * p.ld;
     const int64_t rope_at = E4M3 ? p.kv + kScaleBytes : 2 * p.kv;
     if (pair) {
         float sn = 0.f, cs = 1.f;
-        if (p.positions) rope_sincos(p.freq_step, p.positions[t], lane, &sn, &cs);
+        if (p.positions) rope_sincos(p.freq_step, pos, lane, &sn, &cs);
         const float r0 = p.positions ? k0 * cs - k1 * sn : k0, r1 = p.positions ? k0 * sn + k1 * cs : k1;
         *reinterpret_cast<uint32_t*>(row + rope_at + 4 * lane) = uint32_t(to_bf16_bits(r0)) | (uint32_t(to_bf16_bits(r1)) << 16);
     }
