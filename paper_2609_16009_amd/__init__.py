@@ -664,6 +664,8 @@ def nmm_gemv_w4(x: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, y: torc
         raise TypeError("x must be bfloat16 or float16, Wq uint8 and y float32")
     if scales.dtype not in (x.dtype, torch.uint8) or (zeros is not None and zeros.dtype != torch.uint8):
         raise TypeError("scales must be of x's type or uint8, zeros uint8")
+    if any(t is not None and t.dim() != 2 for t in (x, Wq, scales, y, zeros)):
+        raise ValueError("nmm_gemv_w4 takes 2-D tensors")
     M, N = x.shape[0], Wq.shape[0]
     K = x.shape[1] if K is None else K
     groups = -(-K // group) if group > 0 else 0

@@ -263,3 +263,35 @@ def test_two_streams_with_their_own_workspaces():
         b.call(out=outs[1], stream=s2)
         torch.cuda.synchronize()
         assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_python_refusals():
+    c = Case(20, 2, 1, 4, 40, [30, 40], 16, True, kv=64, rope=32)
+    c.call()
+    half = c.dq.half()
+    for bad in (dict(q=half), dict(out=torch.zeros((2, 1, 4, 64), device="cuda")), dict(q=c.dq[0, 0])):
+        with pytest.raises(TypeError):
+            c.call(**bad)
+    ok = torch.zeros((2, 1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in (dict(out=ok[:1]), dict(out=ok[..., :63]), dict(q=c.dq[..., :95], out=ok), dict(pages=None), dict(lens=None), dict(lens=c.d_lens[:1]),
+                dict(pages=c.d_pages[:, :1]), dict(pages=c.d_pages.long()), dict(lens=c.d_lens.long()), dict(prefix_pages=None),
+                dict(prefix_pages=c.d_prefix[:1]), dict(page_size=24), dict(page_size=0), dict(max_len=-1), dict(prefix_len=-1),
+                dict(kv_lora=48, out=ok), dict(rope=12), dict(lens=c.d_lens.cpu()), dict(kv_lora=512, out=ok)):
+        with pytest.raises((ValueError, nmm.NmmError)):                 # the binding's checks, the library's
+            c.call(**bad)
+
+
+@FORMATS
+def test_a_sequence_whose_row_is_nan_spoils_no_other(fp8):
+    c = Case(21, 4, 1, 16, 90, [70, 3, 129, 1], 16, fp8)
+    at = int(c.pages[1, 0]) * 16 + 2
+    if fp8:
+        c.cache[at, 5] = 0x7F
+    else:
+        c.cache[at, 5] = float("nan")
+    out = c.call()
+    assert bool(torch.isnan(out[1]).any())
+    ref, mag = c.reference()
+    o = out.double().cpu().numpy()
+    keep = [0, 2, 3]
+    assert (np.abs(o[keep] - ref[keep]) <= (2.0 ** -8 + 2.0 ** -12) * mag[keep] + 2.0 ** -8 * np.abs(ref[keep])).all()

@@ -94,8 +94,121 @@ def test_row_bytes():
         assert nmm.nmm_latent_cache_row_bytes(*bad) == 0
 
 
+def w4_args(**kw):
+    d = dict(M=4, K=512, N=256, dt=nmm.NMM_BF16, format=nmm.NMM_W4_INT, group=128, x=ALIGNED, ldx=512, Wq=ALIGNED, ldwq=256,
+             scales=ALIGNED, lds=4, zeros=ALIGNED, ldz=4, y=ALIGNED, ldy=256, workspace=None, bytes=0, stream=None)
+    d.update(kw)
+    return tuple(d.values())
+
+
+MX = dict(format=nmm.NMM_W4_MX, group=32, zeros=None, lds=16)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=7), nmm.NMM_ERR_DTYPE), (dict(format=0), nmm.NMM_ERR_DTYPE), (dict(format=3), nmm.NMM_ERR_DTYPE),
+    (dict(M=-1), nmm.NMM_ERR_SHAPE), (dict(K=-1), nmm.NMM_ERR_SHAPE), (dict(N=-1), nmm.NMM_ERR_SHAPE),
+    (dict(M=1 << 31), nmm.NMM_ERR_SHAPE), (dict(K=1 << 31), nmm.NMM_ERR_SHAPE), (dict(N=1 << 31), nmm.NMM_ERR_SHAPE),
+    (dict(group=16), nmm.NMM_ERR_SHAPE), (dict(group=96), nmm.NMM_ERR_SHAPE), (dict(group=0), nmm.NMM_ERR_SHAPE),
+    (dict(group=-32), nmm.NMM_ERR_SHAPE), (dict(MX, group=64), nmm.NMM_ERR_SHAPE), (dict(MX, zeros=ALIGNED), nmm.NMM_ERR_ARG),
+    (dict(ldx=504), nmm.NMM_ERR_SHAPE), (dict(ldwq=240), nmm.NMM_ERR_SHAPE), (dict(lds=3), nmm.NMM_ERR_SHAPE),
+    (dict(ldz=3), nmm.NMM_ERR_SHAPE), (dict(ldy=255), nmm.NMM_ERR_SHAPE), (dict(ldx=1 << 31), nmm.NMM_ERR_SHAPE),
+    (dict(ldx=514), nmm.NMM_ERR_ALIGN), (dict(ldwq=264), nmm.NMM_ERR_ALIGN), (dict(x=ALIGNED + 8), nmm.NMM_ERR_ALIGN),
+    (dict(Wq=ALIGNED + 8), nmm.NMM_ERR_ALIGN), (dict(scales=ALIGNED + 1), nmm.NMM_ERR_ALIGN),
+    (dict(y=ALIGNED + 2), nmm.NMM_ERR_ALIGN), (dict(x=None), nmm.NMM_ERR_NULL), (dict(Wq=None), nmm.NMM_ERR_NULL),
+    (dict(scales=None), nmm.NMM_ERR_NULL), (dict(y=None), nmm.NMM_ERR_NULL),
+    (dict(N=1 << 23, ldy=1 << 23), nmm.NMM_ERR_SHAPE),                       # a weight of 2^31 bytes
+    (dict(M=32, ldx=1 << 26), nmm.NMM_ERR_SHAPE),                            # 32 rows of x past 2^31 bytes
+    (dict(K=16384, ldx=16384, ldwq=8192, lds=128, ldz=128), nmm.NMM_ERR_WORKSPACE),
+    (dict(K=16384, ldx=16384, ldwq=8192, lds=128, ldz=128, workspace=ALIGNED, bytes=65536), nmm.NMM_ERR_WORKSPACE),
+])
+def test_gemv_w4_refuses(kw, status):
+    assert L.nmm_gemv_w4(*w4_args(**kw)) == status
+
+
+def test_gemv_w4_empty_and_workspace():
+    assert L.nmm_gemv_w4(*w4_args(M=0, y=None)) == nmm.NMM_OK
+    assert L.nmm_gemv_w4(*w4_args(N=0, y=None)) == nmm.NMM_OK
+    size = L.nmm_gemv_w4_workspace_size
+    for bad in ((-1, 512, 256, 128), (4, -1, 256, 128), (4, 512, -1, 128), (4, 512, 256, 96), (4, 512, 256, 0), (4, 512, 256, 16),
+                (0, 512, 256, 128), (4, 0, 256, 128), (1 << 31, 512, 256, 128)):
+        assert size(*bad) == 0
+    tickets = 65536
+    for M in (1, 2, 4, 5, 8, 9, 16, 17, 33, 100, 20000):
+        for K in (32, 256, 257, 1536, 4099, 7168, 16384, 65536):
+            for N in (1, 63, 512, 2112, 7168, 24576):
+                for group in (32, 64, 128, 1024):
+                    ws = size(M, K, N, group)
+                    rows = 1 if M == 1 else 2 if M == 2 else 4 if M <= 4 else 8 if M <= 8 else 16 if M <= 16 else 32
+                    if K <= 256:
+                        assert ws == 0, (M, K, N, group)
+                    if ws:      # whole partial tiles of at least two slices, no more of them than slots of K
+                        assert (ws - tickets) % (rows * 64) == 0, (M, K, N, group)
+                        assert ws - tickets >= 2 * rows * N * 4
+                        assert ws - tickets <= -(-K // 256) * -(-M // rows) * rows * (N + 127) * 4
+
+
+def batch_of(cache=None, **kw):
+    a = fill(nmm.nmm_latent_attn_batch(), dict(
+        batch=4, tokens=1, heads=16, q=ALIGNED, stride_qb=16 * 576, stride_qt=0, ldq=576, page_size=64, prefix_pages=ALIGNED,
+        prefix_len=128, pages=ALIGNED, ld_pages=8, lens=ALIGNED, max_len=512, scale=0.04, out=ALIGNED, stride_ob=16 * 512,
+        stride_ot=0, ldo=512), kw)
+    a.cache = cache_of(**(cache or {}))
+    return a
+
+
+@pytest.mark.parametrize("cache,status", BAD_CACHE)
+def test_batched_attention_refuses_a_bad_cache(cache, status):
+    assert L.nmm_latent_attention_batch(ctypes.byref(batch_of(cache)), None, 0, None) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(batch=-1), nmm.NMM_ERR_SHAPE), (dict(tokens=-1), nmm.NMM_ERR_SHAPE), (dict(heads=-1), nmm.NMM_ERR_SHAPE),
+    (dict(batch=1 << 20, heads=1), nmm.NMM_ERR_SHAPE), (dict(batch=1 << 14, heads=1 << 10), nmm.NMM_ERR_SHAPE),
+    (dict(batch=1 << 62, tokens=4, heads=1), nmm.NMM_ERR_SHAPE),
+    (dict(prefix_len=-1), nmm.NMM_ERR_SHAPE), (dict(max_len=-1), nmm.NMM_ERR_SHAPE), (dict(max_len=1 << 30), nmm.NMM_ERR_SHAPE),
+    (dict(prefix_len=1 << 30), nmm.NMM_ERR_SHAPE), (dict(page_size=0), nmm.NMM_ERR_SHAPE), (dict(page_size=48), nmm.NMM_ERR_SHAPE),
+    (dict(page_size=1 << 17), nmm.NMM_ERR_SHAPE), (dict(page_size=-64), nmm.NMM_ERR_SHAPE),
+    (dict(ld_pages=7), nmm.NMM_ERR_SHAPE), (dict(ldq=568), nmm.NMM_ERR_SHAPE), (dict(ldo=508), nmm.NMM_ERR_SHAPE),
+    (dict(stride_qb=-8), nmm.NMM_ERR_SHAPE), (dict(stride_ot=-4), nmm.NMM_ERR_SHAPE),
+    (dict(ldq=580), nmm.NMM_ERR_ALIGN), (dict(stride_qb=9220), nmm.NMM_ERR_ALIGN), (dict(stride_qt=4), nmm.NMM_ERR_ALIGN),
+    (dict(ldo=514), nmm.NMM_ERR_ALIGN), (dict(stride_ob=8194), nmm.NMM_ERR_ALIGN), (dict(stride_ot=2), nmm.NMM_ERR_ALIGN),
+    (dict(q=ALIGNED + 8), nmm.NMM_ERR_ALIGN), (dict(out=ALIGNED + 4), nmm.NMM_ERR_ALIGN),
+    (dict(pages=ALIGNED + 2), nmm.NMM_ERR_ALIGN), (dict(lens=ALIGNED + 2), nmm.NMM_ERR_ALIGN),
+    (dict(prefix_pages=ALIGNED + 2), nmm.NMM_ERR_ALIGN),
+    (dict(q=None), nmm.NMM_ERR_NULL), (dict(out=None), nmm.NMM_ERR_NULL), (dict(pages=None), nmm.NMM_ERR_NULL),
+    (dict(lens=None), nmm.NMM_ERR_NULL), (dict(prefix_pages=None), nmm.NMM_ERR_NULL),
+    (dict(scale=float("nan")), nmm.NMM_ERR_ARG), (dict(scale=float("inf")), nmm.NMM_ERR_ARG),
+    (dict(), nmm.NMM_ERR_WORKSPACE),
+])
+def test_batched_attention_refuses(kw, status):
+    assert L.nmm_latent_attention_batch(ctypes.byref(batch_of(**kw)), None, 0, None) == status
+
+
+def test_batched_attention_empty_and_workspace():
+    for kw in (dict(batch=0), dict(tokens=0), dict(heads=0, q=None, out=None)):
+        assert L.nmm_latent_attention_batch(ctypes.byref(batch_of(**kw)), None, 0, None) == nmm.NMM_OK
+    assert L.nmm_latent_attention_batch(None, None, 0, None) == nmm.NMM_ERR_NULL
+    size = lambda **kw: L.nmm_latent_attention_batch_workspace_size(ctypes.byref(batch_of(**kw)))
+    assert L.nmm_latent_attention_batch_workspace_size(None) == 0
+    assert size(batch=-1) == 0 and size(page_size=48) == 0 and size(cache=dict(format=0)) == 0
+    # one span of one kind of positions needs no partial results, nor does nothing at all
+    assert size(prefix_len=0, max_len=64) == 0 and size(max_len=0, prefix_len=64) == 0 and size(prefix_len=0, max_len=0) == 0
+    per_slot = lambda rows: rows * (512 + 2) * 4
+    for batch, heads, prefix, own in ((1, 1, 1, 1), (4, 16, 128, 512), (1, 128, 0, 100000), (64, 16, 0, 4097), (3, 7, 100000, 1),
+                                      (1, 1, (1 << 30) - 1, (1 << 30) - 1)):
+        ws = size(batch=batch, heads=heads, prefix_len=prefix, max_len=own)
+        if prefix and own:
+            assert ws
+        if ws:
+            slots, rest = divmod(ws - 65536, per_slot(batch * heads))
+            assert rest == 0 and 2 <= slots <= 64, (batch, heads, prefix, own)
+
+
 STRUCTS = {"nmm_latent_cache": ["data", "rows", "ld", "kv_lora", "rope", "format"],
-           "nmm_cache_entries": ["tokens", "src", "src_type", "ld_src", "slots", "gamma", "eps", "positions", "rope_theta"]}
+           "nmm_cache_entries": ["tokens", "src", "src_type", "ld_src", "slots", "gamma", "eps", "positions", "rope_theta"],
+           "nmm_latent_attn_batch": ["batch", "tokens", "heads", "q", "stride_qb", "stride_qt", "ldq", "cache", "page_size",
+                                     "prefix_pages", "prefix_len", "pages", "ld_pages", "lens", "max_len", "scale", "out",
+                                     "stride_ob", "stride_ot", "ldo"]}
 
 
 def test_struct_layouts_match_the_header(tmp_path):

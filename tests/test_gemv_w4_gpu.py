@@ -166,3 +166,79 @@ def test_streams_captured_replays_and_the_same_bits():
     other = run(args, 4, 96, stream=side)
     side.synchronize()
     assert torch.equal(other[:, :96], y)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 7, 8, 9, 16, 17, 33])
+@pytest.mark.parametrize("group,mx,zeros", [(32, True, False), (32, False, True), (128, False, True), (512, False, False)])
+def test_every_end_of_a_slot(M, group, mx, zeros):
+    for K in (225, 255, 256, 257, 1023, 1032, 1281, 2311, 4095):       # slots of 256, four of them in flight
+        check(M * K, M, K, 70, group, mx, zeros, fp16=K % 2 == 0)
+
+
+@pytest.mark.parametrize("M", [1, 8, 12, 32])
+def test_many_slices_and_slots(M):
+    check(M, M, 40000, 130, 32, False, True)                           # K-slices as long as their scales allow
+    check(M, M, 40000, 130, 32, True, False)
+    check(M, M, 60001, 65, 4096, False, True)                          # groups longer than a slice
+
+
+def test_more_row_blocks_than_counters():
+    M, K, N = 130, 544, 1 << 19                                        # 128 rows a launch
+    rng = np.random.default_rng(9)
+    x = torch.from_numpy(rng.integers(-4, 5, (M, K)).astype(np.float32)).to(torch.bfloat16).cuda()
+    codes = torch.randint(0, 256, (N, 272), dtype=torch.uint8, device="cuda")
+    scales = (2.0 ** torch.randint(-2, 3, (N, 17), device="cuda")).to(torch.bfloat16)
+    y = torch.full((M, N), float("nan"), device="cuda")
+    nmm.nmm_gemv_w4(x, codes, scales, y, group=32)
+    at = torch.cat((torch.arange(0, N, 4097, device="cuda"), torch.tensor([N - 1], device="cuda")))
+    W = ob.w4_decode(codes[at].cpu().numpy(), scales[at].double().cpu().numpy(), 32, K)
+    assert np.array_equal(y[:, at].double().cpu().numpy(), x.double().cpu().numpy() @ W.T)
+    assert bool(torch.isfinite(y).all())
+
+
+@pytest.mark.parametrize("M", [4, 20])
+@pytest.mark.parametrize("mx", [False, True])
+def test_what_is_not_finite_stays_in_its_row(M, mx):
+    args, ref, _ = make(17, M, 700, 96, 32, mx, not mx, False, True)
+    args["x"][1, 300] = float("inf")
+    args["x"][2, 5] = float("nan")
+    if mx:
+        args["scales"][7, 3] = 255
+    else:
+        args["scales"][7, 3] = float("nan")
+    y = run(args, M, 96)[:, :96].double().cpu().numpy()
+    assert not np.isfinite(y[1]).any()
+    assert np.isnan(y[2]).all() and np.isnan(y[:, 7]).all()
+    rows, cols = np.delete(np.arange(M), [1, 2]), np.delete(np.arange(96), 7)
+    assert np.array_equal(y[np.ix_(rows, cols)], ref[np.ix_(rows, cols)])
+
+
+def test_two_streams_with_their_own_workspaces():
+    args, _, _ = make(3, 4, 16384, 96, 32, False, True, False, integer=False)
+    other, _, _ = make(4, 24, 8192, 200, 128, False, False, False, integer=False)
+    want = run(args, 4, 96)[:, :96].clone(), run(other, 24, 200)[:, :200].clone()
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        y1, y2 = torch.zeros((4, 96), device="cuda"), torch.zeros((24, 200), device="cuda")
+        torch.cuda.synchronize()
+        nmm.nmm_gemv_w4(y=y1, stream=s1, **args)
+        nmm.nmm_gemv_w4(y=y2, stream=s2, **other)
+        torch.cuda.synchronize()
+        assert torch.equal(y1, want[0]) and torch.equal(y2, want[1])
+
+
+def test_python_refusals():
+    x = torch.zeros((2, 64), dtype=torch.bfloat16, device="cuda")
+    w, s, y = torch.zeros((8, 32), dtype=torch.uint8, device="cuda"), torch.zeros_like(x[:1, :2]).repeat(8, 1), torch.zeros((2, 8), device="cuda")
+    z = torch.zeros((8, 2), dtype=torch.uint8, device="cuda")
+    nmm.nmm_gemv_w4(x, w, s, y, group=32, zeros=z)
+    for bad in (dict(x=x.float()), dict(Wq=w.to(torch.int8)), dict(y=y.bfloat16()), dict(scales=s.float()), dict(scales=s.half()),
+                dict(zeros=z.to(torch.int8))):
+        with pytest.raises(TypeError):
+            nmm.nmm_gemv_w4(**{**dict(x=x, Wq=w, scales=s, y=y, group=32, zeros=z), **bad})
+    for bad in (dict(x=x.cpu()), dict(y=y[:1]), dict(y=y[:, :7]), dict(scales=s[:7]), dict(scales=s[:, :1]), dict(zeros=z[:7]),
+                dict(zeros=z[:, :1]), dict(K=65), dict(Wq=w[:, :16]), dict(group=48), dict(group=0), dict(K=-1),
+                dict(scales=z), dict(x=x[0]), dict(Wq=w[0]), dict(y=y[0]), dict(scales=s[:, 0]), dict(x=x.t())):
+        with pytest.raises((ValueError, nmm.NmmError)):                 # the binding's checks, the library's
+            nmm.nmm_gemv_w4(**{**dict(x=x, Wq=w, scales=s, y=y, group=32, zeros=z), **bad})
