@@ -642,7 +642,7 @@ def _same_device(where: str, *tensors) -> None:
     """Every tensor on the current device: the library launches there and reads plain pointers."""
     dev = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and not (t.is_cuda and t.get_device() == dev):
+        if t is not None and t.get_device() != dev:          # (-1 for a host tensor)
             raise ValueError(f"{where}: every tensor must be on the current device (cuda:{dev}), one is on {t.device}")
 
 
@@ -664,13 +664,13 @@ def nmm_gemv_w4(x: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, y: torc
         raise TypeError("x must be bfloat16 or float16, Wq uint8 and y float32")
     if scales.dtype not in (x.dtype, torch.uint8) or (zeros is not None and zeros.dtype != torch.uint8):
         raise TypeError("scales must be of x's type or uint8, zeros uint8")
-    if any(t is not None and t.dim() != 2 for t in (x, Wq, scales, y, zeros)):
+    if x.dim() != 2 or Wq.dim() != 2 or scales.dim() != 2 or y.dim() != 2 or (zeros is not None and zeros.dim() != 2):
         raise ValueError("nmm_gemv_w4 takes 2-D tensors")
-    M, N = x.shape[0], Wq.shape[0]
-    K = x.shape[1] if K is None else K
+    (M, width), (N, half), (n_s, g_s), (m_y, n_y) = x.shape, Wq.shape, scales.shape, y.shape
+    K = width if K is None else K
     groups = -(-K // group) if group > 0 else 0
-    if y.shape[0] < M or y.shape[1] < N or x.shape[1] < K or 2 * Wq.shape[1] < K or scales.shape[0] < N or \
-            scales.shape[1] < groups or (zeros is not None and (zeros.shape[0] < N or zeros.shape[1] < groups)):
+    if m_y < M or n_y < N or width < K or 2 * half < K or n_s < N or g_s < groups or \
+            (zeros is not None and (zeros.shape[0] < N or zeros.shape[1] < groups)):
         raise ValueError("x [M, >= K], Wq [N, >= K / 2], scales and zeros [N, >= groups], y [M, N] do not fit each other")
     fmt = NMM_W4_MX if scales.dtype == torch.uint8 else NMM_W4_INT
     L = lib()
@@ -690,13 +690,12 @@ def _cache_struct(cache: torch.Tensor, kv_lora: int, rope: int) -> nmm_latent_ca
     """The pool [rows, >= row] of a tensor: uint8 for 8-bit rows (in bytes), bfloat16 for bf16 ones."""
     if cache.dim() != 2 or cache.dtype not in (torch.uint8, torch.bfloat16):
         raise TypeError("a latent cache is a 2-D uint8 (8-bit rows) or bfloat16 tensor")
-    c = nmm_latent_cache()
-    c.data, c.rows, c.ld = cache.data_ptr(), cache.shape[0], _ld(cache) * cache.element_size()
-    c.kv_lora, c.rope = int(kv_lora), int(rope)
-    c.format = NMM_CACHE_E4M3 if cache.dtype == torch.uint8 else NMM_CACHE_BF16
-    if cache.shape[1] * cache.element_size() < nmm_latent_cache_row_bytes(kv_lora, rope, c.format):
+    e4m3 = cache.dtype == torch.uint8
+    rows, width = cache.shape
+    if (width < kv_lora + 16 + 2 * rope) if e4m3 else (width < kv_lora + rope):
         raise ValueError("the cache's rows are shorter than its format's")
-    return c
+    return nmm_latent_cache(cache.data_ptr(), rows, _ld(cache) * (1 if e4m3 else 2), int(kv_lora), int(rope),
+                            NMM_CACHE_E4M3 if e4m3 else NMM_CACHE_BF16)
 
 
 def nmm_latent_cache_write(src: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor, *, kv_lora: int, rope: int,
@@ -713,13 +712,9 @@ def nmm_latent_cache_write(src: torch.Tensor, slots: torch.Tensor, cache: torch.
     if gamma is not None and (gamma.dtype != torch.bfloat16 or gamma.shape != (kv_lora,) or gamma.stride(0) != 1):
         raise ValueError("gamma must be a contiguous bfloat16 vector of kv_lora values")
     n = src.shape[0]
-    e = nmm_cache_entries()
-    e.tokens, e.src, e.ld_src = n, src.data_ptr(), _ld(src)
-    e.src_type = NMM_SRC_F32 if src.dtype == torch.float32 else NMM_SRC_BF16
-    e.slots = _index("slots", slots, torch.int64, n)
-    e.gamma, e.eps = gamma.data_ptr() if gamma is not None else None, float(eps)
-    e.positions = _index("positions", positions, torch.int64, n) if positions is not None else None
-    e.rope_theta = float(theta)
+    e = nmm_cache_entries(n, src.data_ptr(), NMM_SRC_F32 if src.dtype == torch.float32 else NMM_SRC_BF16, _ld(src),
+                          _index("slots", slots, torch.int64, n), gamma.data_ptr() if gamma is not None else None, float(eps),
+                          _index("positions", positions, torch.int64, n) if positions is not None else None, float(theta))
     _check(lib().nmm_latent_cache_write(ctypes.byref(_cache_struct(cache, kv_lora, rope)), ctypes.byref(e),
                                         _stream(stream)), "nmm_latent_cache_write")
     return cache
@@ -752,27 +747,29 @@ def nmm_latent_attention_batch(q: torch.Tensor, cache: torch.Tensor, out: torch.
         raise TypeError("q and out must be bfloat16 tensors [batch, (tokens,) heads, width]")
     if out.shape[:-1] != q.shape[:-1] or q.shape[-1] < kv_lora + rope or out.shape[-1] < kv_lora:
         raise ValueError("q and out must have the same batch, tokens and heads, and rows of kv_lora + rope and kv_lora")
-    a = nmm_latent_attn_batch()
-    a.batch, a.tokens, a.heads = q.shape[0], q.shape[1] if q.dim() == 4 else 1, q.shape[-2]
-    a.q, a.stride_qb, a.stride_qt, a.ldq = q.data_ptr(), q.stride(0), q.stride(1) if q.dim() == 4 else 0, _ld(q)
-    a.cache, a.page_size = _cache_struct(cache, kv_lora, rope), int(page_size)
+    batch, tokens, heads, qs, os = q.shape[0], 1, q.shape[-2], q.stride(), out.stride()
+    if q.dim() == 4:
+        tokens, q_t, o_t = q.shape[1], qs[1], os[1]
+    else:
+        q_t = o_t = 0
+    pre = own = n_own = ld_pages = None
     if prefix_len > 0:
         if prefix_pages is None:
             raise ValueError("prefix_pages: a prefix needs its pages")
-        a.prefix_pages = _index("prefix_pages", prefix_pages, torch.int32, -(-prefix_len // max(1, page_size)))
-    a.prefix_len, a.max_len = int(prefix_len), int(max_len)
+        pre = _index("prefix_pages", prefix_pages, torch.int32, -(-prefix_len // max(1, page_size)))
     if max_len > 0:
-        if pages is None or pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] < a.batch or \
+        if pages is None or pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] < batch or \
                 pages.shape[1] * page_size < max_len or (pages.shape[1] > 1 and pages.stride(1) != 1):
             raise ValueError("pages must be an int32 tensor [batch, >= pages of max_len], its last dimension contiguous")
         if lens is None:
             raise ValueError("lens: sequences need their lengths")
-        a.pages, a.ld_pages = pages.data_ptr(), max(pages.stride(0), pages.shape[1])
-        if a.batch > 1 and pages.stride(0) < pages.shape[1]:
+        ld_pages = max(pages.stride(0), pages.shape[1])
+        if batch > 1 and pages.stride(0) < pages.shape[1]:
             raise ValueError("pages: rows may not overlap")
-        a.lens = _index("lens", lens, torch.int32, a.batch)
-    a.scale = float(scale)
-    a.out, a.stride_ob, a.stride_ot, a.ldo = out.data_ptr(), out.stride(0), out.stride(1) if q.dim() == 4 else 0, _ld(out)
+        own, n_own = pages.data_ptr(), _index("lens", lens, torch.int32, batch)
+    a = nmm_latent_attn_batch(batch, tokens, heads, q.data_ptr(), qs[0], q_t, _ld(q), _cache_struct(cache, kv_lora, rope),
+                              int(page_size), pre, int(prefix_len), own, ld_pages or 0, n_own, int(max_len), float(scale),
+                              out.data_ptr(), os[0], o_t, _ld(out))
     L, ref = lib(), ctypes.byref(a)
     _call(L.nmm_latent_attention_batch, "nmm_latent_attention_batch",
           lambda: L.nmm_latent_attention_batch_workspace_size(ref), (ref,), workspace, q.device, stream)
