@@ -221,7 +221,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
 
     // Chunk ck of the walk.  The tiles that read the same rows start their walks at different chunks, so that each
     // row comes from memory once, for one of them, and from L2 for the others.
-    const int first = nchunks ? int(uint32_t(it.tile) * uint32_t(nchunks) / uint32_t(it.tiles)) : 0;
+    const int first = nchunks ? int(uint64_t(it.tile) * uint64_t(nchunks) / uint64_t(it.tiles)) : 0;
     auto start_of = [&](int ck) {
         int c = ck + first;
         c = c >= nchunks ? c - nchunks : c;
@@ -595,7 +595,7 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
     const gbytes zero_row = opaque_zero_row();
 
     // the walk, as in narrow_block
-    const int first = n ? int(uint32_t(it.tile) * uint32_t(n) / uint32_t(it.tiles)) : 0;
+    const int first = n ? int(uint64_t(it.tile) * uint64_t(n) / uint64_t(it.tiles)) : 0;
     auto start_of = [&](int ck) {
         int c = ck + first;
         c = c >= n ? c - n : c;
