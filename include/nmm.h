@@ -452,7 +452,9 @@ nmm_status nmm_mla_decode_step(const nmm_mla_chain* chain, const nmm_latent_attn
  *   NMM_W4_MX   c = the e2m1 value of the code (bit 3 the sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6); s = 2^(b - 127) of a
  *               byte b (255: NaN), group = 32, no zeros
  * Codes are widened exactly, products summed in fp32, and a group's scale is applied to its fp32 sum: no
- * weight is rounded.  Any M (in blocks of up to 32 rows, each reading the weight once).
+ * weight is rounded.  Any M (in blocks of up to 32 rows, each reading the weight once).  A value of x, a scale or a
+ * zero point affects its row of y only (of W: its column); a row of x that holds an infinity or NaN gives values that
+ * are not finite, NaN where the formula would have an infinity (NMM_W4_INT).
  *   dt, x, ldx   as for nmm_gemv_nt.
  *   Wq, ldwq     codes, row-major [N, ceil(K / 2)] bytes, k even in the low four bits; 16-byte aligned, ldwq
  *                in bytes, >= ceil(K / 2) and a multiple of 16 (a row's last 16 bytes are read whole; codes past K
@@ -477,6 +479,7 @@ size_t nmm_gemv_w4_workspace_size(int64_t M, int64_t K, int64_t N, int64_t group
  *   NMM_CACHE_BF16  row = kv_lora latents and rope values, bf16: the rows nmm_mla_kv_update writes
  *   NMM_CACHE_E4M3  row = kv_lora e4m3 codes | 16 scale bytes | rope values in bf16.  Latents
  *                   32 b .. 32 b + 31 share scale byte b: code c stands for e4m3(c) * 2^(byte - 127).
+ *                   Scale bytes past kv_lora / 32 are written as 127 and not read.
  *                   656 bytes at kv_lora 512, rope 64, against 1152.
  *
  *   data     16-byte aligned; row r starts at data + r * ld, ld in BYTES, a multiple of 16 and at least
@@ -566,7 +569,7 @@ nmm_status nmm_latent_cache_read(const nmm_latent_cache* cache, int64_t tokens, 
  *   out   bf16, out[b * stride_ob + t * stride_ot + h * ldo + c], c < kv_lora; 8-byte aligned, strides
  *         and ldo >= kv_lora multiples of 4.
  * Positions on a page outside the pool are left out; a row that sees no position gives zeros.  Results are
- * deterministic.  Workspace: nmm_latent_attention_batch_workspace_size.
+ * deterministic.  out may overlap nothing that the call reads.  Workspace: nmm_latent_attention_batch_workspace_size.
  */
 typedef struct {
     int64_t batch, tokens, heads;

@@ -9,18 +9,27 @@
 // kinds of tile are cut into spans of positions so that their workgroups fill the chip, run in one launch, and
 // leave (reference, sum, unnormalised output) partials which a merge launch joins in a fixed order.
 //
-// One workgroup (4 waves) takes a tile of 16 HT rows over a span, in chunks of 64 positions:
-//  * Staging.  A chunk's rows lie in LDS as bf16, [9 column blocks][64 rows][8 pieces of 16 bytes]: the latents'
+// A workgroup of 4 waves takes a tile over a span, chunk by chunk:
+//  * Staging.  A chunk's rows lie in LDS as bf16, [9 column blocks][positions][8 pieces of 16 bytes]: the latents'
 //    eight blocks of 64 columns, then RoPE's (columns that the cache lacks are zeros).  Piece c of row r sits in
 //    slot c ^ f(r), which keeps the key reads (8 rows, one column) and the transposed value reads (4 rows, 2 pieces)
 //    free of bank conflicts.  bf16 rows come by LDS-direct loads of 8 rows x 128 bytes; 8-bit rows come into
 //    registers a chunk ahead and are widened on their way to LDS (exact: a power of two per 32 values).  A wave's
-//    lanes look up one position's cache row each; rows that do not exist (past the end, on a page outside the
-//    pool) read a row of zeros and are masked.
-//  * S^T = K Q^T, 16 positions a wave, Q in registers as fragments; P = 2^(s - reference), the
-//    reference moved only when a chunk exceeds it by 2^8; O^T = V^T P^T, a quarter of the columns a wave.
+//    lanes look up one position's page each, a chunk before its rows are loaded; rows that do not exist (past the end,
+//    on a page outside the pool) read zeros and are masked.
+//  * S^T = K Q^T, Q in registers as fragments; P = 2^(s - reference), the reference moved only when a chunk
+//    exceeds it by 2^8; O^T = V^T P^T, a quarter of the columns a wave.
 //    Scores, sums and outputs are fp32; P is rounded to bf16 for the matrix cores (2^-9 relative, where the output
 //    itself is rounded to bf16) and summed before its rounding.
+// Tiles of 16 and 32 rows (narrow_block) take chunks of 64 positions, 16 a wave; tiles of 64 (wide_block) chunks of 32 in
+// a software pipeline.
+//
+// What bounds it.  64 sequences of 16 heads over 2049 .. 4097 own positions, 8-bit rows: 48 us for 130 MB (26 us at
+// the rate of a large copy); a chunk of 64 positions takes 6800 cycles of a workgroup, two of them on a CU, of which widening
+// the rows into LDS is 2700.  16 sequences of 128 heads behind 8192 positions, bf16 rows: 66 us for 40 GFLOP (33 us at the rate
+// of a large matrix product); 64 positions take 5300 cycles (6050 with 8-bit rows) where their MFMAs alone would take 2180: every
+// key and value fragment is read from LDS by each of the four waves' quarters, and Q's start (7 us) and the fp32
+// partials' end (4 us, and 8 us of the merge) are not hidden.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -139,7 +148,8 @@ __device__ __forceinline__ int64_t row_offset(int r, int T, int H, int64_t sb, i
 
 // LDS-direct loads of 16-byte pieces of cache rows, a row per lane: with 32-bit offsets into the pool, a row that does
 // not exist out of its range (zeros), or, for a pool of 2 GB and more, with 64-bit addresses and the zero row (the
-// compiler takes those loads to count as LDS operations too, and so waits for every LDS read at once: 10 % slower).
+// compiler takes those loads to count as LDS operations too, and so waits for every LDS read at once: 71 instead of
+// 69 us for 16 x 128 heads behind 8192 positions).
 template <bool BIG>
 struct StageRows;
 template <>
@@ -210,7 +220,8 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
     static_assert(HT == 1 || HT == 2, "16 or 32 rows");
     constexpr int kAhead = HT == 2 ? 6 : 9, kAheadV = 8;
     // 16 rows: one chunk buffer (kv_b is kv_a), so that two workgroups share a CU and one's loads run beside the
-    // other's work; a chunk is staged between two others' work instead of beside it
+    // other's work; a chunk is staged between two others' work instead of beside it (64 x 16 heads over 4097 positions: 53
+    // to 48.5 us with 8-bit rows, 68 to 62 with bf16 ones)
     constexpr bool SINGLE = HT == 1;
     const int tid = threadIdx.x, lane = tid & 63;
     const int pw = __builtin_amdgcn_readfirstlane(tid >> 6) & (kWavesB - 1);
@@ -1142,12 +1153,14 @@ struct BatchPlan {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Time of a chunk in a tile of 16 ht rows, relative to 16 rows.
+// Time of a chunk in a tile of 16 ht rows, relative to 16 rows (measured, per 64 positions).
 int chunk_cost(int ht) { return ht == 4 ? 16 : ht == 2 ? 11 : 10; }
 
 // The partition in tiles of 16 ht rows, and an estimate of its time.
 int64_t plan_tiles(const nmm_latent_attn_batch& a, int ht, BatchPlan* out) {
-    const int64_t kCus = ht == 1 ? 512 : 256;      // workgroups that run at once
+    // workgroups that run at once (16 rows, two a CU: 50.0 us with spans for 256, 48.5 for 512, 62 for 768 at 64 x 16 heads
+    // over 4097 positions)
+    const int64_t kCus = ht == 1 ? 512 : 256;
     BatchPlan q;
     q.ht = ht;
     const int64_t th = a.tokens * a.heads, rows = a.batch * th;
@@ -1199,8 +1212,10 @@ int64_t plan_tiles(const nmm_latent_attn_batch& a, int ht, BatchPlan* out) {
     return best;
 }
 
-// A sequence's own positions take the smallest tile that holds its rows; with a prefix, whose rows are all
-// sequences', tiles of 64 for both where that is estimated to be faster.
+// A sequence's own positions take the smallest tile that holds its rows (16 heads, 64 sequences over 4097 positions: 48.9 us
+// in tiles of 16, 55.8 of 32, 60.1 of 64; 32 heads, 16 over 2000: 21.4 in tiles of 32, 25.2 of 64); with a prefix, whose rows
+// are all sequences', tiles of 64 for both where that is estimated to be faster (32 x 2 x 16 behind 16000: 70.8 us against
+// 85.0; 8 x 16 behind 2000 stays at 16: 16.9 against 22.3).
 void plan_batch(const nmm_latent_attn_batch& a, BatchPlan* out) {
     const int64_t th = a.tokens * a.heads;
     const int ht = th <= 16 ? 1 : th <= 32 ? 2 : 4;

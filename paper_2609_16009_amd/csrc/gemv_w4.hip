@@ -3,21 +3,29 @@
 //
 // The weight is what has to be read, a quarter of a 16-bit one's bytes, so at few rows of x the work is to
 // keep enough of it in flight and to widen it in the shadow of its loads:
-//  * A workgroup owns 64 NT rows of the weight, 16 NT a wave, and a slice of K.  x's rows of the slice are staged in
-//    LDS once, for all waves, and so are the rows' scales and zero points; then each wave streams its rows through a ring
-//    of its own, D slots of 256 k (128 bytes, one cache line, of each row) in flight, with no barrier in the loop.
+//  * A workgroup owns 16 rows of the weight per wave (4 to 8 waves) and a slice of K, which its waves stream through a ring
+//    in LDS, four slots of 256 k (128 bytes, one cache line, of each row).
 //    Loads go straight to LDS, 8 rows x 128 bytes each; chunks of 16 bytes are permuted within a row so that
-//    fragment reads hit every bank once.
+//    fragment reads hit every bank once.  The slice's scales and zero points are staged once, beside the first slots.
+//  * Up to 8 rows of x (w4_few_kernel) x's part of the slice is staged once too and each wave goes through its rows on its own,
+//    with no barrier in the loop.  More rows (w4_rows_kernel, 16 or 32 at a time) lie in the ring beside the weight, a barrier a
+//    slot; a wave there multiplies 32 rows of the weight and half of a slot.
 //  * Chunk i of a row is 32 k, one step of v_mfma_f32_16x16x32 and one group at most: lane (g, j) reads dword g
 //    of row j, 8 codes, and widens them exactly.  An integer code u is, as the e4m3 byte u, the number
 //    u * 2^-9 (subnormals and the first binade of e4m3 are one uniform grid), so v_cvt_scalef32_pk_{bf16,f16}_fp8 with
 //    a scale of 2^9 yields u; e2m1 has v_cvt_scalef32_pk_{bf16,f16}_fp4.  No weight is ever rounded: the scale is applied
 //    to the group's fp32 sum.
-//  * Zero points: sum_k x (u - z) = sum_k x u - z sum_k x, the second sum by one more MFMA with ones per
-//    step, shared by the wave's row tiles.
+//  * Zero points: sum_k x (u - z) = sum_k x u - z sum_k x.  The second sum is taken once per workgroup while the first slots
+//    are on their way (up to 8 rows of x), or by one more MFMA with ones a step.
 //  * x is the A operand and the weight the B operand, so that a lane's four sums belong to one weight row
 //    and share its scale.
 //  * K is split over workgroups to fill the chip; the last to finish adds the slices in slice order (handoff.h).
+//
+// What bounds it.  One row of x, K 16384, N 7168, groups of 128: 16.2 us for 60.6 MB (14.1 us called in a row), 3.7 TB/s; the
+// same launch without its products 13.9 us, without scales and hand-over either 11.7 (5.2 TB/s), so what widening the codes
+// adds is most of the rest: 9 instructions for 512 codes, and a SIMD holds two waves.  8 rows, K 1536, N 24576, a power of
+// two per 32: 9.4 us for 20.9 MB (9.0 without products), six slots a workgroup and so mostly the start.  32 rows of K 16384,
+// N 7168: 28 us, 269 TFLOP/s (22 without products, 18.8 without x's loads either); the MFMAs of x's sums are 2.5 us of it.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -594,6 +602,10 @@ struct W4Plan {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kLim = int64_t(1) << 31;
+// The partition's estimate, in the time that a wave's slot of 2 KB takes at a CU's share of the memory rate (170 cycles): a CU
+// takes its workgroups one after the other, each its waves' slots and a start (2 us), and a split K once the hand-over
+// (1.4 us).  One row, K 16384, N 7168: 16.5 us in 256 workgroups of 7 waves and 16 slots; in workgroups of 4 waves, two a
+// CU, 17.8 in 448 and 21.5 in 560, which are 3 on some CUs; K 512, N 512: 4.2 us in 8 workgroups of 4 waves, 4.7 in 4 of 8.
 constexpr int64_t kCus = 256;
 constexpr int64_t kStartCost = 28, kSplitCost = 20;
 
