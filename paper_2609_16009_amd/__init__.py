@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -134,10 +135,10 @@ EXPORTS = {
                                    _i64, _p, _i64, _p, _sz, _p]),
     "nmm_gemv_w4_workspace_size": (_sz, [_i64, _i64, _i64, _i64]),
     "nmm_latent_cache_row_bytes": (_sz, [ctypes.c_int, _i64, _i64]),
-    "nmm_latent_cache_write": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), ctypes.POINTER(nmm_cache_entries), _p]),
-    "nmm_latent_cache_read": (ctypes.c_int, [ctypes.POINTER(nmm_latent_cache), _i64, _p, _p, _i64, _p]),
-    "nmm_latent_attention_batch": (ctypes.c_int, [ctypes.POINTER(nmm_latent_attn_batch), _p, _sz, _p]),
-    "nmm_latent_attention_batch_workspace_size": (_sz, [ctypes.POINTER(nmm_latent_attn_batch)]),
+    "nmm_latent_cache_write": (ctypes.c_int, [_p, _p, _p]),
+    "nmm_latent_cache_read": (ctypes.c_int, [_p, _i64, _p, _p, _i64, _p]),
+    "nmm_latent_attention_batch": (ctypes.c_int, [_p, _p, _sz, _p]),
+    "nmm_latent_attention_batch_workspace_size": (_sz, [_p]),
     "nmm_gemv_workspace_size": (_sz, [_i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_batched_gemv_workspace_size": (_sz, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_mla_decode_chain_workspace_size": (_sz, [ctypes.POINTER(nmm_mla_chain)]),
@@ -648,9 +649,17 @@ def _same_device(where: str, *tensors) -> None:
 
 def _index(where: str, t: torch.Tensor, dtype: torch.dtype, n: int) -> int:
     """The address of n contiguous indices."""
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or (n > 1 and t.stride(0) != 1):
+    if t.dtype != dtype or t.dim() != 1 or t.numel() < n or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{where}: indices must be a contiguous {dtype} vector of at least {n}")
     return t.data_ptr()
+
+
+# The bytes of nmm_latent_cache, nmm_cache_entries and nmm_latent_attn_batch.  (Packed in one go: filling a ctypes structure takes
+# three times as long, a tenth of a small call.)
+_CACHE_FIELDS = "Pqqqqi4x"
+_CACHE = struct.Struct("@" + _CACHE_FIELDS)
+_ENTRIES = struct.Struct("@qPi4xqPPf4xPf4x")
+_ATTN_BATCH = struct.Struct("@qqqPqqq" + _CACHE_FIELDS + "qPqPqPqf4xPqqq")
 
 
 def nmm_gemv_w4(x: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, y: torch.Tensor, *, group: int,
@@ -664,7 +673,7 @@ def nmm_gemv_w4(x: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, y: torc
         raise TypeError("x must be bfloat16 or float16, Wq uint8 and y float32")
     if scales.dtype not in (x.dtype, torch.uint8) or (zeros is not None and zeros.dtype != torch.uint8):
         raise TypeError("scales must be of x's type or uint8, zeros uint8")
-    if x.dim() != 2 or Wq.dim() != 2 or scales.dim() != 2 or y.dim() != 2 or (zeros is not None and zeros.dim() != 2):
+    if not (x.dim() == Wq.dim() == scales.dim() == y.dim() == 2 and (zeros is None or zeros.dim() == 2)):
         raise ValueError("nmm_gemv_w4 takes 2-D tensors")
     (M, width), (N, half), (n_s, g_s), (m_y, n_y) = x.shape, Wq.shape, scales.shape, y.shape
     K = width if K is None else K
@@ -672,11 +681,11 @@ def nmm_gemv_w4(x: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, y: torc
     if m_y < M or n_y < N or width < K or 2 * half < K or n_s < N or g_s < groups or \
             (zeros is not None and (zeros.shape[0] < N or zeros.shape[1] < groups)):
         raise ValueError("x [M, >= K], Wq [N, >= K / 2], scales and zeros [N, >= groups], y [M, N] do not fit each other")
-    fmt = NMM_W4_MX if scales.dtype == torch.uint8 else NMM_W4_INT
+    z, ldz = (None, 0) if zeros is None else (zeros.data_ptr(), _ld(zeros))
     L = lib()
     _call(L.nmm_gemv_w4, "nmm_gemv_w4", lambda: L.nmm_gemv_w4_workspace_size(M, K, N, group),
-          (M, K, N, code, fmt, group, x.data_ptr(), _ld(x), Wq.data_ptr(), _ld(Wq), scales.data_ptr(), _ld(scales),
-           zeros.data_ptr() if zeros is not None else None, _ld(zeros) if zeros is not None else 0, y.data_ptr(), _ld(y)),
+          (M, K, N, code, NMM_W4_MX if scales.dtype == torch.uint8 else NMM_W4_INT, group, x.data_ptr(), _ld(x),
+           Wq.data_ptr(), _ld(Wq), scales.data_ptr(), _ld(scales), z, ldz, y.data_ptr(), _ld(y)),
           workspace, x.device, stream)
     return y
 
@@ -686,16 +695,17 @@ def nmm_latent_cache_row_bytes(kv_lora: int, rope: int, format: int = NMM_CACHE_
     return int(lib().nmm_latent_cache_row_bytes(format, kv_lora, rope))
 
 
-def _cache_struct(cache: torch.Tensor, kv_lora: int, rope: int) -> nmm_latent_cache:
-    """The pool [rows, >= row] of a tensor: uint8 for 8-bit rows (in bytes), bfloat16 for bf16 ones."""
-    if cache.dim() != 2 or cache.dtype not in (torch.uint8, torch.bfloat16):
-        raise TypeError("a latent cache is a 2-D uint8 (8-bit rows) or bfloat16 tensor")
+def _pool(cache: torch.Tensor, kv_lora: int, rope: int) -> tuple:
+    """The fields of nmm_latent_cache for a tensor [rows, >= row]: uint8 for 8-bit rows (in bytes), bfloat16 for bf16 ones."""
     e4m3 = cache.dtype == torch.uint8
+    if cache.dim() != 2 or not (e4m3 or cache.dtype == torch.bfloat16):
+        raise TypeError("a latent cache is a 2-D uint8 (8-bit rows) or bfloat16 tensor")
     rows, width = cache.shape
     if (width < kv_lora + 16 + 2 * rope) if e4m3 else (width < kv_lora + rope):
         raise ValueError("the cache's rows are shorter than its format's")
-    return nmm_latent_cache(cache.data_ptr(), rows, _ld(cache) * (1 if e4m3 else 2), int(kv_lora), int(rope),
-                            NMM_CACHE_E4M3 if e4m3 else NMM_CACHE_BF16)
+    ld = _ld(cache)
+    return (cache.data_ptr(), rows, ld, kv_lora, rope, NMM_CACHE_E4M3) if e4m3 else \
+        (cache.data_ptr(), rows, 2 * ld, kv_lora, rope, NMM_CACHE_BF16)
 
 
 def nmm_latent_cache_write(src: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor, *, kv_lora: int, rope: int,
@@ -705,18 +715,19 @@ def nmm_latent_cache_write(src: torch.Tensor, slots: torch.Tensor, cache: torch.
     and, where the cache is uint8, its latents to 8 bits.  src [tokens, >= kv_lora + rope] fp32 or bf16; slots and
     positions int64 [tokens]; without gamma no RMSNorm, without positions no RoPE.  A slot outside the cache is skipped."""
     _same_device("nmm_latent_cache_write", src, slots, cache, gamma, positions)
-    if src.dim() != 2 or src.dtype not in (torch.float32, torch.bfloat16):
+    src32 = src.dtype == torch.float32
+    if src.dim() != 2 or not (src32 or src.dtype == torch.bfloat16):
         raise TypeError("src must be a 2-D float32 or bfloat16 tensor")
-    if src.shape[1] < kv_lora + rope:
+    n, width = src.shape
+    if width < kv_lora + rope:
         raise ValueError("src's rows are shorter than kv_lora + rope")
-    if gamma is not None and (gamma.dtype != torch.bfloat16 or gamma.shape != (kv_lora,) or gamma.stride(0) != 1):
+    if gamma is not None and (gamma.dtype != torch.bfloat16 or gamma.dim() != 1 or gamma.numel() != kv_lora or gamma.stride(0) != 1):
         raise ValueError("gamma must be a contiguous bfloat16 vector of kv_lora values")
-    n = src.shape[0]
-    e = nmm_cache_entries(n, src.data_ptr(), NMM_SRC_F32 if src.dtype == torch.float32 else NMM_SRC_BF16, _ld(src),
-                          _index("slots", slots, torch.int64, n), gamma.data_ptr() if gamma is not None else None, float(eps),
-                          _index("positions", positions, torch.int64, n) if positions is not None else None, float(theta))
-    _check(lib().nmm_latent_cache_write(ctypes.byref(_cache_struct(cache, kv_lora, rope)), ctypes.byref(e),
-                                        _stream(stream)), "nmm_latent_cache_write")
+    entries = _ENTRIES.pack(n, src.data_ptr(), NMM_SRC_F32 if src32 else NMM_SRC_BF16, _ld(src),
+                            _index("slots", slots, torch.int64, n), 0 if gamma is None else gamma.data_ptr(), eps,
+                            0 if positions is None else _index("positions", positions, torch.int64, n), theta)
+    _check(lib().nmm_latent_cache_write(_CACHE.pack(*_pool(cache, kv_lora, rope)), entries, _stream(stream)),
+           "nmm_latent_cache_write")
     return cache
 
 
@@ -727,7 +738,7 @@ def nmm_latent_cache_read(cache: torch.Tensor, slots: torch.Tensor, out: torch.T
     if out.dim() != 2 or out.dtype != torch.bfloat16 or out.shape[1] < kv_lora + rope:
         raise ValueError("out must be a bfloat16 tensor [tokens, >= kv_lora + rope]")
     n = out.shape[0]
-    _check(lib().nmm_latent_cache_read(ctypes.byref(_cache_struct(cache, kv_lora, rope)), n,
+    _check(lib().nmm_latent_cache_read(_CACHE.pack(*_pool(cache, kv_lora, rope)), n,
                                        _index("slots", slots, torch.int64, n), out.data_ptr(), _ld(out),
                                        _stream(stream)), "nmm_latent_cache_read")
     return out
@@ -743,36 +754,32 @@ def nmm_latent_attention_batch(q: torch.Tensor, cache: torch.Tensor, out: torch.
     bf16; cache [rows, ...] uint8 (8-bit rows) or bf16 in pages of page_size rows; pages int32 [batch, >= pages of
     max_len], lens int32 [batch] (this step's tokens counted), prefix_pages int32."""
     _same_device("nmm_latent_attention_batch", q, cache, out, pages, lens, prefix_pages)
-    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.dim() not in (3, 4) or out.dim() != q.dim():
+    dims, shape, o_shape, qs, os = q.dim(), q.shape, out.shape, q.stride(), out.stride()
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or dims not in (3, 4) or len(o_shape) != dims:
         raise TypeError("q and out must be bfloat16 tensors [batch, (tokens,) heads, width]")
-    if out.shape[:-1] != q.shape[:-1] or q.shape[-1] < kv_lora + rope or out.shape[-1] < kv_lora:
+    if o_shape[:-1] != shape[:-1] or shape[-1] < kv_lora + rope or o_shape[-1] < kv_lora:
         raise ValueError("q and out must have the same batch, tokens and heads, and rows of kv_lora + rope and kv_lora")
-    batch, tokens, heads, qs, os = q.shape[0], 1, q.shape[-2], q.stride(), out.stride()
-    if q.dim() == 4:
-        tokens, q_t, o_t = q.shape[1], qs[1], os[1]
-    else:
-        q_t = o_t = 0
-    pre = own = n_own = ld_pages = None
+    batch, heads = shape[0], shape[-2]
+    tokens, q_t, o_t = (shape[1], qs[1], os[1]) if dims == 4 else (1, 0, 0)
+    pre = own = n_own = ld_pages = 0
     if prefix_len > 0:
         if prefix_pages is None:
             raise ValueError("prefix_pages: a prefix needs its pages")
         pre = _index("prefix_pages", prefix_pages, torch.int32, -(-prefix_len // max(1, page_size)))
     if max_len > 0:
-        if pages is None or pages.dtype != torch.int32 or pages.dim() != 2 or pages.shape[0] < batch or \
-                pages.shape[1] * page_size < max_len or (pages.shape[1] > 1 and pages.stride(1) != 1):
-            raise ValueError("pages must be an int32 tensor [batch, >= pages of max_len], its last dimension contiguous")
+        if pages is None or pages.dtype != torch.int32 or pages.dim() != 2:
+            raise ValueError("pages must be an int32 tensor [batch, >= pages of max_len]")
+        (rows, width), (step, one) = pages.shape, pages.stride()
+        if rows < batch or width * page_size < max_len or (width > 1 and one != 1) or (batch > 1 and step < width):
+            raise ValueError("pages must be an int32 tensor [batch, >= pages of max_len], its rows contiguous and apart")
         if lens is None:
             raise ValueError("lens: sequences need their lengths")
-        ld_pages = max(pages.stride(0), pages.shape[1])
-        if batch > 1 and pages.stride(0) < pages.shape[1]:
-            raise ValueError("pages: rows may not overlap")
-        own, n_own = pages.data_ptr(), _index("lens", lens, torch.int32, batch)
-    a = nmm_latent_attn_batch(batch, tokens, heads, q.data_ptr(), qs[0], q_t, _ld(q), _cache_struct(cache, kv_lora, rope),
-                              int(page_size), pre, int(prefix_len), own, ld_pages or 0, n_own, int(max_len), float(scale),
-                              out.data_ptr(), os[0], o_t, _ld(out))
-    L, ref = lib(), ctypes.byref(a)
+        own, n_own, ld_pages = pages.data_ptr(), _index("lens", lens, torch.int32, batch), max(step, width)
+    args = _ATTN_BATCH.pack(batch, tokens, heads, q.data_ptr(), qs[0], q_t, _ld(q), *_pool(cache, kv_lora, rope), page_size, pre,
+                            prefix_len, own, ld_pages, n_own, max_len, scale, out.data_ptr(), os[0], o_t, _ld(out))
+    L = lib()
     _call(L.nmm_latent_attention_batch, "nmm_latent_attention_batch",
-          lambda: L.nmm_latent_attention_batch_workspace_size(ref), (ref,), workspace, q.device, stream)
+          lambda: L.nmm_latent_attention_batch_workspace_size(args), (args,), workspace, q.device, stream)
     return out
 
 

@@ -228,3 +228,17 @@ def test_struct_layouts_match_the_header(tmp_path):
         assert got[(st, "sizeof")] == ctypes.sizeof(cls), st
         for f in fields:
             assert got[(st, f)] == getattr(cls, f).offset, (st, f)
+
+
+def test_packed_arguments_match_the_structs():
+    c = cache_of(data=1 << 40, rows=7, ld=672, rope=32, kv_lora=256, format=nmm.NMM_CACHE_BF16)
+    pool = (1 << 40, 7, 672, 256, 32, nmm.NMM_CACHE_BF16)
+    assert nmm._CACHE.pack(*pool) == bytes(c)
+    e = entries_of(tokens=3, src=1 << 41, src_type=nmm.NMM_SRC_BF16, ld_src=584, slots=1 << 42, gamma=None, eps=0.5, positions=8,
+                   rope_theta=2.0)
+    assert nmm._ENTRIES.pack(3, 1 << 41, nmm.NMM_SRC_BF16, 584, 1 << 42, 0, 0.5, 8, 2.0) == bytes(e)
+    a = batch_of(dict(data=1 << 40, rows=7, ld=672, rope=32, kv_lora=256, format=nmm.NMM_CACHE_BF16), batch=2, tokens=3, heads=5,
+                 q=1 << 43, stride_qb=11, stride_qt=12, ldq=13, page_size=16, prefix_pages=1 << 44, prefix_len=17, pages=1 << 45,
+                 ld_pages=18, lens=1 << 46, max_len=19, scale=0.25, out=1 << 47, stride_ob=20, stride_ot=21, ldo=22)
+    assert nmm._ATTN_BATCH.pack(2, 3, 5, 1 << 43, 11, 12, 13, *pool, 16, 1 << 44, 17, 1 << 45, 18, 1 << 46, 19, 0.25, 1 << 47, 20,
+                                21, 22) == bytes(a)
