@@ -359,20 +359,38 @@ __device__ __forceinline__ void finish(const W4Params& p, const W4Tile& w, int t
     if (tid == 0) s_last = arrive(p.tickets + tile, unsigned(p.ks));
     __syncthreads();
     if (!s_last) return;
-    constexpr int kBatch = 8;
-    for (int o = tid; o < w.rows * w.mrows; o += threads) {
-        float v = 0.f;
+    // four columns a thread, two of them at once and four slices: one round trip for most
+    constexpr int kBatch = 4, kPieces = 2;
+    const int total = w.rows * w.mrows;
+    for (int o0 = 4 * tid; o0 < total; o0 += 4 * kPieces * threads) {
+        f32x4 v[kPieces];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int q0 = 0; q0 < p.ks; q0 += kBatch) {
-            float u[kBatch];
+            f32x4 u[kPieces][kBatch];
 #pragma unroll
-            for (int q = 0; q < kBatch; ++q)
-                u[q] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
-                    pr, q0 + q < p.ks ? uint32_t((q0 + q) * part + o) * 4u : kOutOfRange, 0, kDevice));
+            for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-            for (int q = 0; q < kBatch; ++q) v += u[q];
+                for (int q = 0; q < kBatch; ++q) {
+                    const int o = o0 + 4 * i * threads;
+                    u[i][q] = __builtin_bit_cast(
+                        f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                   pr, q0 + q < p.ks && o < total ? uint32_t((q0 + q) * part + o) * 4u : kOutOfRange, 0, kDevice));
+                }
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                for (int q = 0; q < kBatch; ++q) v[i] += u[i][q];
         }
-        const int m = o / w.rows, n = w.n0 + o - m * w.rows;
-        if (n < p.N) p.y[int64_t(w.m0 + m) * p.ldy + n] = v;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int o = o0 + 4 * i * threads;
+            const int m = o / w.rows, n = w.n0 + o - m * w.rows;
+            if (o >= total) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < p.N) p.y[int64_t(w.m0 + m) * p.ldy + n + e] = v[i][e];
+        }
     }
 }
 
