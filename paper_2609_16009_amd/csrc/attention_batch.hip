@@ -216,9 +216,10 @@ template <int HT, bool E4M3, bool BIG>
 __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it, uint16_t* const kv_a, uint16_t* const kv_b,
                                             uint16_t* const pbuf, float* const red, int* const flags) {
     constexpr int HB = 16 * HT;
-    // K and V fragments read ahead of their MFMAs: LDS takes about 130 cycles, a step's HT MFMAs 16 HT
+    // K and V fragments read ahead of their MFMAs: LDS takes about 130 cycles, a step's HT MFMAs 16 HT.  (16 rows: two
+    // workgroups a CU have half the registers each, and hide the rest for each other: 47.3 us with 9 and 8 ahead, 45.5 with 4.)
     static_assert(HT == 1 || HT == 2, "16 or 32 rows");
-    constexpr int kAhead = HT == 2 ? 6 : 9, kAheadV = 8;
+    constexpr int kAhead = HT == 2 ? 6 : 4, kAheadV = HT == 2 ? 8 : 4;
     // 16 rows: one chunk buffer (kv_b is kv_a), so that two workgroups share a CU and one's loads run beside the
     // other's work; a chunk is staged between two others' work instead of beside it (64 x 16 heads over 4097 positions: 53
     // to 48.5 us with 8-bit rows, 68 to 62 with bf16 ones)
@@ -298,7 +299,6 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
             *reinterpret_cast<u32x4*>(dst + 2 * i * kBlockElems + w8_second) = hi8 ? lo : up;
         }
     };
-    auto commit_at = [&](uint16_t* buf, int ps, int step) { commit_part(buf, ps, step); };
 
     // ---- Q rows to buffer b, in the chunk's layout (rows past the tile's and columns past the cache's: zeros)
     {
@@ -318,13 +318,15 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
         }
     }
     int rows_cur = row_of(start_of(0));
-    auto stage_chunk = [&](int rows, uint16_t* buf) {
+    // (rows_after: 16 rows, 8 bits: what is loaded next)
+    auto stage_chunk = [&](int rows, uint16_t* buf, int rows_after) {
         if constexpr (E4M3) {
 #pragma unroll
             for (int ps = 0; ps < 2; ++ps) {
                 if constexpr (!SINGLE) load_raw(rows, ps);
 #pragma unroll
-                for (int i = 0; i < 5; ++i) commit_at(buf, ps, i);
+                for (int i = 0; i < 5; ++i) commit_part(buf, ps, i);
+                if constexpr (SINGLE) load_raw(rows_after, ps);
             }
         } else {
 #pragma unroll
@@ -339,7 +341,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
         load_raw(rows_cur, 0);
         load_raw(rows_cur, 1);
     }
-    if constexpr (!SINGLE) stage_chunk(rows_cur, kv_a);
+    if constexpr (!SINGLE) stage_chunk(rows_cur, kv_a, -1);
     int rows_next = row_of(start_of(1));
     __builtin_amdgcn_s_waitcnt(0);
     lds_sync();
@@ -360,7 +362,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
         for (int u = 0; u < kSteps; ++u)
             asm("" : "+a"(qf[t][u]));
     if constexpr (SINGLE) {
-        stage_chunk(rows_cur, kv_a);
+        stage_chunk(rows_cur, kv_a, rows_next);
         if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);
         lds_sync();
     } else if constexpr (E4M3) {
@@ -401,10 +403,6 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
         const uint64_t present = __builtin_amdgcn_ballot_w64(rows_cur >= 0);
         // the next chunk (behind the last: rows of zeros, which nothing reads)
         typename StageRows<BIG>::Row rp[2];
-        if constexpr (E4M3 && SINGLE) {
-            load_raw(rows_next, 0);
-            load_raw(rows_next, 1);
-        }
         if constexpr (!E4M3 && !SINGLE) {
             rp[0] = stage.row(rows_next, 16 * pw + (lane >> 3));
             rp[1] = stage.row(rows_next, 16 * pw + 8 + (lane >> 3));
@@ -432,7 +430,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
             if constexpr (SINGLE) {
             } else if constexpr (E4M3) {
                 // the first half of the next chunk's rows, in the MFMAs' shadow
-                if (u % 3 == 2 && u < 15) commit_at(nxt, 0, u / 3);
+                if (u % 3 == 2 && u < 15) commit_part(nxt, 0, u / 3);
                 if (u == 15) load_raw(rows_next, 1);
             } else {
                 stage_bf16(rp[u & 1], nxt, u >> 1, u & 1);
@@ -543,7 +541,7 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
             if (v + kAheadV < 2 * kTilesW) vf[v % kAheadV] = v_frag(v + kAheadV);
             if constexpr (E4M3 && !SINGLE) {
                 // the second half of the next chunk's rows; then the loads of the one after it
-                if (v % 3 == 2 && v < 15) commit_at(nxt, 1, v / 3);
+                if (v % 3 == 2 && v < 15) commit_part(nxt, 1, v / 3);
                 if (v == 15) {
                     rows_after = row_at(page_after, start_of(ck + 2));
                     load_raw(rows_after, 0);
@@ -552,13 +550,15 @@ __device__ __forceinline__ void narrow_block(const BatchParams& p, const Item it
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (SINGLE) {
-            // every wave is done with this chunk: the next one takes its place
+            // every wave is done with this chunk: the next one takes its place, and as its registers fall free the one
+            // after it is loaded
             lds_sync();
-            stage_chunk(rows_next, nxt);
+            rows_after = row_at(page_after, start_of(ck + 2));
+            stage_chunk(rows_next, nxt, rows_after);
         }
         // the next chunk has landed, and every wave is done with this one and with P
         if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);
-        if constexpr (!E4M3 || SINGLE) rows_after = row_at(page_after, start_of(ck + 2));
+        if constexpr (!E4M3 && !SINGLE) rows_after = row_at(page_after, start_of(ck + 2));
         rows_cur = rows_next;
         rows_next = rows_after;
         lds_sync();
