@@ -24,9 +24,10 @@
 // Tiles of 16 and 32 rows (narrow_block) take chunks of 64 positions, 16 a wave; tiles of 64 (wide_block) chunks of 32 in
 // a software pipeline.
 //
-// What bounds it.  64 sequences of 16 heads over 2049 .. 4097 own positions, 8-bit rows: 48 us for 130 MB (26 us at
-// the rate of a large copy); a chunk of 64 positions takes 6800 cycles of a workgroup, two of them on a CU, of which widening
-// the rows into LDS is 2700.  16 sequences of 128 heads behind 8192 positions, bf16 rows: 66 us for 40 GFLOP (33 us at the rate
+// What bounds it.  64 sequences of 16 heads over 2049 .. 4097 own positions, 8-bit rows: 46 us for 130 MB (26 us at
+// the rate of a large copy), 38 where all rows come from L2: two workgroups a CU spend more on widening the rows into LDS than on
+// the products, each with one chunk's loads in flight.  16 sequences of 128 heads behind 8192 positions, bf16 rows: 66 us for
+// 40 GFLOP (33 us at the rate
 // of a large matrix product); 64 positions take 5300 cycles (6050 with 8-bit rows) where their MFMAs alone would take 2180: every
 // key and value fragment is read from LDS by each of the four waves' quarters, and Q's start (7 us) and the fp32
 // partials' end (4 us, and 8 us of the merge) are not hidden.

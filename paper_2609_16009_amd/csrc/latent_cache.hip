@@ -7,13 +7,14 @@
 // the bf16 row that the same token would have had.  v * 2^-e is exact, so a code has one rounding.
 //
 //  * Writing: a wave owns a token, a lane eight latents, four lanes a scale block, whose maximum meets by
-//    two DPP exchanges; the sum of squares is a butterfly over the wave.  Lanes below rope / 2 take a RoPE
+//    two DPP exchanges; the sum of squares is a butterfly over the wave, and RMSNorm and RoPE are in fp64 up to
+//    the entry's rounding.  Lanes below rope / 2 take a RoPE
 //    pair each.  Nothing leaves the wave, so tokens need no barrier and any number of them fills the chip.
 //  * Reading: a thread owns 16 bytes of an output row, so stores are whole lines and the loads of a row
 //    are contiguous too.
 // Bound by bytes for many rows and by one chain of round trips for few: 40001 8-bit rows of 656 bytes read into bf16
-// ones in 16.1 us (72 MB, 4.5 TB/s, against 5.1 of a large copy); 8192 rows written from fp32 and read back 14.0 us (two
-// launches, 39 MB), of which RoPE's angles in fp64 are 0.9; 64 rows 5.8 us, 2.9 a launch.
+// ones in 16.1 us (72 MB, 4.5 TB/s, against 5.1 of a large copy); 8192 rows written from fp32 and read back 14.9 us (two
+// launches, 39 MB), of which RMSNorm and RoPE in fp64 are 1.8; 64 rows 5.8 us, 2.9 a launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -50,16 +51,35 @@ __device__ __forceinline__ float dpp_move(float x) {
 }
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
+template <int CTRL>
+__device__ __forceinline__ double dpp_move(double x) {
+    const uint64_t u = __double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_mov_dpp(int(uint32_t(u)), CTRL, 0xF, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_mov_dpp(int(uint32_t(u >> 32)), CTRL, 0xF, 0xF, false);
+    return __longlong_as_double((uint64_t(hi) << 32) | lo);
+}
+
 // The sum over the wave in every lane, in a fixed order: quads, half rows, rows, then across rows.
-__device__ __forceinline__ float sum64(float x) {
+__device__ __forceinline__ double sum64(double x) {
     x += dpp_move<0xB1>(x);
     x += dpp_move<0x4E>(x);
     x += dpp_move<0x141>(x);
     x += dpp_move<0x140>(x);
-    u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    uint64_t u = __double_as_longlong(x);
+    u32x2 lo = __builtin_amdgcn_permlane16_swap(uint32_t(u), uint32_t(u), false, false);
+    u32x2 hi = __builtin_amdgcn_permlane16_swap(uint32_t(u >> 32), uint32_t(u >> 32), false, false);
+    x = __longlong_as_double((uint64_t(hi[0]) << 32) | lo[0]) + __longlong_as_double((uint64_t(hi[1]) << 32) | lo[1]);
+    u = __double_as_longlong(x);
+    lo = __builtin_amdgcn_permlane32_swap(uint32_t(u), uint32_t(u), false, false);
+    hi = __builtin_amdgcn_permlane32_swap(uint32_t(u >> 32), uint32_t(u >> 32), false, false);
+    return __longlong_as_double((uint64_t(hi[0]) << 32) | lo[0]) + __longlong_as_double((uint64_t(hi[1]) << 32) | lo[1]);
+}
+
+// x^(-1/2): the fp32 instruction and one Newton step in fp64 (1e-14), or in fp64 altogether outside fp32's range.
+__device__ __forceinline__ double inverse_root(double x) {
+    if (!(x > 1e-30 && x < 1e30)) return 1.0 / __builtin_sqrt(x);
+    const double y = double(__builtin_amdgcn_rsqf(float(x)));
+    return y * (1.5 - 0.5 * x * y * y);
 }
 
 __device__ __forceinline__ float bf16_up(uint32_t bits) { return __uint_as_float(bits << 16); }
@@ -108,24 +128,29 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const WriteP
     if (p.gamma) {
         uint4 g{0, 0, 0, 0};
         if (has) g = *reinterpret_cast<const uint4*>(p.gamma + c);
-        float ss = 0.f;
+        // in fp64: an entry that fp32 moves over a rounding boundary of bf16 may move a whole step of its 8-bit code
+        double ss = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss += v[i] * v[i];
-        const float inv = 1.0f / __builtin_sqrtf(sum64(ss) / float(p.kv) + p.eps);
+        for (int i = 0; i < 8; ++i) ss += double(v[i]) * double(v[i]);
+        const double inv = inverse_root(sum64(ss) / double(p.kv) + double(p.eps));
         const uint32_t w[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[2 * i] = v[2 * i] * inv * bf16_up(w[i] & 0xFFFFu);
-            v[2 * i + 1] = v[2 * i + 1] * inv * bf16_up(w[i] >> 16);
+            v[2 * i] = float(double(v[2 * i]) * inv * double(bf16_up(w[i] & 0xFFFFu)));
+            v[2 * i + 1] = float(double(v[2 * i + 1]) * inv * double(bf16_up(w[i] >> 16)));
         }
     }
     if (slot < 0 || slot >= p.rows) return;        // (checked here, so that the row is loaded beside its slot)
     uint8_t* const row = p.data + slot * p.ld;
     const int64_t rope_at = E4M3 ? p.kv + kScaleBytes : 2 * p.kv;
     if (pair) {
-        float sn = 0.f, cs = 1.f;
-        if (p.positions) rope_sincos(p.freq_step, pos, lane, &sn, &cs);
-        const float r0 = p.positions ? k0 * cs - k1 * sn : k0, r1 = p.positions ? k0 * sn + k1 * cs : k1;
+        float r0 = k0, r1 = k1;
+        if (p.positions) {
+            double sn, cs;
+            rope_sincos64(p.freq_step, pos, lane, &sn, &cs);
+            r0 = float(double(k0) * cs - double(k1) * sn);
+            r1 = float(double(k0) * sn + double(k1) * cs);
+        }
         *reinterpret_cast<uint32_t*>(row + rope_at + 4 * lane) = uint32_t(to_bf16_bits(r0)) | (uint32_t(to_bf16_bits(r1)) << 16);
     }
     uint32_t h[8];

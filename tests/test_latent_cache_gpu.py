@@ -191,3 +191,26 @@ def test_other_stream_and_graph_replays():
         replayed = out.clone()
         step()
         assert torch.equal(replayed, out), i
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_entries_are_rounded_once(fp8):
+    # RMSNorm and RoPE are in fp64 (their angles below 2^17 to 2^-35) up to a float that is rounded to bf16: it ends on the wrong side
+    # of one of bf16's boundaries where the value is within half a float step of it, 2^-17 of the values; four times that are
+    # allowed (in fp32, with errors around 2^-23, twice as many would be wrong)
+    kv, rope, eps, theta, tokens = 512, 64, 1e-6, 10000.0, 2048
+    rng = np.random.default_rng(31)
+    src = rng.standard_normal((tokens, kv + rope)).astype(np.float32)
+    gamma = ob.bf16_round(1 + 0.1 * rng.standard_normal(kv))
+    pos = rng.integers(0, 2 ** 17, tokens)
+    cache = pool(tokens, kv, rope, fp8)
+    slots = torch.arange(tokens, device="cuda")
+    nmm.nmm_latent_cache_write(torch.from_numpy(src).cuda(), slots, cache, kv_lora=kv, rope=rope, gamma=bf16(gamma).cuda(), eps=eps,
+                               positions=torch.from_numpy(pos).cuda(), theta=theta)
+    out = torch.zeros((tokens, kv + rope), dtype=torch.bfloat16, device="cuda")
+    nmm.nmm_latent_cache_read(cache, slots, out, kv_lora=kv, rope=rope)
+    entry = ob.bf16_round(ob.cache_entry(src, kv, rope, gamma, eps, pos, theta))
+    if fp8:
+        entry = ob.dequantise_rows(ob.quantise_rows(entry, kv), kv, rope)
+    wrong = (out.double().cpu().numpy() != entry).mean()
+    assert wrong <= 2.0 ** -15, wrong
