@@ -23,7 +23,7 @@
 //
 // What bounds it.  One row of x, K 16384, N 7168, groups of 128: 16.2 us for 60.6 MB (14.1 us called in a row), 3.7 TB/s; the
 // same launch without its products 13.9 us, without scales and hand-over either 11.7 (5.2 TB/s), so what widening the codes
-// adds is most of the rest: 9 instructions for 512 codes, and a SIMD holds two waves.  8 rows, K 1536, N 24576, a power of
+// adds is most of the rest: 7 instructions for 512 codes, and a SIMD holds two waves.  8 rows, K 1536, N 24576, a power of
 // two per 32: 9.4 us for 20.9 MB (9.0 without products), six slots a workgroup and so mostly the start.  32 rows of K 16384,
 // N 7168: 26 us, 288 TFLOP/s (18.2 without products and hand-over, 14.6 without x's loads either); the MFMAs of x's sums are
 // 2.5 us of it.
