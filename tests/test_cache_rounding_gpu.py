@@ -1,0 +1,135 @@
+"""nmm_latent_cache_write rounds RMSNorm's and RoPE's results to bf16 once: each entry is the bf16 number nearest to the
+64-bit formula's value, also beside a tie, where a value rounded to a float first lands on the tie and from there goes to even.
+
+What the kernel's fp64 may be off by, and so how near to a boundary between two bf16 numbers an entry has to lie to be left out:
+RMSNorm 2^-40 of the value (16 levels of sums, the inverse root's Newton step from an fp32 one, 1.5 * (2^-22)^2, two products);
+RoPE 2^-33 of |k0| + |k1| at positions below 2^17 (the angle: 2 j 2^-53 of pos * theta^(-2 j / rope), j theta^(-2 j / rope) at most
+1.3 here, and the product's and its reduction's own rounding, 2^-36, twice: the kernel's and the oracle's)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import batch as ob
+
+pytestmark = pytest.mark.gpu
+
+nmm = pytest.importorskip("paper_2609_16009_amd")
+
+FORMATS = pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "e4m3"])
+
+
+def to_boundary(v):
+    """How far each value is from the nearest boundary between two bf16 numbers."""
+    m, e = np.frexp(np.abs(v))
+    return np.abs(np.ldexp(m * 256 - np.floor(m * 256) - 0.5, e - 8))
+
+
+def written(src, kv, rope, fp8, gamma=None, eps=0.0, pos=None, theta=1e4):
+    """The rows' bytes."""
+    n = len(src)
+    width = nmm.nmm_latent_cache_row_bytes(kv, rope, nmm.NMM_CACHE_E4M3 if fp8 else nmm.NMM_CACHE_BF16)
+    cache = torch.zeros((n, width), dtype=torch.uint8, device="cuda")
+    g = None if gamma is None else torch.from_numpy(gamma.astype(np.float32)).to(torch.bfloat16).cuda()
+    p = None if pos is None else torch.from_numpy(np.asarray(pos, dtype=np.int64)).cuda()
+    nmm.nmm_latent_cache_write(torch.from_numpy(src).cuda(), torch.arange(n, device="cuda"),
+                               cache if fp8 else cache.view(torch.bfloat16), kv_lora=kv, rope=rope, gamma=g, eps=float(eps),
+                               positions=p, theta=theta)
+    return cache.cpu().numpy()
+
+
+def rows_of(entry, kv, fp8):
+    return ob.quantise_rows(entry, kv) if fp8 else ob.bf16_encode(entry).view(np.uint8).reshape(len(entry), -1)
+
+
+@FORMATS
+def test_every_entry_is_the_nearest(fp8):
+    kv, rope, theta, tokens = 512, 64, 1e4, 8192
+    eps = np.float32(1e-6)
+    rng = np.random.default_rng(31)
+    src = rng.standard_normal((tokens, kv + rope)).astype(np.float32)
+    gamma = ob.bf16_round(1 + 0.1 * rng.standard_normal(kv))
+    pos = rng.integers(0, 2 ** 17, tokens)
+    exact = ob.cache_entry(src, kv, rope, gamma, float(eps), pos, theta)
+    once = ob.bf16_round(exact)
+    k = np.abs(src[:, kv:].astype(np.float64)).reshape(tokens, -1, 2).sum(-1).repeat(2, 1)
+    off = np.concatenate((2.0 ** -40 * np.abs(exact[:, :kv]), 2.0 ** -33 * k), 1)
+    sure = to_boundary(exact) > off
+    assert (~sure).sum() <= 8                                   # about 2^-24 of the RoPE values
+    by_float = once != ob.bf16_round(exact.astype(np.float32))
+    assert (by_float & sure).sum() >= 20                        # entries that a float on the way would move
+    got, want = written(src, kv, rope, fp8, gamma, eps, pos, theta), rows_of(once, kv, fp8)
+    # bytes that only sure entries decide: two a value, or a block of 32 codes and its scale
+    if fp8:
+        block = sure[:, :kv].reshape(tokens, -1, 32).all(-1)
+        clear = np.concatenate((block.repeat(32, 1), block, np.ones((tokens, 16 - kv // 32), bool), sure[:, kv:].repeat(2, 1)), 1)
+    else:
+        clear = sure.repeat(2, 1)
+    wrong = (got != want) & clear
+    assert not wrong.any(), f"{wrong.sum()} bytes, first {np.argwhere(wrong)[0]}"
+
+
+TIES = [1 + 2.0 ** -8, 1 + 3 * 2.0 ** -8, 1.5 + 2.0 ** -8, 1.5 + 3 * 2.0 ** -8]     # two whose even neighbour is below, two above
+
+
+@FORMATS
+def test_rope_beside_a_tie(fp8):
+    # pair 3 of 4 turns by pos * 10^-12: k0 cos - k1 sin is a tie of bf16 plus or minus 10^-12 to 10^-10
+    kv, rope = 32, 8
+    src, pos = [], []
+    for tie in TIES:
+        for k1 in (-1.0, 1.0):
+            for sign in (-1.0, 1.0):
+                for p in (1, 10, 100):
+                    row = np.zeros(kv + rope)
+                    row[-2:] = sign * tie, k1
+                    src.append(row)
+                    pos.append(p)
+    src = np.array(src, dtype=np.float32)
+    exact = ob.cache_entry(src, kv, rope, None, 0.0, pos, 1e16)
+    beside = to_boundary(exact[:, -2])
+    assert ((beside > 0.9e-12) & (beside < 1.1e-10)).all()
+    want = rows_of(ob.bf16_round(exact), kv, fp8)
+    assert np.array_equal(written(src, kv, rope, fp8, pos=pos, theta=1e16)[:, -4:], want[:, -4:])
+
+
+@FORMATS
+@pytest.mark.parametrize("above", [False, True])
+def test_norm_beside_a_tie(above, fp8):
+    # mean(c^2) + eps = 1 +- 2^-31 in exactly representable terms: the latent c_0, a tie, is normalised to c_0 (1 -+ 2^-32)
+    kv = 32
+    small = [2.0 ** -10, 2.0 ** -11, 2.0 ** -11, 2.0 ** -11, 2.0 ** -12, 2.0 ** -12, 2.0 ** -12, 2.0 ** -13, 2.0 ** -13, 2.0 ** -13]
+    for tie in TIES[:2]:
+        for sign in (-1.0, 1.0):
+            src = np.zeros((1, kv), dtype=np.float32)
+            src[0, 0] = sign * tie
+            eps = 1 - tie * tie / kv
+            if above:                                           # squares of 2^-19 - 2^-26 in all, 32 (2^-24 - 2^-31)
+                src[0, 1:1 + len(small)] = small
+                eps -= 2.0 ** -24
+            else:
+                src[0, 1] = 2.0 ** -13
+            assert float(np.float32(eps)) == eps
+            assert (src.astype(np.float64) ** 2).sum() / kv + eps == (1 - 2.0 ** -31 if above else 1 + 2.0 ** -31)
+            exact = ob.cache_entry(src, kv, 0, np.ones(kv), eps)
+            assert 2.0 ** -33 < to_boundary(exact[0, 0]) < 2.0 ** -31
+            want = rows_of(ob.bf16_round(exact), kv, fp8)
+            assert np.array_equal(written(src, kv, 0, fp8, np.ones(kv), eps), want), (tie, sign)
+
+
+@pytest.mark.parametrize("B,prefix,fp8", [(5, 100, True), (9, 300, False)])
+def test_a_steps_rows_are_the_nearest(B, prefix, fp8):
+    # the rows that a decode batch's step writes, from the products it took: byte for byte
+    from test_batch_step_gpu import EPS, KV, ROPE, THETA, Step
+
+    s = Step(B, B, prefix, 40, fp8)
+    gamma = s.gamma.double().cpu().numpy()
+    for t in range(3):
+        s.next_token(50 * B + t)
+        s.run()
+        torch.cuda.synchronize()
+        src, pos, slots = s.entry.double().cpu().numpy(), s.positions.cpu().numpy(), s.slots.cpu().numpy()
+        exact = ob.cache_entry(src, KV, ROPE, gamma, float(np.float32(EPS)), pos, THETA)
+        k = np.abs(src[:, KV:]).reshape(B, -1, 2).sum(-1).repeat(2, 1)
+        assert (to_boundary(exact) > np.concatenate((2.0 ** -40 * np.abs(exact[:, :KV]), 2.0 ** -33 * k), 1)).all()
+        got = s.cache[torch.from_numpy(slots).cuda()].view(torch.uint8).cpu().numpy()
+        assert np.array_equal(got, rows_of(ob.bf16_round(exact), KV, fp8))
