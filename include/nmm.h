@@ -605,8 +605,14 @@ size_t nmm_mla_query_path_workspace_size(const nmm_mla_query_path* qp);
 size_t nmm_latent_attention_ex_workspace_size(int64_t heads, int64_t seq, int64_t d_qk, int64_t d_v, int64_t splits);
 size_t nmm_mla_decode_step_workspace_size(const nmm_mla_chain* chain, const nmm_latent_attn* attn);
 
-/* Zero a workspace on `stream` with a fill kernel (no memset node, so it is safe to capture). */
+/* Zero a workspace on `stream` with a fill kernel (no memset node, so it is safe to capture).  Where `stream` records a graph
+ * the fill is recorded: the workspace is zeroed when that graph is replayed, not before, and so is good for the calls
+ * recorded behind it in the same graph only. */
 nmm_status nmm_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
+
+/* *id = a number of the capture that `stream` records into, another one for each capture; 0 while it records none (the
+ * null stream never does). */
+nmm_status nmm_stream_capture_id(void* stream, uint64_t* id);
 
 /*
  * The host-side partition the library would launch for these sizes (a pure function: no GPU

@@ -144,6 +144,7 @@ EXPORTS = {
     "nmm_mla_decode_chain_workspace_size": (_sz, [ctypes.POINTER(nmm_mla_chain)]),
     "nmm_latent_attention_workspace_size": (_sz, [_i64, _i64, _i64, _i64]),
     "nmm_workspace_init": (ctypes.c_int, [_p, _sz, _p]),
+    "nmm_stream_capture_id": (ctypes.c_int, [_p, ctypes.POINTER(ctypes.c_uint64)]),
     "nmm_gemv_plan": (ctypes.c_int, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int,
                                      ctypes.POINTER(nmm_plan_info)]),
     "nmm_read_probe": (ctypes.c_int, [_p, _sz, _p, _i64, ctypes.c_int, _p]),
@@ -213,7 +214,11 @@ class Workspace:
     A workspace serves one stream at a time: calls that may overlap need different workspaces.
     A new buffer is zeroed on the stream of the call that needs it (allocated there too, so that
     torch's allocator orders its reuse with that stream); the buffers it replaces are kept until
-    the Workspace is dropped, because kernels enqueued earlier may still be using them."""
+    the Workspace is dropped, because kernels enqueued earlier may still be using them.
+
+    A buffer that a captured call needed is zeroed by that graph, at each of its replays and not before: it
+    serves the rest of that capture, and the next call outside it gets another.  (Call once before capturing,
+    and all graphs share one buffer; graphs that share one must not be replayed at the same time.)"""
 
     def __init__(self, device=None):
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
@@ -229,20 +234,34 @@ class Workspace:
         # what calls launch with, (pointer, bytes), replaced as one and never that of a buffer given up
         self.held = (0, 0) if t is None else (t.data_ptr(), t.numel())
         self._buf = t
+        self._capture = 0           # the capture whose graph zeroes the buffer; 0: it has been zeroed
 
     def get(self, nbytes: int, stream=None) -> tuple[int, int]:
         if nbytes == 0:
             return 0, 0
-        if self.buf is None or self.buf.numel() < nbytes:
-            ts = _torch_stream(stream, self.device)
-            size = max(nbytes, 1 << 20, 2 * self.buf.numel() if self.buf is not None else 0)
+        have = 0 if self.buf is None else self.buf.numel()
+        if have >= nbytes and not self._capture:
+            return self.held
+        ts = _torch_stream(stream, self.device)
+        capture = _capture_id(ts.cuda_stream)
+        if have < nbytes or self._capture != capture:
+            size = max(nbytes, 1 << 20, 2 * have if have < nbytes else have)
             with torch.cuda.stream(ts):
                 buf = torch.empty(size, dtype=torch.uint8, device=self.device)
             _check(lib().nmm_workspace_init(buf.data_ptr(), size, ts.cuda_stream), "nmm_workspace_init")
             if self.buf is not None:
                 self._retired.append(self.buf)
             self.buf = buf
-        return self.held
+            if capture:
+                # (held by no call outside: each asks here first)
+                self._capture, self.held = capture, (0, 0)
+        return self.buf.data_ptr(), self.buf.numel()
+
+
+def _capture_id(handle: int) -> int:
+    n = ctypes.c_uint64()
+    _check(lib().nmm_stream_capture_id(handle, ctypes.byref(n)), "nmm_stream_capture_id")
+    return n.value
 
 
 def _torch_stream(stream, device) -> torch.cuda.Stream:

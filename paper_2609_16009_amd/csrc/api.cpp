@@ -712,6 +712,17 @@ nmm_status nmm_workspace_init(void* workspace, size_t workspace_bytes, void* str
     return launch_zero_fill(workspace, workspace_bytes, stream);
 }
 
+nmm_status nmm_stream_capture_id(void* stream, uint64_t* id) {
+    if (!id) return NMM_ERR_NULL;
+    *id = 0;
+    if (!stream) return NMM_OK;      // (asked about while another stream records, the runtime returns an error)
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    unsigned long long n = 0;
+    if (hipStreamGetCaptureInfo(static_cast<hipStream_t>(stream), &status, &n) != hipSuccess) return NMM_ERR_HIP;
+    if (status != hipStreamCaptureStatusNone) *id = uint64_t(n) + 1;
+    return NMM_OK;
+}
+
 const char* nmm_status_string(nmm_status s) {
     switch (s) {
         case NMM_OK: return "NMM_OK";

@@ -582,3 +582,9 @@ def test_auto_path_per_shape(M, K, N, want):
     # single K-slice; the choice depends on the shape alone
     code = {"gemv": nmm.NMM_PATH_GEMV, "mfma": nmm.NMM_PATH_MFMA}[want]
     assert nmm.nmm_gemv_plan(M, K, N)["path"] == code
+
+
+def test_the_null_stream_records_nothing():
+    n = ctypes.c_uint64(7)
+    assert L.nmm_stream_capture_id(None, None) == nmm.NMM_ERR_NULL
+    assert L.nmm_stream_capture_id(None, ctypes.byref(n)) == nmm.NMM_OK and n.value == 0
