@@ -557,7 +557,8 @@ nmm_status nmm_latent_cache_read(const nmm_latent_cache* cache, int64_t tokens, 
  * rounded to bf16 (nearest, ties to even), the operand of the per-head W_UV that follows.
  *   batch, tokens, heads  >= 0, batch * tokens * heads < 2^24 (0: nothing to do).
  *   q     bf16, q[b * stride_qb + t * stride_qt + h * ldq + d], d < kv_lora + rope: latent part, then RoPE's,
- *         as nmm_mla_query makes it; 16-byte aligned, strides and ldq >= kv_lora + rope multiples of 8.
+ *         as nmm_mla_query makes it; 16-byte aligned, ldq >= kv_lora + rope, ldq and the strides multiples of 8 (a
+ *         stride may be 0: one query for all).
  *   cache the pool in either format.  Rows past a length are never read; a row below it that holds NaN or
  *         infinity spoils every token of its sequence, whether the token sees it or not.
  *   page_size     a power of two up to 65536.
@@ -567,7 +568,7 @@ nmm_status nmm_latent_cache_read(const nmm_latent_cache* cache, int64_t tokens, 
  *   max_len       what the launch is planned for: lens[b] above it counts as max_len, below 0 as 0.
  *                 The plan does not look at lens, so a captured call follows them as they change.
  *   out   bf16, out[b * stride_ob + t * stride_ot + h * ldo + c], c < kv_lora; 8-byte aligned, strides
- *         and ldo >= kv_lora multiples of 4.
+ *         and ldo >= kv_lora multiples of 4 (the stride of an axis of one is not looked at further); no row may lie over another.
  * Positions on a page outside the pool are left out; a row that sees no position gives zeros.  Results are
  * deterministic.  out may overlap nothing that the call reads.  Workspace: nmm_latent_attention_batch_workspace_size.
  */

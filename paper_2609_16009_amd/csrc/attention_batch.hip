@@ -1279,6 +1279,8 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
     if (a.max_len > 0 && (a.ld_pages < cdiv(a.max_len, a.page_size) || a.ld_pages >= kLim)) return NMM_ERR_SHAPE;
     const int64_t rows = a.batch * a.tokens * a.heads;
     if (rows == 0) return NMM_OK;
+    // (rows of out over each other would be written by several workgroups)
+    if ((a.batch > 1 && a.stride_ob < a.cache.kv_lora) || (a.tokens > 1 && a.stride_ot < a.cache.kv_lora)) return NMM_ERR_SHAPE;
     if (!a.q || !a.out) return NMM_ERR_NULL;
     if (a.prefix_len > 0 && !a.prefix_pages) return NMM_ERR_NULL;
     if (a.max_len > 0 && (!a.pages || !a.lens)) return NMM_ERR_NULL;

@@ -242,3 +242,15 @@ def test_packed_arguments_match_the_structs():
                  ld_pages=18, lens=1 << 46, max_len=19, scale=0.25, out=1 << 47, stride_ob=20, stride_ot=21, ldo=22)
     assert nmm._ATTN_BATCH.pack(2, 3, 5, 1 << 43, 11, 12, 13, *pool, 16, 1 << 44, 17, 1 << 45, 18, 1 << 46, 19, 0.25, 1 << 47, 20,
                                 21, 22) == bytes(a)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(stride_ob=508), nmm.NMM_ERR_SHAPE), (dict(stride_ob=0), nmm.NMM_ERR_SHAPE),
+    (dict(tokens=2, stride_ot=508, stride_ob=32 * 512), nmm.NMM_ERR_SHAPE), (dict(tokens=2, stride_ot=0), nmm.NMM_ERR_SHAPE),
+    # an axis of one has no rows to lie over each other, and q may be one row for all
+    (dict(batch=1, stride_ob=0), nmm.NMM_ERR_WORKSPACE), (dict(stride_ot=0), nmm.NMM_ERR_WORKSPACE),
+    (dict(heads=8, tokens=2, stride_ot=512, ldo=1024), nmm.NMM_ERR_WORKSPACE),
+    (dict(stride_qb=0), nmm.NMM_ERR_WORKSPACE), (dict(tokens=2, stride_ot=16 * 512, stride_ob=32 * 512), nmm.NMM_ERR_WORKSPACE),
+])
+def test_batched_attention_refuses_outputs_over_each_other(kw, status):
+    assert L.nmm_latent_attention_batch(ctypes.byref(batch_of(**kw)), None, 0, None) == status
