@@ -8,7 +8,7 @@
 //
 //  * Writing: a wave owns a token, a lane eight latents, four lanes a scale block, whose maximum meets by
 //    two DPP exchanges; the sum of squares is a butterfly over the wave, and RMSNorm and RoPE are in fp64 up to
-//    the entry's one rounding.  Lanes below rope / 2 take a RoPE
+//    the entry's rounding.  Lanes below rope / 2 take a RoPE
 //    pair each.  Nothing leaves the wave, so tokens need no barrier and any number of them fills the chip.
 //  * Reading: a thread owns 16 bytes of an output row, so stores are whole lines and the loads of a row
 //    are contiguous too.
@@ -128,8 +128,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const WriteP
     if (p.gamma) {
         uint4 g{0, 0, 0, 0};
         if (has) g = *reinterpret_cast<const uint4*>(p.gamma + c);
-        // in fp64, rounded to bf16 once: an entry that falls on the other side of a boundary between two bf16 numbers may move a
-        // whole step of its 8-bit code
+        // in fp64: an entry that fp32 moves over a rounding boundary of bf16 may move a whole step of its 8-bit code
         double ss = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += double(v[i]) * double(v[i]);
@@ -137,8 +136,8 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const WriteP
         const uint32_t w[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[2 * i] = to_odd_float(double(v[2 * i]) * inv * double(bf16_up(w[i] & 0xFFFFu)));
-            v[2 * i + 1] = to_odd_float(double(v[2 * i + 1]) * inv * double(bf16_up(w[i] >> 16)));
+            v[2 * i] = float(double(v[2 * i]) * inv * double(bf16_up(w[i] & 0xFFFFu)));
+            v[2 * i + 1] = float(double(v[2 * i + 1]) * inv * double(bf16_up(w[i] >> 16)));
         }
     }
     if (slot < 0 || slot >= p.rows) return;        // (checked here, so that the row is loaded beside its slot)
@@ -149,8 +148,8 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const WriteP
         if (p.positions) {
             double sn, cs;
             rope_sincos64(p.freq_step, pos, lane, &sn, &cs);
-            r0 = to_odd_float(double(k0) * cs - double(k1) * sn);
-            r1 = to_odd_float(double(k0) * sn + double(k1) * cs);
+            r0 = float(double(k0) * cs - double(k1) * sn);
+            r1 = float(double(k0) * sn + double(k1) * cs);
         }
         *reinterpret_cast<uint32_t*>(row + rope_at + 4 * lane) = uint32_t(to_bf16_bits(r0)) | (uint32_t(to_bf16_bits(r1)) << 16);
     }
