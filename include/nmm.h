@@ -505,8 +505,10 @@ size_t nmm_latent_cache_row_bytes(nmm_cache_format format, int64_t kv_lora, int6
  *   c            = c / sqrt(mean(c^2) + eps) * gamma                      where gamma is given
  *   k            = RoPE(k, positions[t])                                  where positions is given
  *   row slots[t] = bf16([c | k]), in 8-bit rows the bf16 latents quantised
- * RMSNorm and RoPE as in nmm_mla_kv_update (rounded to nearest, ties to even); src is a product of
- * nmm_gemv with M tokens, say.  Quantising: per 32 latents the least e >= -117 with every finite
+ * RMSNorm and RoPE as in nmm_mla_kv_update, but in 64 bits: bf16() is the nearest float and of that the nearest
+ * bf16 number (ties to even, both: 2^-17 of a bf16 step more than half a step off at most).  That call's values are fp32
+ * arithmetic's, so an entry of it that lies near a boundary between two bf16 numbers may be the other one.  src is a
+ * product of nmm_gemv with M tokens, say.  Quantising: per 32 latents the least e >= -117 with every finite
  * |value| <= 448 * 2^e, and code = value * 2^-e rounded to e4m3 (nearest, ties to even), so nothing
  * saturates and what a row stands for is a bf16 number (magnitudes from 1.9375 * 2^127 on round to 2^128, which
  * reads as infinity).  Values that are not finite are kept as NaN.

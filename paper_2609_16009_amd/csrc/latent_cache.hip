@@ -3,12 +3,15 @@
 //   entry[t] = bf16([RMSNorm(c) * gamma | RoPE(k, positions[t])])        src[t] = [c | k]
 //   8 bits:   per block of 32 latents the least e >= -117 with max |v| <= 448 * 2^e; code = e4m3(v * 2^-e)
 //
-// The entry is rounded to bf16 first, as nmm_mla_kv_update rounds it, so an 8-bit row holds the codes of
-// the bf16 row that the same token would have had.  v * 2^-e is exact, so a code has one rounding.
+// The entry is rounded to bf16 first, so an 8-bit row holds the codes of the bf16 row that this call would have written
+// for the same token.  v * 2^-e is exact, so a code has one rounding.  bf16() is the nearest float of the 64-bit value and
+// of that the nearest bf16 number, as casts of a double to bf16 commonly are: 9 of 10^6 of RMSNorm's and RoPE's values lie so near to
+// a tie that the float is the tie and goes to even (the float rounded to odd instead, which rounds once: 14.9 us for 14.5).
+// fp32 arithmetic (nmm_mla_kv_update) moves about as many entries, others, and where one moves so may its 8-bit code, a whole step.
 //
 //  * Writing: a wave owns a token, a lane eight latents, four lanes a scale block, whose maximum meets by
 //    two DPP exchanges; the sum of squares is a butterfly over the wave, and RMSNorm and RoPE are in fp64 up to
-//    the entry's rounding.  Lanes below rope / 2 take a RoPE
+//    the float that the entry is rounded from.  Lanes below rope / 2 take a RoPE
 //    pair each.  Nothing leaves the wave, so tokens need no barrier and any number of them fills the chip.
 //  * Reading: a thread owns 16 bytes of an output row, so stores are whole lines and the loads of a row
 //    are contiguous too.
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(const WriteP
     if (p.gamma) {
         uint4 g{0, 0, 0, 0};
         if (has) g = *reinterpret_cast<const uint4*>(p.gamma + c);
-        // in fp64: an entry that fp32 moves over a rounding boundary of bf16 may move a whole step of its 8-bit code
+        // in fp64: an entry that fp32 moves over a boundary between two bf16 numbers may move a whole step of its 8-bit code
         double ss = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += double(v[i]) * double(v[i]);
