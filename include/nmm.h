@@ -452,7 +452,8 @@ nmm_status nmm_mla_decode_step(const nmm_mla_chain* chain, const nmm_latent_attn
  *   NMM_W4_MX   c = the e2m1 value of the code (bit 3 the sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6); s = 2^(b - 127) of a
  *               byte b (255: NaN), group = 32, no zeros
  * Codes are widened exactly, products summed in fp32, and a group's scale is applied to its fp32 sum: no
- * weight is rounded.  Any M (in blocks of up to 32 rows, each reading the weight once).  A value of x, a scale or a
+ * weight is rounded.  The zero point is taken off that sum, sum x code - z sum x, so the error is a rounding of
+ * sum |x| s (code + z): a group whose codes all are its zero point may leave one where the formula has 0.  Any M (in blocks of up to 32 rows, each reading the weight once).  A value of x, a scale or a
  * zero point affects its row of y only (of W: its column); a row of x that holds an infinity or NaN gives values that
  * are not finite, NaN where the formula would have an infinity (NMM_W4_INT).
  *   dt, x, ldx   as for nmm_gemv_nt.
@@ -479,12 +480,13 @@ size_t nmm_gemv_w4_workspace_size(int64_t M, int64_t K, int64_t N, int64_t group
  *   NMM_CACHE_BF16  row = kv_lora latents and rope values, bf16: the rows nmm_mla_kv_update writes
  *   NMM_CACHE_E4M3  row = kv_lora e4m3 codes | 16 scale bytes | rope values in bf16.  Latents
  *                   32 b .. 32 b + 31 share scale byte b: code c stands for e4m3(c) * 2^(byte - 127).
- *                   Scale bytes past kv_lora / 32 are written as 127 and not read.
+ *                   Scale bytes past kv_lora / 32 are written as 127 and not read.  Bytes 3 to 254 are exact (the
+ *                   library writes 10 to 247); below 3 some of bf16's subnormals are lost, and 255 makes its block NaN.
  *                   656 bytes at kv_lora 512, rope 64, against 1152.
  *
  *   data     16-byte aligned; row r starts at data + r * ld, ld in BYTES, a multiple of 16 and at least
  *            nmm_latent_cache_row_bytes(format, kv_lora, rope).  Offsets are 64-bit: a pool may be of any size.
- *   rows     rows of the pool, < 2^31.
+ *   rows     rows of the pool, < 2^31, as is ld.
  *   kv_lora  a multiple of 32 in [32, 512];   rope  a multiple of 8 in [0, 64].
  */
 typedef enum { NMM_CACHE_BF16 = 1, NMM_CACHE_E4M3 = 2 } nmm_cache_format;
@@ -518,6 +520,7 @@ size_t nmm_latent_cache_row_bytes(nmm_cache_format format, int64_t kv_lora, int6
  *   slots        [tokens], positions [tokens] or NULL: int64 on the device; positions in [0, 2^31).
  *   gamma        [kv_lora] bf16, 16-byte aligned, or NULL.
  *   eps          finite, >= 0 (with gamma).   rope_theta  finite, > 0 (with positions).
+ *   tokens       at most 2^26 - 4.
  * Needs no workspace.
  */
 typedef enum { NMM_SRC_F32 = 0, NMM_SRC_BF16 = 1 } nmm_src_type;
@@ -539,7 +542,8 @@ nmm_status nmm_latent_cache_write(const nmm_latent_cache* cache, const nmm_cache
 /*
  * nmm_latent_cache_read -- out[t, :kv_lora + rope] = what row slots[t] stands for, bf16 (exact), for
  * t < tokens.  A slot outside the pool leaves its row of out as it was; a slot may be named any
- * number of times.  out 16-byte aligned, ldo >= kv_lora + rope a multiple of 8 (elements).
+ * number of times.  out 16-byte aligned, ldo >= kv_lora + rope a multiple of 8 (elements).  tokens * (kv_lora + rope)
+ * below 2^35 - 2048.
  */
 nmm_status nmm_latent_cache_read(const nmm_latent_cache* cache, int64_t tokens, const int64_t* slots, void* out,
                                  int64_t ldo, void* stream);
@@ -557,18 +561,20 @@ nmm_status nmm_latent_cache_read(const nmm_latent_cache* cache, int64_t tokens, 
  *
  * Scores, softmax and sums are fp32; probabilities are rounded to bf16 for the product with v and out is
  * rounded to bf16 (nearest, ties to even), the operand of the per-head W_UV that follows.
- *   batch, tokens, heads  >= 0, batch * tokens * heads < 2^24 (0: nothing to do).
+ *   batch, tokens, heads  >= 0, batch < 2^20, tokens and heads < 2^16, batch * tokens * heads < 2^24 (0: nothing to do).
+ *         Strides are below 2^40, ldq, ldo and ld_pages below 2^31.
  *   q     bf16, q[b * stride_qb + t * stride_qt + h * ldq + d], d < kv_lora + rope: latent part, then RoPE's,
  *         as nmm_mla_query makes it; 16-byte aligned, ldq >= kv_lora + rope, ldq and the strides multiples of 8 (a
  *         stride may be 0: one query for all).
  *   cache the pool in either format.  Rows past a length are never read; a row below it that holds NaN or
  *         infinity spoils every token of its sequence, whether the token sees it or not.
- *   page_size     a power of two up to 65536.
+ *   page_size     a power of two up to 65536.   prefix_len, max_len  below 2^30.
  *   prefix_pages  int32 [ceil(prefix_len / page_size)] on the device (unused where prefix_len is 0).
  *   pages, lens   int32 [batch, ld_pages] and [batch] on the device, ld_pages >= ceil(max_len / page_size);
- *                 unused where max_len is 0.  Entries past a sequence's length are not read.
+ *                 unused where max_len is 0.  Entries past a sequence's length are not used.
  *   max_len       what the launch is planned for: lens[b] above it counts as max_len, below 0 as 0.
- *                 The plan does not look at lens, so a captured call follows them as they change.
+ *                 The plan does not look at lens, so a captured call follows them as they change.  It cuts max_len
+ *                 into spans, a workgroup each: where no sequence comes near it, few of them have work to do.
  *   out   bf16, out[b * stride_ob + t * stride_ot + h * ldo + c], c < kv_lora; 8-byte aligned, strides
  *         and ldo >= kv_lora multiples of 4 (the stride of an axis of one is not looked at further); no row may lie over another.
  * Positions on a page outside the pool are left out; a row that sees no position gives zeros.  Results are

@@ -12,21 +12,23 @@
 // A workgroup of 4 waves takes a tile over a span, chunk by chunk:
 //  * Staging.  A chunk's rows lie in LDS as bf16, [9 column blocks][positions][8 pieces of 16 bytes]: the latents'
 //    eight blocks of 64 columns, then RoPE's (columns that the cache lacks are zeros).  Piece c of row r sits in
-//    slot c ^ f(r), which keeps the key reads (8 rows, one column) and the transposed value reads (4 rows, 2 pieces)
-//    free of bank conflicts.  bf16 rows come by LDS-direct loads of 8 rows x 128 bytes; 8-bit rows come into
+//    slot c ^ f(r), which spreads the key reads (8 rows, one column) and the transposed value reads (4 rows, 2 pieces)
+//    over all banks.  (By the counters 21 to 32 % of the cycles that LDS is busy are conflicts all the same; they have not been
+//    traced to their accesses.)  bf16 rows come by LDS-direct loads of 8 rows x 128 bytes; 8-bit rows come into
 //    registers a chunk ahead and are widened on their way to LDS (exact: a power of two per 32 values).  A wave's
 //    lanes look up one position's page each, a chunk before its rows are loaded; rows that do not exist (past the end,
 //    on a page outside the pool) read zeros and are masked.
 //  * S^T = K Q^T, Q in registers as fragments; P = 2^(s - reference), the reference moved only when a chunk
 //    exceeds it by 2^8; O^T = V^T P^T, a quarter of the columns a wave.
-//    Scores, sums and outputs are fp32; P is rounded to bf16 for the matrix cores (2^-9 relative, where the output
-//    itself is rounded to bf16) and summed before its rounding.
+//    Scores, sums and outputs are fp32; P is rounded to bf16 for the matrix cores (2^-8 of each probability at most, as much as
+//    the output's own rounding to bf16: against 64 bits 1.8e-3 to 2.0e-3 in all, 1.7e-3 with fp32 probabilities) and summed before
+//    its rounding.
 // Tiles of 16 and 32 rows (narrow_block) take chunks of 64 positions, 16 a wave; tiles of 64 (wide_block) chunks of 32 in
 // a software pipeline.
 //
-// What bounds it.  64 sequences of 16 heads over 2049 .. 4097 own positions, 8-bit rows: 46 us for 130 MB (26 us at
+// What bounds it.  64 sequences of 16 heads over 2049 .. 4097 own positions, 8-bit rows: 45 us for 130 MB (26 us at
 // the rate of a large copy), 38 where all rows come from L2: two workgroups a CU spend more on widening the rows into LDS than on
-// the products, each with one chunk's loads in flight.  16 sequences of 128 heads behind 8192 positions, bf16 rows: 66 us for
+// the products, each with one chunk's loads in flight.  16 sequences of 128 heads behind 8192 positions, bf16 rows: 67 us for
 // 40 GFLOP (33 us at the rate
 // of a large matrix product); 64 positions take 5300 cycles (6050 with 8-bit rows) where their MFMAs alone would take 2180: every
 // key and value fragment is read from LDS by each of the four waves' quarters, and Q's start (7 us) and the fp32

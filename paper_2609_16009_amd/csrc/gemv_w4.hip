@@ -6,7 +6,7 @@
 //  * A workgroup owns 16 rows of the weight per wave (4 to 8 waves) and a slice of K, which its waves stream through a ring
 //    in LDS, four slots of 256 k (128 bytes, one cache line, of each row).
 //    Loads go straight to LDS, 8 rows x 128 bytes each; chunks of 16 bytes are permuted within a row so that
-//    fragment reads hit every bank once.  The slice's scales and zero points are staged once, beside the first slots.
+//    a read of the weight's fragments hits every bank once, and one of 16 rows of x too (8 rows of x lie on half of the banks).  The slice's scales and zero points are staged once, beside the first slots.
 //  * Up to 8 rows of x (w4_few_kernel) x's part of the slice is staged once too and each wave goes through its rows on its own,
 //    with no barrier in the loop.  More rows (w4_rows_kernel, 16 or 32 at a time) lie in the ring beside the weight, a barrier a
 //    slot; a wave there multiplies 32 rows of the weight and half of a slot.
@@ -21,12 +21,14 @@
 //    and share its scale.
 //  * K is split over workgroups to fill the chip; the last to finish adds the slices in slice order (handoff.h).
 //
-// What bounds it.  One row of x, K 16384, N 7168, groups of 128: 16.2 us for 60.6 MB (14.1 us called in a row), 3.7 TB/s; the
-// same launch without its products 13.9 us, without scales and hand-over either 11.7 (5.2 TB/s), so what widening the codes
-// adds is most of the rest: 7 instructions for 512 codes, and a SIMD holds two waves.  8 rows, K 1536, N 24576, a power of
-// two per 32: 9.4 us for 20.9 MB (9.0 without products), six slots a workgroup and so mostly the start.  32 rows of K 16384,
+// What bounds it (in a replayed graph; with weights that rotate over 1 GiB, so that none is left in a cache, each within 0.6 us of
+// that).  One row of x, K 16384, N 7168, groups of 128: 16.0 us for 60.6 MB, 3.8 TB/s; the same launch without its products 13.9 us,
+// without scales and hand-over either 11.7 (5.2 TB/s): half of what is above the loads is widening the codes (7 instructions for
+// 512 codes, and a SIMD holds two waves) with their products, half scales and hand-over.  8 rows, K 1536, N 24576, a power of
+// two per 32: 9.2 us for 20.9 MB (9.0 without products), six slots a workgroup and so mostly the start.  32 rows of K 16384,
 // N 7168: 26 us, 288 TFLOP/s (18.2 without products and hand-over, 14.6 without x's loads either); the MFMAs of x's sums are
-// 2.5 us of it.
+// 2.5 us of it.  Of the cycles that LDS is busy 22, 46 and 22 % are bank conflicts by the counters: x's 8 rows account for some
+// of the 46, the others have not been traced to their accesses.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

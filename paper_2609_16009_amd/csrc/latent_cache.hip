@@ -16,8 +16,9 @@
 //  * Reading: a thread owns 16 bytes of an output row, so stores are whole lines and the loads of a row
 //    are contiguous too.
 // Bound by bytes for many rows and by one chain of round trips for few: 40001 8-bit rows of 656 bytes read into bf16
-// ones in 16.1 us (72 MB, 4.5 TB/s, against 5.1 of a large copy); 8192 rows written from fp32 and read back 14.9 us (two
-// launches, 39 MB), of which RMSNorm and RoPE in fp64 are 1.8; 64 rows 5.8 us, 2.9 a launch.
+// ones in 16.4 us (72 MB, 4.4 TB/s, against 5.1 of a large copy) with 216 MB in turn, which the last-level cache holds, and 23.4 with
+// 1 GiB; 8192 rows written from fp32 and read back 14.6 us (two launches, 39 MB; 17.6 with 1 GiB in turn), of which RMSNorm
+// and RoPE in fp64 are 0.9; 64 rows 5.4 us for both launches.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
