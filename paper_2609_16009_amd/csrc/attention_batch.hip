@@ -997,6 +997,9 @@ __device__ __forceinline__ void wide_block(const BatchParams& p, const Item it, 
         step(std::true_type{}, n - 1, last == 0 ? b0 : last == 1 ? b1 : last == 2 ? b2 : b3, nullptr, nullptr, nullptr);
     }
 
+    // (the loads of the chunks behind the last, and of a span without positions: none may write LDS after the workgroup has left)
+    if constexpr (!E4M3) __builtin_amdgcn_s_waitcnt(0);
+
     // ---- the rows' sums: a wave's four lanes of a row, then the two position groups
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
