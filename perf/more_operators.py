@@ -19,7 +19,6 @@ own = False
 
 HIDDEN, INNER = 7168, 2048              # a layer's width and an expert's
 MAX_WEIGHT = 16384 * 7168               # elements of the largest dense weight
-MAX_EXPERTS = 64 * HIDDEN * INNER       # elements of a third of the largest experts' weights
 MAX_PRODUCTS = 2048 * HIDDEN * INNER    # (pairs of the largest call) x a third of an expert's elements
 ACTS = ("none", "relu", "silu", "gelu", "gelu_tanh")
 
