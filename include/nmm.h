@@ -601,6 +601,135 @@ nmm_status nmm_latent_attention_batch(const nmm_latent_attn_batch* attn, void* w
                                       void* stream);
 size_t nmm_latent_attention_batch_workspace_size(const nmm_latent_attn_batch* attn);
 
+/*
+ * nmm_gemv_nt_act -- nmm_gemv_nt's product with what follows it in a feed-forward layer in the same launch:
+ *     z[m,r] = sum_k x[m,k] Wt[r,k] + bias[r]                 r < N, or r < 2 N where gated
+ *     v[m,n] = act(z[m,n])                                    or, gated, act(z[m,n]) * z[m, N + n]
+ *     y[m,n] = v[m,n] + residual[m,n]
+ * Gated weights hold the gate's N rows, then the N rows of what it is multiplied with.  Products and everything
+ * after them are fp32, y is rounded once (nearest, ties to even).  Any M (blocks of up to 128 rows, each reading Wt once).
+ *   act          none; relu: max(z, 0), NaN kept; silu: z / (1 + e^-z); gelu: z / 2 (1 + erf(z / sqrt 2)); gelu_tanh:
+ *                z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
+ *   x, ldx, Wt, ldwt   as for nmm_gemv_nt; the extent of Wt counts its N or 2 N rows.
+ *   bias         [N] or [2 N] of type dt, 2-byte aligned, or NULL.
+ *   residual     [M, ldr] of type dt, 2-byte aligned, ldr >= N, or NULL.  It may be y (the same address and leading dimension);
+ *                otherwise y and y_f32 may overlap nothing that the call reads (NMM_ERR_ARG for the residual, x and each other).
+ *   y, ldy       of type dt, 2-byte aligned, ldy >= N;   y_f32, ldyf   the same values before their rounding, 4-byte
+ *                aligned.  Either may be NULL, not both.
+ * K == 0 leaves act(bias) and the residual.  Workspace: nmm_gemv_nt_act_workspace_size (0 where K is not split).
+ */
+typedef enum { NMM_ACT_NONE = 0, NMM_ACT_RELU = 1, NMM_ACT_SILU = 2, NMM_ACT_GELU = 3, NMM_ACT_GELU_TANH = 4 } nmm_act;
+
+typedef struct {
+    int64_t M, K, N;
+    nmm_dtype dt;
+    nmm_act act;
+    int gated;                 /* 0 or 1 */
+    const void* x;
+    int64_t ldx;
+    const void* Wt;
+    int64_t ldwt;
+    const void* bias;
+    const void* residual;
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+    float* y_f32;
+    int64_t ldyf;
+} nmm_nt_act;
+
+nmm_status nmm_gemv_nt_act(const nmm_nt_act* product, void* workspace, size_t workspace_bytes, void* stream);
+size_t nmm_gemv_nt_act_workspace_size(const nmm_nt_act* product);
+
+/*
+ * nmm_moe_route -- the experts of every token, and the order in which nmm_moe_experts takes the (token, expert) pairs:
+ *     s[t,e] = 1 / (1 + e^-logits[t,e])  or softmax_e(logits[t])          c[t,e] = s[t,e] + bias[e]
+ *     a group of experts / groups consecutive experts counts its best c (group_top 1) or the sum of its best two (2);
+ *     the top_groups groups that count most stay;
+ *     chosen[t, 0 .. top_k - 1] = the experts of those groups with the largest c, descending
+ *     weights[t,i] = scale * s[t, chosen[t,i]]    (renormalize: / sum_i s[t, chosen[t,i]])
+ * Ties go to the lowest index.  Scores are computed and compared in 64 bits, weights rounded once to fp32.  A c that is
+ * NaN counts as minus infinity (and its s as NaN where it becomes a weight), a sum of zero gives NaN as the formula does.
+ *   logits       [tokens, ld_logits] fp32 or bf16 (nmm_gemv_nt's product, say), aligned to its type.
+ *   bias         [experts] fp32, or NULL.
+ *   mask         [tokens] bytes, or NULL: a token whose byte is 0 (padding) gets chosen = -1, weights = 0 and no pairs.
+ *   experts      1 .. 1024;   top_k   1 .. 32, at most the experts of top_groups groups;
+ *   groups       1 .. 64, a divisor of experts;   top_groups   1 .. groups;   group_top 1 or 2.   scale finite.
+ *   chosen       int32 [tokens, top_k];   weights   fp32 [tokens, top_k].
+ *   offsets      int32 [experts + 1];   pairs   int32 [tokens * top_k]: pairs[offsets[e] .. offsets[e + 1]) are the pairs
+ *                t * top_k + i with chosen[t,i] = e, ascending; those behind offsets[experts] are left as they were.
+ *   tokens       tokens * top_k < 2^26 (0: offsets are zeroed).
+ * Deterministic.  Workspace: nmm_moe_route_workspace_size.
+ */
+typedef enum { NMM_SCORE_SOFTMAX = 1, NMM_SCORE_SIGMOID = 2 } nmm_score;
+
+typedef struct {
+    int64_t tokens, experts, top_k;
+    const void* logits;
+    nmm_src_type logits_type;
+    int64_t ld_logits;
+    nmm_score score;
+    const float* bias;
+    int64_t groups, top_groups, group_top;
+    int renormalize;           /* 0 or 1 */
+    float scale;
+    const uint8_t* mask;
+    int32_t* chosen;
+    float* weights;
+    int32_t* offsets;
+    int32_t* pairs;
+} nmm_moe_router;
+
+nmm_status nmm_moe_route(const nmm_moe_router* router, void* workspace, size_t workspace_bytes, void* stream);
+size_t nmm_moe_route_workspace_size(const nmm_moe_router* router);
+
+/*
+ * nmm_moe_experts -- the products of the chosen experts and their weighted sum, for the experts first .. first + local - 1
+ * that this GPU holds (first 0 and local = experts: all of them).  With e = chosen[t,i] - first:
+ *     h[t,i]  = dt(act(x[t] . W1[e, :inner]^T) * (x[t] . W1[e, inner:]^T))
+ *     y[t]    = dt(residual[t] + sum_i weights[t,i] (h[t,i] . W2[e]^T))            over the i whose expert is here
+ * Sums are fp32; h is rounded to dt, the operand of the second product, and y once (nearest, ties to even).  The i of a token
+ * are added in order; a token with none gets its residual, or zeros.  The weights of an expert are read once per
+ * up to 128 of its rows, those of an expert that nobody chose not at all.
+ *   tokens, top_k, experts, first, local   tokens * top_k < 2^26, top_k 1 .. 32, experts 1 .. 1024,
+ *                first >= 0, local >= 0, first + local <= experts.
+ *   hidden, inner   > 0 (the sizes of x[t] and h[t,i]).
+ *   x, ldx       [tokens, ldx] of type dt, 16-byte aligned, ldx >= hidden and a multiple of 8; below 2^31 bytes in all.
+ *   W1, ldw1, stride1   [local][2 inner, ldw1]: gate rows, then up rows; 16-byte aligned, ldw1 >= hidden, both multiples of 8.
+ *   W2, ldw2, stride2   [local][hidden, ldw2], likewise, ldw2 >= inner.  The matrices of one expert below 2^31 bytes each; strides
+ *                (elements, at least a matrix) are 64-bit.
+ *   chosen, weights, offsets, pairs   as nmm_moe_route leaves them.  Indices that point outside are skipped; pairs and
+ *                offsets that do not belong to chosen leave y undefined.
+ *   residual, ldr   [tokens, ldr] of type dt, or NULL; it may be y (the same address and leading dimension).
+ *   y, ldy       of type dt, 2-byte aligned, ldy >= hidden; otherwise it may overlap nothing that the call reads (NMM_ERR_ARG
+ *                for the residual and x).
+ * Deterministic; the launches depend on the sizes alone, so a captured call follows chosen as it changes.  Workspace:
+ * nmm_moe_experts_workspace_size, about tokens * top_k * (2 inner + 4 hidden) bytes.
+ */
+typedef struct {
+    int64_t tokens, top_k, experts, first, local;
+    int64_t hidden, inner;
+    nmm_dtype dt;
+    nmm_act act;
+    const void* x;
+    int64_t ldx;
+    const void* W1;
+    int64_t ldw1, stride1;
+    const void* W2;
+    int64_t ldw2, stride2;
+    const int32_t* chosen;
+    const float* weights;
+    const int32_t* offsets;
+    const int32_t* pairs;
+    const void* residual;
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+} nmm_moe_ffn;
+
+nmm_status nmm_moe_experts(const nmm_moe_ffn* ffn, void* workspace, size_t workspace_bytes, void* stream);
+size_t nmm_moe_experts_workspace_size(const nmm_moe_ffn* ffn);
+
 /* Workspace sizes in bytes (0 when none is needed; never fails: invalid sizes give 0). */
 size_t nmm_gemv_workspace_size(int64_t M, int64_t K, int64_t N, nmm_dtype dt, nmm_path path);
 size_t nmm_batched_gemv_workspace_size(int64_t batch, int64_t M, int64_t K, int64_t N,

@@ -26,6 +26,8 @@ NMM_ROUND_EVEN, NMM_ROUND_AWAY = 0, 1
 NMM_CACHE_BF16, NMM_CACHE_E4M3 = 1, 2
 NMM_SRC_F32, NMM_SRC_BF16 = 0, 1
 NMM_W4_INT, NMM_W4_MX = 1, 2
+NMM_ACT_NONE, NMM_ACT_RELU, NMM_ACT_SILU, NMM_ACT_GELU, NMM_ACT_GELU_TANH = range(5)
+NMM_SCORE_SOFTMAX, NMM_SCORE_SIGMOID = 1, 2
 NMM_NOALLOC_SCRATCH_BYTES = 8 << 20   # nmm_gemv_noalloc's scratch per GPU
 
 _i64 = ctypes.c_int64
@@ -101,6 +103,26 @@ class nmm_latent_attn_batch(ctypes.Structure):
                 ("scale", ctypes.c_float), ("out", _p), ("stride_ob", _i64), ("stride_ot", _i64), ("ldo", _i64)]
 
 
+class nmm_nt_act(ctypes.Structure):
+    _fields_ = [("M", _i64), ("K", _i64), ("N", _i64), ("dt", ctypes.c_int), ("act", ctypes.c_int), ("gated", ctypes.c_int),
+                ("x", _p), ("ldx", _i64), ("Wt", _p), ("ldwt", _i64), ("bias", _p), ("residual", _p), ("ldr", _i64), ("y", _p),
+                ("ldy", _i64), ("y_f32", _p), ("ldyf", _i64)]
+
+
+class nmm_moe_router(ctypes.Structure):
+    _fields_ = [("tokens", _i64), ("experts", _i64), ("top_k", _i64), ("logits", _p), ("logits_type", ctypes.c_int),
+                ("ld_logits", _i64), ("score", ctypes.c_int), ("bias", _p), ("groups", _i64), ("top_groups", _i64),
+                ("group_top", _i64), ("renormalize", ctypes.c_int), ("scale", ctypes.c_float), ("mask", _p), ("chosen", _p),
+                ("weights", _p), ("offsets", _p), ("pairs", _p)]
+
+
+class nmm_moe_ffn(ctypes.Structure):
+    _fields_ = [(n, _i64) for n in ("tokens", "top_k", "experts", "first", "local", "hidden", "inner")] + \
+               [("dt", ctypes.c_int), ("act", ctypes.c_int), ("x", _p), ("ldx", _i64), ("W1", _p), ("ldw1", _i64),
+                ("stride1", _i64), ("W2", _p), ("ldw2", _i64), ("stride2", _i64), ("chosen", _p), ("weights", _p),
+                ("offsets", _p), ("pairs", _p), ("residual", _p), ("ldr", _i64), ("y", _p), ("ldy", _i64)]
+
+
 EXPORTS = {
     "nmm_gemv": (ctypes.c_int, [_i64, _i64, _i64, ctypes.c_int, _p, _i64, _p, _i64, _p, _i64,
                                 ctypes.c_int, _p, _sz, _p]),
@@ -139,6 +161,12 @@ EXPORTS = {
     "nmm_latent_cache_read": (ctypes.c_int, [_p, _i64, _p, _p, _i64, _p]),
     "nmm_latent_attention_batch": (ctypes.c_int, [_p, _p, _sz, _p]),
     "nmm_latent_attention_batch_workspace_size": (_sz, [_p]),
+    "nmm_gemv_nt_act": (ctypes.c_int, [_p, _p, _sz, _p]),
+    "nmm_gemv_nt_act_workspace_size": (_sz, [_p]),
+    "nmm_moe_route": (ctypes.c_int, [_p, _p, _sz, _p]),
+    "nmm_moe_route_workspace_size": (_sz, [_p]),
+    "nmm_moe_experts": (ctypes.c_int, [_p, _p, _sz, _p]),
+    "nmm_moe_experts_workspace_size": (_sz, [_p]),
     "nmm_gemv_workspace_size": (_sz, [_i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_batched_gemv_workspace_size": (_sz, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int]),
     "nmm_mla_decode_chain_workspace_size": (_sz, [ctypes.POINTER(nmm_mla_chain)]),
@@ -800,6 +828,115 @@ def nmm_latent_attention_batch(q: torch.Tensor, cache: torch.Tensor, out: torch.
     _call(L.nmm_latent_attention_batch, "nmm_latent_attention_batch",
           lambda: L.nmm_latent_attention_batch_workspace_size(args), (args,), workspace, q.device, stream)
     return out
+
+
+# The bytes of nmm_nt_act, nmm_moe_router and nmm_moe_ffn.
+_NT_ACT = struct.Struct("@qqqiii4xPqPqPPqPqPq")
+_ROUTER = struct.Struct("@qqqPi4xqi4xPqqqif" + "PPPPP")
+_FFN = struct.Struct("@qqqqqqqiiPqPqqPqqPPPPPqPq")
+
+
+def nmm_gemv_nt_act(x: torch.Tensor, Wt: torch.Tensor, y: torch.Tensor | None, *, act: int = NMM_ACT_NONE, gated: bool = False,
+                    bias: torch.Tensor | None = None, residual: torch.Tensor | None = None, y_f32: torch.Tensor | None = None,
+                    K: int | None = None, workspace=None, stream=None) -> torch.Tensor:
+    """y[M,N] = act(x[M,K] . Wt[N,K]^T + bias) + residual, or gated (Wt [2 N, K]: the gate's rows, then those it is multiplied
+    with) act(gate) * up + residual.  x, Wt, bias, residual and y are bf16 or fp16, y_f32 (optional; y may then be None) holds
+    the values before their rounding.  ``residual`` may be ``y``.  K is x's width unless given."""
+    _same_device("nmm_gemv_nt_act", x, Wt, y, bias, residual, y_f32)
+    code, dt = _CODES.get(x.dtype), x.dtype
+    out = y if y is not None else y_f32
+    if out is None:
+        raise ValueError("nmm_gemv_nt_act needs y or y_f32")
+    if code is None or Wt.dtype != dt or (y is not None and y.dtype != dt) or (y_f32 is not None and y_f32.dtype != torch.float32):
+        raise TypeError("x, Wt and y must be bfloat16 or float16 alike, y_f32 float32")
+    if not (x.dim() == Wt.dim() == out.dim() == 2):
+        raise ValueError("nmm_gemv_nt_act takes 2-D tensors")
+    (M, width), (rows, w_width), N = x.shape, Wt.shape, out.shape[1]
+    K = width if K is None else K
+    if out.shape[0] != M or width < K or w_width < K or rows != (2 * N if gated else N) or \
+            (y is not None and y_f32 is not None and y_f32.shape != y.shape):
+        raise ValueError("x [M, >= K], Wt [N, >= K] (gated [2 N, >= K]) and y [M, N] do not fit each other")
+    if bias is not None and (bias.dtype != dt or bias.dim() != 1 or bias.numel() != rows or (rows > 1 and bias.stride(0) != 1)):
+        raise ValueError("bias must be a contiguous vector of x's type, one value per row of Wt")
+    if residual is not None and (residual.dtype != dt or residual.shape != out.shape):
+        raise ValueError("residual must have x's type and y's shape")
+    args = _NT_ACT.pack(M, K, N, code, act, 1 if gated else 0, x.data_ptr(), _ld(x), Wt.data_ptr(), _ld(Wt),
+                        0 if bias is None else bias.data_ptr(), *((0, 0) if residual is None else (residual.data_ptr(), _ld(residual))),
+                        *((0, 0) if y is None else (y.data_ptr(), _ld(y))),
+                        *((0, 0) if y_f32 is None else (y_f32.data_ptr(), _ld(y_f32))))
+    L = lib()
+    _call(L.nmm_gemv_nt_act, "nmm_gemv_nt_act", lambda: L.nmm_gemv_nt_act_workspace_size(args), (args,), workspace, x.device, stream)
+    return out
+
+
+def _pairs_of(where: str, t: torch.Tensor, dtype: torch.dtype, shape: tuple) -> int:
+    """The address of a contiguous [tokens, top_k] tensor."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{where} must be a contiguous {dtype} tensor [tokens, top_k]")
+    return t.data_ptr()
+
+
+def nmm_moe_route(logits: torch.Tensor, chosen: torch.Tensor, weights: torch.Tensor, offsets: torch.Tensor, pairs: torch.Tensor, *,
+                  score: int, bias: torch.Tensor | None = None, groups: int = 1, top_groups: int = 1, group_top: int = 1,
+                  renormalize: bool = False, scale: float = 1.0, mask: torch.Tensor | None = None, workspace=None,
+                  stream=None) -> tuple:
+    """The top_k experts of every token (see nmm.h): logits [tokens, experts] fp32 or bf16; chosen int32 and weights fp32
+    [tokens, top_k]; offsets int32 [experts + 1] and pairs int32 [tokens * top_k], the pairs in the order of the experts; bias
+    fp32 [experts], mask uint8 or bool [tokens] (0: padding).  Returns (chosen, weights, offsets, pairs)."""
+    _same_device("nmm_moe_route", logits, chosen, weights, offsets, pairs, bias, mask)
+    f32 = logits.dtype == torch.float32
+    if logits.dim() != 2 or not (f32 or logits.dtype == torch.bfloat16) or chosen.dim() != 2:
+        raise TypeError("logits must be a 2-D float32 or bfloat16 tensor, chosen a 2-D int32 one")
+    (T, E), k = logits.shape, chosen.shape[1]
+    if bias is not None and (bias.dtype != torch.float32 or bias.dim() != 1 or bias.numel() != E or (E > 1 and bias.stride(0) != 1)):
+        raise ValueError("bias must be a contiguous float32 vector, one value per expert")
+    if mask is not None and (mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 1 or mask.numel() != T or
+                             (T > 1 and mask.stride(0) != 1)):
+        raise ValueError("mask must be a contiguous uint8 or bool vector, one value per token")
+    args = _ROUTER.pack(T, E, k, logits.data_ptr(), NMM_SRC_F32 if f32 else NMM_SRC_BF16, _ld(logits), score,
+                        0 if bias is None else bias.data_ptr(), groups, top_groups, group_top, 1 if renormalize else 0, scale,
+                        0 if mask is None else mask.data_ptr(), _pairs_of("chosen", chosen, torch.int32, (T, k)),
+                        _pairs_of("weights", weights, torch.float32, (T, k)), _index("offsets", offsets, torch.int32, E + 1),
+                        _index("pairs", pairs, torch.int32, T * k))
+    L = lib()
+    _call(L.nmm_moe_route, "nmm_moe_route", lambda: L.nmm_moe_route_workspace_size(args), (args,), workspace, logits.device, stream)
+    return chosen, weights, offsets, pairs
+
+
+def nmm_moe_experts(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, chosen: torch.Tensor, weights: torch.Tensor,
+                    offsets: torch.Tensor, pairs: torch.Tensor, y: torch.Tensor, *, act: int = NMM_ACT_SILU, first: int = 0,
+                    hidden: int | None = None, inner: int | None = None, residual: torch.Tensor | None = None, workspace=None,
+                    stream=None) -> torch.Tensor:
+    """y[t] = residual[t] + sum_i weights[t,i] (act(x[t] . gate^T) * (x[t] . up^T)) . w2[e]^T over the experts e = chosen[t,i] in
+    first .. first + local - 1 that w1 [local, 2 inner, >= hidden] (gate rows, then up rows) and w2 [local, hidden, >= inner]
+    hold.  x, w1, w2, residual and y are bf16 or fp16 alike; chosen, weights, offsets and pairs as nmm_moe_route leaves them.
+    ``residual`` may be ``y``.  hidden is y's width and inner half of w1's rows unless given."""
+    _same_device("nmm_moe_experts", x, w1, w2, chosen, weights, offsets, pairs, y, residual)
+    code, dt = _CODES.get(x.dtype), x.dtype
+    if code is None or w1.dtype != dt or w2.dtype != dt or y.dtype != dt:
+        raise TypeError("x, w1, w2 and y must be bfloat16 or float16 alike")
+    if not (x.dim() == y.dim() == chosen.dim() == 2 and w1.dim() == w2.dim() == 3) or offsets.dim() != 1:
+        raise ValueError("x, y and chosen must be 2-D, w1 and w2 3-D tensors, offsets a vector")
+    T, k = chosen.shape
+    hidden = y.shape[1] if hidden is None else hidden
+    inner = w1.shape[1] // 2 if inner is None else inner
+    local, experts = w1.shape[0], offsets.numel() - 1
+    if x.shape[0] != T or y.shape[0] != T or x.shape[1] < hidden or y.shape[1] < hidden or w2.shape[0] != local or \
+            w1.shape[1] != 2 * inner or w1.shape[2] < hidden or w2.shape[1] != hidden or w2.shape[2] < inner:
+        raise ValueError("x [tokens, >= hidden], w1 [local, 2 inner, >= hidden], w2 [local, hidden, >= inner] and y [tokens, >= hidden] "
+                         "do not fit each other")
+    if residual is not None and (residual.dtype != dt or residual.shape != y.shape):
+        raise ValueError("residual must have x's type and y's shape")
+    # (no experts here: tensors without values, whose strides say nothing)
+    ld1, ld2 = (_ld(w1), _ld(w2)) if local else (0, 0)
+    args = _FFN.pack(T, k, experts, first, local, hidden, inner, code, act, x.data_ptr(), _ld(x), w1.data_ptr(), ld1,
+                     w1.stride(0), w2.data_ptr(), ld2, w2.stride(0), _pairs_of("chosen", chosen, torch.int32, (T, k)),
+                     _pairs_of("weights", weights, torch.float32, (T, k)), _index("offsets", offsets, torch.int32, experts + 1),
+                     _index("pairs", pairs, torch.int32, T * k),
+                     *((0, 0) if residual is None else (residual.data_ptr(), _ld(residual))), y.data_ptr(), _ld(y))
+    L = lib()
+    _call(L.nmm_moe_experts, "nmm_moe_experts", lambda: L.nmm_moe_experts_workspace_size(args), (args,), workspace, x.device, stream)
+    return y
 
 
 def nmm_read_probe(buf: torch.Tensor, out: torch.Tensor, grid: int, unroll: int = 4, stream=None) -> None:

@@ -29,6 +29,7 @@
 #include "latent_row.h"
 #include "nmm_internal.h"
 #include "rope.h"
+#include "wave64.h"
 
 namespace nmm {
 namespace {
@@ -53,32 +54,6 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_move(float x) {
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, false));
 }
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-
-template <int CTRL>
-__device__ __forceinline__ double dpp_move(double x) {
-    const uint64_t u = __double_as_longlong(x);
-    const uint32_t lo = __builtin_amdgcn_mov_dpp(int(uint32_t(u)), CTRL, 0xF, 0xF, false);
-    const uint32_t hi = __builtin_amdgcn_mov_dpp(int(uint32_t(u >> 32)), CTRL, 0xF, 0xF, false);
-    return __longlong_as_double((uint64_t(hi) << 32) | lo);
-}
-
-// The sum over the wave in every lane, in a fixed order: quads, half rows, rows, then across rows.
-__device__ __forceinline__ double sum64(double x) {
-    x += dpp_move<0xB1>(x);
-    x += dpp_move<0x4E>(x);
-    x += dpp_move<0x141>(x);
-    x += dpp_move<0x140>(x);
-    uint64_t u = __double_as_longlong(x);
-    u32x2 lo = __builtin_amdgcn_permlane16_swap(uint32_t(u), uint32_t(u), false, false);
-    u32x2 hi = __builtin_amdgcn_permlane16_swap(uint32_t(u >> 32), uint32_t(u >> 32), false, false);
-    x = __longlong_as_double((uint64_t(hi[0]) << 32) | lo[0]) + __longlong_as_double((uint64_t(hi[1]) << 32) | lo[1]);
-    u = __double_as_longlong(x);
-    lo = __builtin_amdgcn_permlane32_swap(uint32_t(u), uint32_t(u), false, false);
-    hi = __builtin_amdgcn_permlane32_swap(uint32_t(u >> 32), uint32_t(u >> 32), false, false);
-    return __longlong_as_double((uint64_t(hi[0]) << 32) | lo[0]) + __longlong_as_double((uint64_t(hi[1]) << 32) | lo[1]);
-}
-
 // x^(-1/2): the fp32 instruction and one Newton step in fp64 (1e-14), or in fp64 altogether outside fp32's range.
 __device__ __forceinline__ double inverse_root(double x) {
     if (!(x > 1e-30 && x < 1e30)) return 1.0 / __builtin_sqrt(x);

@@ -128,6 +128,10 @@ nmm_status plan_gemv(int64_t batch, int64_t M, int64_t K, int64_t N, int dt, int
                      int unroll = 0);
 nmm_status validate_workspace(const void* ws, size_t bytes, size_t need);
 
+// Whether an element of n rows a (`wa` bytes each, `lda` apart) is also one of rows b.  Rows of one pitch that take turns (two
+// column ranges of one buffer) do not overlap; of other pitches, what they span decides.
+bool rows_overlap(const void* a, int64_t lda, int64_t wa, const void* b, int64_t ldb, int64_t wb, int64_t n);
+
 // Launchers (defined next to their kernels).  They assume validated arguments.
 // `tickets` points into a workspace's counter block and `part` past it (both unused when the
 // plan does not split K).

@@ -1,0 +1,260 @@
+"""nmm_moe_experts against its formula in 64 bits (oracle/ffn.py derives how far it may be off).
+
+Sparse small integers make h and every sum exact, so those results must be equal, after one rounding to the output's type.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ffn
+
+pytestmark = pytest.mark.gpu
+
+nmm = pytest.importorskip("paper_2609_16009_amd")
+
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TYPES = pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+
+
+def order(chosen, E):
+    """offsets and pairs of a choice, as the router leaves them."""
+    flat = chosen.reshape(-1)
+    live = flat >= 0
+    pairs = np.argsort(np.where(live, flat, E), kind="stable")
+    pairs[np.count_nonzero(live):] = -5                           # places that nobody may read
+    return np.concatenate(([0], np.cumsum(np.bincount(flat[live], minlength=E)))).astype(np.int32), pairs.astype(np.int32)
+
+
+def dev(a, dt=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if dt is None else t.to(dt)).cuda()
+
+
+class Case:
+    def __init__(self, seed, T, E, k, hidden, inner, dt=torch.bfloat16, integer=False, first=0, local=None, residual=True, chosen=None,
+                 pad=0):
+        rng = np.random.default_rng(seed)
+        self.T, self.E, self.k, self.hidden, self.inner, self.dt, self.integer, self.first = T, E, k, hidden, inner, dt, integer, first
+        self.local = local = E - first if local is None else local
+        up8 = lambda n: (n + 7) // 8 * 8 + 8 * pad
+
+        def tensor(shape, width, sigma, sparse=0):
+            if integer:      # a few -1, 0, 1 a row, so that |z| <= 12 and |h| <= 144
+                v = np.zeros(shape)
+                if sparse:
+                    idx = rng.integers(0, shape[-1], (*shape[:-1], 12))
+                    np.put_along_axis(v, idx, rng.integers(-1, 2, idx.shape).astype(np.float64), -1)
+                else:
+                    v = rng.integers(-1, 2, shape).astype(np.float64)
+            else:
+                v = rng.standard_normal(shape) * sigma
+            full = np.full((*shape[:-1], width), np.nan, dtype=np.float32)
+            full[..., :shape[-1]] = v
+            t = torch.from_numpy(full).to(dt)
+            return t.cuda(), t[..., :shape[-1]].double().numpy()
+
+        self.x, self.xv = tensor((T, hidden), up8(hidden), 1.0, 1)
+        self.w1, self.w1v = tensor((local, 2 * inner, hidden), up8(hidden), hidden ** -0.5)
+        self.w2, self.w2v = tensor((local, hidden, inner), up8(inner), inner ** -0.5)
+        self.res, self.resv = tensor((T, hidden), hidden + 3 * pad, 1.0) if residual else (None, None)
+        if chosen is None:
+            chosen = np.stack([rng.permutation(E)[:k] for _ in range(T)]) if T else np.zeros((0, k))
+        self.chosen = np.asarray(chosen, dtype=np.int32)
+        self.weights = (2.0 ** rng.integers(-2, 2, (T, k)) if integer else rng.random((T, k)) + 0.1).astype(np.float32)
+        self.route = [dev(self.chosen), dev(self.weights), *map(dev, order(self.chosen, E))]
+
+    def run(self, act=2, y=None, **kw):
+        self.out = torch.full((self.T, self.hidden + 5), 7.0, dtype=self.dt, device="cuda") if y is None else y
+        return nmm.nmm_moe_experts(self.x, self.w1, self.w2, *self.route, self.out[:, :self.hidden], hidden=self.hidden, inner=self.inner,
+                                   first=self.first, act=act, residual=None if self.res is None else self.res[:, :self.hidden], **kw)
+
+    def check(self, act=2, **kw):
+        self.run(act, **kw)
+        got = self.out.double().cpu().numpy()
+        assert (got[:, self.hidden:] == 7).all(), "columns past hidden"
+        got = got[:, :self.hidden]
+        ref, err = ffn.experts(self.xv, self.w1v, self.w2v, self.chosen, self.weights, self.first, act, HALF[self.dt], self.resv)
+        if self.integer:
+            want = torch.from_numpy(ref.astype(np.float32)).to(self.dt).double().numpy()
+            assert np.array_equal(got, want), (self.T, self.E, self.k, self.hidden, self.inner, np.argwhere(got != want)[:4])
+        else:
+            bad = ~(np.abs(got - ref) <= err + HALF[self.dt] * (np.abs(ref) + err) + 2.0 ** -25)
+            assert not bad.any(), (self.T, self.E, self.k, self.hidden, self.inner, bad.sum(), np.argwhere(bad)[:4])
+
+
+@TYPES
+@pytest.mark.parametrize("act", [0, 1])
+def test_integers_exact_at_every_token_count(dt, act):
+    for T in (1, 2, 3, 4, 5, 8, 9, 16, 17, 33, 70, 140):
+        Case(T, T, 8, 3, 72, 40, dt, integer=True, residual=T % 2 == 0).check(act)
+
+
+@TYPES
+@pytest.mark.parametrize("hidden,inner", [(1, 1), (7, 3), (8, 16), (17, 15), (64, 64), (65, 33), (130, 129), (257, 100), (1037, 331)])
+def test_integers_exact_at_odd_sizes(hidden, inner, dt):
+    for T, E, k in ((1, 4, 2), (6, 5, 2), (40, 3, 2), (150, 2, 1)):
+        Case(T + hidden, T, E, k, hidden, inner, dt, integer=True, pad=T % 2).check(1)
+
+
+@TYPES
+@pytest.mark.parametrize("act", range(5))
+def test_every_activation(act, dt):
+    for T, E, k, hidden, inner in ((1, 16, 8, 256, 128), (11, 6, 2, 333, 77), (90, 4, 2, 136, 200), (300, 4, 3, 128, 72)):
+        Case(T + act, T, E, k, hidden, inner, dt, residual=T % 2 == 1).check(act)
+
+
+@pytest.mark.parametrize("T,E,k,hidden,inner", [(1, 64, 8, 7168, 256), (64, 16, 4, 1024, 512), (200, 8, 2, 2048, 128)])
+def test_larger_sizes(T, E, k, hidden, inner):
+    Case(T, T, E, k, hidden, inner).check()
+
+
+def test_uneven_choices():
+    for T in (5, 40, 200):
+        for E in (1, 3, 64):
+            one = np.full((T, 1), E - 1)
+            Case(T, T, E, 1, 96, 64, integer=True, chosen=one).check(1)          # one expert has all
+        half = np.where(np.arange(T)[:, None] % 2 == 0, 5, np.arange(T)[:, None] % 32)
+        Case(T, T, 32, 1, 96, 64, integer=True, chosen=half).check(1)
+        same = np.full((T, 2), 3)                                                # the same expert twice
+        Case(T, T, 8, 2, 96, 64, integer=True, chosen=same).check(1)
+
+
+@pytest.mark.parametrize("first,local", [(0, 8), (8, 8), (3, 1), (15, 1), (0, 0), (16, 0), (5, 11)])
+def test_experts_of_one_gpu(first, local):
+    for T in (1, 9, 64):
+        Case(T, T, 16, 4, 88, 48, integer=True, first=first, local=local, residual=T != 9).check(1)
+
+
+def test_shards_add_up():
+    """Two halves of the experts, the second onto the first one's result: what all of them give, in fp16 integers exactly."""
+    a = Case(4, 30, 12, 3, 64, 40, torch.float16, integer=True)
+    a.run(1)
+    b = Case(4, 30, 12, 3, 64, 40, torch.float16, integer=True)
+    w1, w2 = b.w1, b.w2
+    y = b.res.clone()
+    for first, local in ((0, 7), (7, 5)):
+        nmm.nmm_moe_experts(b.x, w1[first:first + local], w2[first:first + local], *b.route, y, hidden=64, inner=40, first=first, act=1,
+                            residual=y)
+    assert torch.equal(y, a.out[:, :64])
+
+
+def test_padded_tokens_keep_their_residual():
+    for T in (1, 10, 100):
+        rng = np.random.default_rng(T)
+        chosen = np.stack([rng.permutation(8)[:2] for _ in range(T)])
+        chosen[::3] = -1
+        c = Case(T, T, 8, 2, 80, 40, integer=True, chosen=chosen)
+        c.check(1)
+        assert torch.equal(c.out[::3, :80], c.res[::3])
+        c = Case(T, T, 8, 2, 80, 40, integer=True, chosen=np.full((T, 2), -1), residual=False)
+        c.check(1)
+        assert not c.out[:, :80].any()
+
+
+def test_a_value_that_is_not_finite_stays_in_its_row():
+    for T in (1, 6, 60):
+        c = Case(T, T, 6, 2, 128, 64)
+        c.run()
+        clean = c.out.clone()
+        hurt = T // 2
+        c.x[hurt, 5] = float("nan")
+        c.run()
+        keep = torch.arange(T, device="cuda") != hurt
+        assert torch.equal(c.out[keep], clean[keep]) and torch.isnan(c.out[hurt, :128]).all()
+
+
+def test_indices_that_point_outside_are_skipped():
+    """Indices that do not fit: nothing is read or written outside, whatever y then holds; then a right call on the workspace."""
+    ws = nmm.Workspace()
+    for T in (1, 7, 50):
+        c = Case(T, T, 8, 2, 96, 48, integer=True)
+        good = [t.clone() for t in c.route]
+        c.route[3].fill_(1 << 30)
+        c.run(1, workspace=ws)
+        c.route[3].fill_(-1)
+        c.run(1, workspace=ws)
+        c.route[3].copy_(good[3])
+        for wild in (-(1 << 31), (1 << 31) - 1, 2 * T + 1, -1):
+            c.route[2].fill_(wild)
+            c.run(1, workspace=ws)
+        c.route[2].copy_(good[2].flip(0))                     # descending
+        c.run(1, workspace=ws)
+        c.route[2].copy_(good[2])
+        c.route[0].add_(1 << 29)                              # no expert that there is
+        c.run(1, workspace=ws)
+        assert torch.equal(c.out[:, :96], c.res)
+        c.route[0].copy_(good[0])
+        c.check(1, workspace=ws)
+
+
+def test_weights_past_two_gigabytes():
+    """Expert strides in 64 bits: the last of 40 experts 5 GB behind the first."""
+    local, hidden, inner = 40, 128, 64
+    stride = 1 << 26
+    c = Case(3, 20, local, 2, hidden, inner, integer=True)
+    pool = torch.zeros((local - 1) * stride + 2 * inner * hidden, dtype=torch.bfloat16, device="cuda")
+    w1 = pool.as_strided((local, 2 * inner, hidden), (stride, hidden, 1))
+    w1.copy_(c.w1)
+    w2 = pool.as_strided((local - 1, hidden, inner), (stride, inner, 1), 1 << 20)
+    w2.copy_(c.w2[:local - 1])
+    keep = c.w2
+    c.w1 = w1
+    c.check(1)
+    c.w1, c.w2 = w1[:local - 1], w2
+    c.local -= 1
+    c.w1v, c.w2v = c.w1v[:-1], c.w2v[:-1]
+    c.check(1)
+    del keep
+
+
+def test_in_place_streams_captures_and_repeats():
+    ws = nmm.Workspace()
+    for T in (1, 16, 200):
+        c = Case(T, T, 16, 4, 256, 96)
+        c.run(workspace=ws)
+        ref = c.out[:, :256].clone()
+        y = c.res.clone()
+        nmm.nmm_moe_experts(c.x, c.w1, c.w2, *c.route, y, act=2, residual=y, workspace=ws)
+        assert torch.equal(y, ref)
+        y = torch.zeros_like(ref)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        nmm.nmm_moe_experts(c.x, c.w1, c.w2, *c.route, y, act=2, residual=c.res, stream=s)
+        s.synchronize()
+        assert torch.equal(y, ref)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            nmm.nmm_moe_experts(c.x, c.w1, c.w2, *c.route, y, act=2, residual=c.res, workspace=ws)
+        rng = np.random.default_rng(T)
+        for i in range(3):
+            # another choice, which the captured launches follow
+            chosen = np.stack([rng.permutation(16)[:4] for _ in range(T)]).astype(np.int32)
+            if i == 2:
+                chosen[:] = 3
+            offsets, pairs = order(chosen, 16)
+            for t, a in zip((c.route[0], c.route[2], c.route[3]), (chosen, offsets, pairs)):
+                t.copy_(torch.from_numpy(a))
+            y.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            c.chosen = chosen
+            c.check(workspace=ws)
+            assert torch.equal(c.out[:, :256], y)
+
+
+def test_binding_refuses():
+    c = Case(1, 4, 8, 2, 64, 32)
+    y = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
+    names = ("x", "w1", "w2", "chosen", "weights", "offsets", "pairs", "y")
+    base = dict(zip(names, (c.x, c.w1, c.w2, *c.route, y)))
+    for bad in (dict(x=c.x.half()), dict(w1=c.w1.float()), dict(w2=c.w2.half()), dict(y=y.float())):
+        with pytest.raises(TypeError):
+            nmm.nmm_moe_experts(**{**base, **bad})
+    for bad in (dict(x=c.x[:3]), dict(y=y[:3]), dict(w1=c.w1[:7]), dict(w1=c.w1[:, :61]), dict(w2=c.w2[:, :60]), dict(hidden=65),
+                dict(inner=33), dict(chosen=c.route[0].long()), dict(weights=c.route[1][:3]), dict(offsets=c.route[2].long()),
+                dict(pairs=c.route[3][:-1]), dict(residual=y.float()), dict(residual=y[:3]), dict(x=c.x.cpu()), dict(w1=c.w1[0])):
+        with pytest.raises(ValueError):
+            nmm.nmm_moe_experts(**{**base, **bad})
+    for bad in (dict(first=1), dict(act=7), dict(offsets=c.route[2][:8])):
+        with pytest.raises(nmm.NmmError):
+            nmm.nmm_moe_experts(**{**base, **bad})

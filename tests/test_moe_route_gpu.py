@@ -1,0 +1,194 @@
+"""nmm_moe_route against its formula in 64 bits: experts, offsets and the order of the pairs must be equal, weights one rounding
+to fp32 away (2^-24, and 2^-50 for 64-bit arithmetic in another order)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ffn
+
+pytestmark = pytest.mark.gpu
+
+nmm = pytest.importorskip("paper_2609_16009_amd")
+
+SOFTMAX, SIGMOID = nmm.NMM_SCORE_SOFTMAX, nmm.NMM_SCORE_SIGMOID
+
+
+def outputs(T, E, k):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    return (torch.full((T, k), -7, **i32), torch.full((T, k), 9.0, device="cuda"), torch.full((E + 1,), -7, **i32),
+            torch.full((T * k,), -7, **i32))
+
+
+def compare(out, logits, k, score, bias=None, mask=None, renormalize=False, scale=1.0, **kw):
+    chosen, weights, offsets, pairs = (o.cpu().numpy() for o in out)
+    np32 = lambda t: None if t is None else t.double().cpu().numpy()
+    r_chosen, r_w, r_off, r_pairs = ffn.route(np32(logits), k, score == SOFTMAX, np32(bias), renormalize=renormalize,
+                                              scale=float(np.float32(scale)), mask=None if mask is None else mask.cpu().numpy(), **kw)
+    assert np.array_equal(chosen, r_chosen)
+    assert np.array_equal(offsets, r_off)
+    assert np.array_equal(pairs[:len(r_pairs)], r_pairs)
+    assert (pairs[len(r_pairs):] == -7).all(), "places behind the last pair"
+    same = np.isnan(r_w) & np.isnan(weights) | (np.abs(weights - r_w) <= 2.0 ** -24 * np.abs(r_w) + 2.0 ** -50 + 2.0 ** -149)
+    assert same.all(), np.argwhere(~same)[:3]
+
+
+def check(seed, T, E, k, score, bias=False, mask=False, dt=torch.float32, sigma=1.5, pad=0, workspace=None, logits=None, **kw):
+    rng = np.random.default_rng(seed)
+    if logits is None:
+        logits = rng.standard_normal((T, E + pad)) * sigma
+    logits = torch.from_numpy(np.asarray(logits, dtype=np.float32)).to(dt).cuda()[:, :E]
+    b = torch.from_numpy(rng.standard_normal(E).astype(np.float32) * 0.1).cuda() if bias else None
+    m = torch.from_numpy((rng.random(T) < 0.7).astype(np.uint8)).cuda() if mask else None
+    out = outputs(T, E, k)
+    got = nmm.nmm_moe_route(logits, *out, score=score, bias=b, mask=m, workspace=workspace, **kw)
+    assert all(a is b_ for a, b_ in zip(got, out))
+    compare(out, logits, k, score, b, m, **kw)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("E,k", [(1, 1), (2, 1), (5, 5), (8, 2), (60, 6), (63, 8), (64, 8), (65, 3), (128, 8), (160, 6), (256, 8), (257, 32),
+                                 (512, 10), (1000, 8), (1024, 32)])
+def test_every_width(E, k, score):
+    for T in (1, 3, 4, 5, 33):
+        check(E + T, T, E, k, score, bias=T % 2 == 0, renormalize=T > 3, scale=2.5, mask=T == 33)
+
+
+@pytest.mark.parametrize("E,groups,top", [(256, 8, 4), (64, 8, 1), (64, 4, 4), (160, 8, 3), (96, 32, 16), (128, 64, 60), (1024, 16, 2),
+                                          (60, 4, 3), (6, 2, 1), (8, 8, 8)])
+@pytest.mark.parametrize("group_top", [1, 2])
+def test_groups(E, groups, top, group_top):
+    k = min(8, E // groups * top)
+    for T in (1, 50):
+        for score in (SOFTMAX, SIGMOID):
+            check(E + T, T, E, k, score, bias=True, groups=groups, top_groups=top, group_top=group_top, renormalize=True)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("groups", [1, 8])
+def test_ties_go_to_the_lowest_index(score, groups):
+    rng = np.random.default_rng(1)
+    for T, E, k in ((1, 256, 8), (40, 64, 8), (9, 1000, 20)):
+        for values in ([0.0], [0.0, 1.0], [-1.0, 0.5, 2.0]):
+            kw = dict(groups=groups, top_groups=4, group_top=2) if groups > 1 else {}
+            check(0, T, E, k, score, logits=rng.choice(values, (T, E)), **kw)
+    check(3, 200, 256, 8, score, dt=torch.bfloat16)          # few distinct bf16 logits among many
+
+
+def test_logits_that_are_not_finite():
+    inf, nan = np.inf, np.nan
+    l = np.zeros((6, 16))
+    l[0, 3:] = -inf                      # fewer finite ones than top_k
+    l[1, :] = -inf                       # none: softmax is NaN
+    l[2, 5], l[2, 6] = nan, 2.0
+    l[3, 2], l[3, 9] = inf, 4.0
+    l[4] = nan
+    l[5, 7:] = 90.0                      # saturated
+    for score in (SOFTMAX, SIGMOID):
+        for renormalize in (False, True):
+            check(0, 6, 16, 6, score, logits=l, renormalize=renormalize)
+            check(0, 6, 16, 6, score, logits=l, renormalize=renormalize, groups=4, top_groups=2, group_top=2)
+
+
+def test_a_bias_that_closes_experts():
+    rng = np.random.default_rng(2)
+    logits = torch.from_numpy(rng.standard_normal((30, 64)).astype(np.float32)).cuda()
+    bias = torch.zeros(64, device="cuda")
+    bias[::2] = -float("inf")
+    out = outputs(30, 64, 8)
+    nmm.nmm_moe_route(logits, *out, score=SIGMOID, bias=bias)
+    compare(out, logits, 8, SIGMOID, bias)
+    assert (out[0] % 2 == 1).all()
+
+
+def test_masks():
+    for T in (1, 4, 70, 3000):
+        for byte in (0, 1):
+            logits = torch.randn((T, 32), device="cuda")
+            mask = torch.full((T,), byte, dtype=torch.uint8, device="cuda")
+            out = outputs(T, 32, 4)
+            nmm.nmm_moe_route(logits, *out, score=SOFTMAX, mask=mask)
+            compare(out, logits, 4, SOFTMAX, mask=mask)
+    logits, mask = torch.randn((9, 32), device="cuda"), torch.rand(9, device="cuda") < 0.5
+    out = outputs(9, 32, 4)
+    nmm.nmm_moe_route(logits, *out, score=SOFTMAX, mask=mask)
+    compare(out, logits, 4, SOFTMAX, mask=mask)
+
+
+@pytest.mark.parametrize("T,E,k", [(1023, 64, 8), (1024, 64, 8), (1025, 64, 8), (1026, 8, 8), (5000, 256, 2), (8192, 16, 1), (8193, 16, 1),
+                                   (20000, 20, 4)])
+def test_many_tokens(T, E, k):
+    check(T, T, E, k, SIGMOID, bias=True, mask=T % 2 == 0, pad=3, renormalize=True)
+
+
+def test_very_many_tokens_and_skew():
+    """A million pairs and more, nearly all of one expert; checked by torch (the experts do not tie)."""
+    T, E, k = 300001, 128, 4
+    g = torch.Generator(device="cuda").manual_seed(5)
+    logits = torch.randn((T, E), generator=g, device="cuda", dtype=torch.float64).float()
+    logits[:, 77] += 9
+    out = outputs(T, E, k)
+    nmm.nmm_moe_route(logits, *out, score=SOFTMAX)
+    order = torch.sort(logits, dim=1, descending=True, stable=True)[1][:, :k]
+    assert torch.equal(out[0].long(), order)
+    flat = order.reshape(-1)
+    assert torch.equal(out[3].long(), torch.sort(flat, stable=True)[1])
+    assert torch.equal(out[2][1:].long(), torch.cumsum(torch.bincount(flat, minlength=E), 0)) and out[2][0] == 0
+    p = torch.softmax(logits.double(), 1).gather(1, order)
+    assert ((out[1].double() - p).abs() <= 2.0 ** -23 * p).all()
+
+
+def test_no_tokens():
+    out = outputs(0, 64, 8)
+    nmm.nmm_moe_route(torch.zeros((0, 64), device="cuda"), *out, score=SOFTMAX)
+    assert not out[2].any()
+
+
+def test_streams_captures_and_one_workspace():
+    """Calls of every size on one workspace, a captured one among them, which follows its logits and mask."""
+    ws = nmm.Workspace()
+    for T, E, k in ((2000, 64, 8), (3, 64, 8), (70, 256, 8), (9000, 60, 2), (64, 1024, 4)):
+        check(T, T, E, k, SIGMOID, workspace=ws)
+    logits, mask = torch.randn((64, 256), device="cuda"), torch.ones(64, dtype=torch.uint8, device="cuda")
+    kw = dict(score=SIGMOID, groups=8, top_groups=4, group_top=2, renormalize=True)
+    big = torch.randn((1500, 256), device="cuda")
+    out, out_big = outputs(64, 256, 8), outputs(1500, 256, 8)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nmm.nmm_moe_route(logits, *out, mask=mask, workspace=ws, **kw)
+        nmm.nmm_moe_route(big, *out_big, workspace=ws, **kw)
+    for i in range(4):
+        logits.normal_()
+        big.normal_()
+        mask.copy_(torch.rand(64, device="cuda") < 0.5)
+        out[3].fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        compare(out, logits, 8, mask=mask, **kw)
+        compare(out_big, big, 8, **kw)
+        check(i, 70, 256, 8, SIGMOID, workspace=ws)
+    s = torch.cuda.Stream()
+    out2 = outputs(64, 256, 8)
+    s.wait_stream(torch.cuda.current_stream())
+    nmm.nmm_moe_route(logits, *out2, mask=mask, stream=s, **kw)
+    s.synchronize()
+    compare(out2, logits, 8, mask=mask, **kw)
+
+
+def test_binding_refuses():
+    logits = torch.zeros((4, 16), device="cuda")
+    c, w, o, p = outputs(4, 16, 2)
+    for bad in (lambda: nmm.nmm_moe_route(logits.half(), c, w, o, p, score=SOFTMAX),
+                lambda: nmm.nmm_moe_route(logits[0], c, w, o, p, score=SOFTMAX)):
+        with pytest.raises(TypeError):
+            bad()
+    f = torch.zeros(16, device="cuda")
+    for bad in (dict(chosen=c.long()), dict(chosen=c[:3]), dict(weights=w[:, :1]), dict(weights=w.double()), dict(offsets=o[:-1]),
+                dict(pairs=p[:-1]), dict(pairs=p.long()), dict(bias=f[:-1]), dict(bias=f.half()), dict(mask=f[:4]),
+                dict(mask=torch.ones(5, dtype=torch.uint8, device="cuda")), dict(chosen=c.t().contiguous().t()),
+                dict(bias=f.cpu())):
+        kw = dict(chosen=c, weights=w, offsets=o, pairs=p, score=SOFTMAX)
+        kw.update(bad)
+        with pytest.raises(ValueError):
+            nmm.nmm_moe_route(logits, **kw)
+    with pytest.raises(nmm.NmmError, match="NMM_ERR_SHAPE"):
+        nmm.nmm_moe_route(logits, c, w, o, p, score=SOFTMAX, groups=3)
