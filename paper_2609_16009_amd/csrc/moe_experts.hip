@@ -9,6 +9,7 @@
 
 #include "nmm_internal.h"
 #include "nt_rows.h"
+#include "nt_wide.h"
 
 namespace nmm {
 namespace {
@@ -92,13 +93,24 @@ void launch_mode(RowsParams p, int64_t pairs, hipStream_t s) {
     hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, NT, NW, D>), grid, block, 0, s, p);
 }
 
+template <int DT, int MODE, int BM, int BN, int S>
+void launch_wide(RowsParams p, int64_t pairs, hipStream_t s) {
+    p.n_blocks = static_cast<int>(cdiv(p.N, MODE == rows::kUp ? BN / 2 : BN));
+    const int64_t tiles = std::min<int64_t>(p.local, pairs) + pairs / BM;
+    const int64_t items = cdiv(p.n_blocks, 8) * 8 * tiles;
+    const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(rows::kWideThreads);
+    hipLaunchKernelGGL((rows::wide_kernel<DT, MODE, BM, BN, S>), grid, block, 0, s, p);
+}
+
 template <int DT, int MODE>
 void launch_rows(const RowsParams& p, int64_t tokens, int64_t pairs, int64_t experts, hipStream_t s) {
     // a token chooses an expert once, so no expert has more rows than there are tokens
     if (tokens <= 4) launch_mode<DT, MODE, 1>(p, pairs, s);
     else if (tokens <= 8) launch_mode<DT, MODE, 2>(p, pairs, s);
     else if (tokens <= 16 || pairs <= 10 * experts) launch_mode<DT, MODE, 4>(p, pairs, s);
-    else launch_mode<DT, MODE, 8>(p, pairs, s);
+    else if (pairs <= 32 * experts) launch_mode<DT, MODE, 8>(p, pairs, s);
+    else if (pairs <= 64 * experts) launch_wide<DT, MODE, 64, 128, 4>(p, pairs, s);
+    else launch_wide<DT, MODE, 128, 128, 4>(p, pairs, s);
 }
 
 template <int DT>

@@ -6,6 +6,7 @@
 
 #include "nmm_internal.h"
 #include "nt_rows.h"
+#include "nt_wide.h"
 
 namespace nmm {
 namespace {
@@ -33,12 +34,21 @@ void launch_nt(const RowsParams& p, hipStream_t s) {
     else launch_rows<DT, XR, 1>(p, s);
 }
 
+template <int DT, int BM, int BN, int S>
+void launch_wide(RowsParams p, hipStream_t s) {
+    p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? BN / 2 : BN));
+    const int64_t items = cdiv(p.n_blocks, 8) * 8 * cdiv(p.M, BM);
+    const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(rows::kWideThreads);
+    hipLaunchKernelGGL((rows::wide_kernel<DT, rows::kDense, BM, BN, S>), grid, block, 0, s, p);
+}
+
 template <int DT>
 void launch(const RowsParams& p, hipStream_t s) {
     if (p.M <= 4) launch_nt<DT, 1>(p, s);
     else if (p.M <= 8) launch_nt<DT, 2>(p, s);
     else if (p.M <= 16) launch_nt<DT, 4>(p, s);
-    else launch_nt<DT, 8>(p, s);
+    else if (p.M <= 32) launch_nt<DT, 8>(p, s);
+    else launch_wide<DT, 64, 64, 4>(p, s);
 }
 
 }  // namespace
