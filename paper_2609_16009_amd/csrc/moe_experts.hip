@@ -82,35 +82,39 @@ nmm_status plan_ffn(const nmm_moe_ffn& a, FfnPlan* q) {
     return NMM_OK;
 }
 
-template <int DT, int MODE, int XR>
-void launch_mode(RowsParams p, int64_t pairs, hipStream_t s) {
-    constexpr int NT = 2, NW = 4, D = 2;
-    p.n_blocks = static_cast<int>(cdiv(p.N, MODE == rows::kUp ? 16 : 16 * NT));
-    // tiles of rows: a cut one per expert that has pairs, and whole ones
-    const int64_t tiles = std::min<int64_t>(p.local, pairs) + pairs / (4 * XR);
-    const int64_t items = cdiv(p.n_blocks, 8) * 8 * tiles;
-    const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(64 * NW);
-    hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, NT, NW, D>), grid, block, 0, s, p);
+// Workgroups of a launch whose tiles have `rows` rows of x: a cut tile per expert that has pairs, and whole ones.
+uint32_t grid_of(const RowsParams& p, int64_t pairs, int64_t rows) {
+    const int64_t tiles = std::min<int64_t>(p.local, pairs) + pairs / rows;
+    return static_cast<uint32_t>(std::min<int64_t>(cdiv(p.n_blocks, 8) * 8 * tiles, kGridMost));
 }
 
-template <int DT, int MODE, int BM, int BN, int S>
+// 32 rows of the weight and two waves a workgroup, of which three share a CU: one token's eight experts of 64 117 us (130 with four
+// waves, whose workgroups have a CU each).
+template <int DT, int MODE, int XR>
+void launch_few(RowsParams p, int64_t pairs, hipStream_t s) {
+    p.n_blocks = static_cast<int>(cdiv(p.N, MODE == rows::kUp ? 16 : 32));
+    hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, 2, 2, 2>), dim3(grid_of(p, pairs, 4 * XR)), dim3(128), 0, s, p);
+}
+
+template <int DT, int MODE, int BM>
 void launch_wide(RowsParams p, int64_t pairs, hipStream_t s) {
+    constexpr int BN = 128;
     p.n_blocks = static_cast<int>(cdiv(p.N, MODE == rows::kUp ? BN / 2 : BN));
-    const int64_t tiles = std::min<int64_t>(p.local, pairs) + pairs / BM;
-    const int64_t items = cdiv(p.n_blocks, 8) * 8 * tiles;
-    const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(rows::kWideThreads);
-    hipLaunchKernelGGL((rows::wide_kernel<DT, MODE, BM, BN, S>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((rows::wide_kernel<DT, MODE, BM, BN, 3>), dim3(grid_of(p, pairs, BM)), dim3(rows::kWideThreads), 0, s, p);
 }
 
 template <int DT, int MODE>
 void launch_rows(const RowsParams& p, int64_t tokens, int64_t pairs, int64_t experts, hipStream_t s) {
-    // a token chooses an expert once, so no expert has more rows than there are tokens
-    if (tokens <= 4) launch_mode<DT, MODE, 1>(p, pairs, s);
-    else if (tokens <= 8) launch_mode<DT, MODE, 2>(p, pairs, s);
-    else if (tokens <= 16 || pairs <= 10 * experts) launch_mode<DT, MODE, 4>(p, pairs, s);
-    else if (pairs <= 32 * experts) launch_mode<DT, MODE, 8>(p, pairs, s);
-    else if (pairs <= 64 * experts) launch_wide<DT, MODE, 64, 128, 4>(p, pairs, s);
-    else launch_wide<DT, MODE, 128, 128, 4>(p, pairs, s);
+    // A token chooses an expert once, so few tokens say how many rows an expert has at most.  With more, tiles hold about twice
+    // the rows that experts have on average, so that nearly all read their weights once: 16 experts of 7168 and 2048, 16 rows
+    // each 249 us in tiles of 64 (257 of 128), 64 rows 293 in tiles of 128 (310 of 64), 128 rows 360 of 256 (393 of 128);
+    // 64 experts of 8 rows 916 in tiles of 16 (930 of 64).
+    if (tokens <= 4) launch_few<DT, MODE, 1>(p, pairs, s);
+    else if (tokens <= 8) launch_few<DT, MODE, 2>(p, pairs, s);
+    else if (tokens <= 16 || pairs <= 10 * experts) launch_few<DT, MODE, 4>(p, pairs, s);
+    else if (pairs <= 40 * experts) launch_wide<DT, MODE, 64>(p, pairs, s);
+    else if (pairs <= 96 * experts) launch_wide<DT, MODE, 128>(p, pairs, s);
+    else launch_wide<DT, MODE, 256>(p, pairs, s);
 }
 
 template <int DT>
@@ -185,6 +189,9 @@ nmm_status nmm_moe_experts(const nmm_moe_ffn* ffn, void* workspace, size_t works
     up.offsets = down.offsets = a.offsets + a.first;
     up.pairs = down.pairs = a.pairs;
     up.act = a.act;
+    up.ks = down.ks = 1;
+    up.rot = rows::rotation(a.ldw1);
+    down.rot = rows::rotation(a.ldw2);
     if (a.local > 0) {
         uint16_t* const h = reinterpret_cast<uint16_t*>(ws + kTicketBytes);
         float* const part = reinterpret_cast<float*>(ws + q.part_at);

@@ -15,14 +15,40 @@ using rows::RowsParams;
 
 constexpr int64_t kLim = int64_t(1) << 31;
 constexpr int kGridMost = 2048;            // workgroups: more items than that are taken in turns
+constexpr int kCus = 256;
+constexpr int kCols = 128;                 // rows of the weight a tile of wide_kernel
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-template <int DT, int XR, int NT>
+struct ActPlan {
+    int rows = 0;                // of x a tile: 4, 8, 16, 32 (rows_kernel) or 64, 128 (wide_kernel)
+    int ks = 1, slice_steps = 0; // slices of K, slots of each
+    size_t ws_bytes = 0;
+};
+
+// Up to 32 rows of x the weight's rows are dealt to workgroups in 16s where that is one a CU at most, else in 32s (launch_nt).  More
+// rows take tiles of 64 or 128 rows of x and 128 of the weight, and K is cut into slices, an XCD's each, while that leaves
+// at most a workgroup per CU and four slots a slice: 256 rows x 7168 x 2 x 2048 75 us whole, 32 in four slices; 128 x 16384 x 7168
+// 60 in four slices, 80 whole.
+ActPlan plan_act(int64_t M, int64_t K, int64_t N, bool gated) {
+    ActPlan q;
+    if (M <= 32) {
+        q.rows = M <= 4 ? 4 : M <= 8 ? 8 : M <= 16 ? 16 : 32;
+        return q;
+    }
+    const int64_t steps = cdiv(K, rows::kWideK);
+    q.rows = M <= 64 ? 64 : 128;
+    const int64_t tiles = cdiv(M, q.rows) * cdiv(N, gated ? kCols / 2 : kCols);
+    while (q.ks < 8 && tiles * q.ks * 2 <= kCus && steps >= q.ks * 8) q.ks *= 2;
+    q.slice_steps = static_cast<int>(std::max<int64_t>(1, cdiv(steps, q.ks)));
+    if (q.ks > 1) q.ws_bytes = size_t(kTicketBytes) + size_t(q.ks) * M * cdiv(N, 4) * 4 * (gated ? 2 : 1) * 4;
+    return q;
+}
+
+template <int DT, int XR, int NT, int NW, int D>
 void launch_rows(RowsParams p, hipStream_t s) {
-    constexpr int NW = 4, D = NT == 1 && XR < 4 ? 3 : 2;
-    p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? 16 : 16 * NT));
+    p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? 8 * NT : 16 * NT));
     const int64_t items = cdiv(p.n_blocks, 8) * 8 * cdiv(p.M, 4 * XR);
     const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(64 * NW);
     hipLaunchKernelGGL((rows::rows_kernel<DT, rows::kDense, XR, NT, NW, D>), grid, block, 0, s, p);
@@ -30,25 +56,35 @@ void launch_rows(RowsParams p, hipStream_t s) {
 
 template <int DT, int XR>
 void launch_nt(const RowsParams& p, hipStream_t s) {
-    if (p.gated || XR >= 4) launch_rows<DT, XR, 2>(p, s);
-    else launch_rows<DT, XR, 1>(p, s);
+    // 16 rows of the weight a workgroup, its four waves sharing K, while every one finds a CU of its own (gated, one row x 7168 x 2 x 2048
+    // 12.0 us against 14.4 in 32s; 32 x 4096 x 4096 13.9 and 15.7); else 32 rows and two waves, so that three workgroups share a
+    // CU (32 x 16384 x 7168 45.2 us against 58.8, one row x 7168 x 2 x 8192 37.8 against 37.2)
+    const int64_t rows16 = cdiv(p.gated ? 2 * int64_t(p.N) : p.N, 16);
+    if (rows16 <= kCus) launch_rows<DT, XR, 1, 4, 2>(p, s);
+    else launch_rows<DT, XR, 2, 2, 2>(p, s);
 }
 
-template <int DT, int BM, int BN, int S>
+template <int DT, int BM>
 void launch_wide(RowsParams p, hipStream_t s) {
-    p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? BN / 2 : BN));
-    const int64_t items = cdiv(p.n_blocks, 8) * 8 * cdiv(p.M, BM);
+    p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? kCols / 2 : kCols));
+    const int64_t items = cdiv(p.n_blocks, 8 / p.ks) * 8 * cdiv(p.M, BM);
     const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(rows::kWideThreads);
-    hipLaunchKernelGGL((rows::wide_kernel<DT, rows::kDense, BM, BN, S>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((rows::wide_kernel<DT, rows::kDense, BM, kCols, 3>), grid, block, 0, s, p);
+    if (p.ks == 1) return;
+    const dim3 all(static_cast<uint32_t>(cdiv(p.M * cdiv(p.N, 4), rows::kFinishThreads)));
+    hipLaunchKernelGGL((rows::finish_kernel<DT>), all, dim3(rows::kFinishThreads), 0, s, p);
 }
 
 template <int DT>
-void launch(const RowsParams& p, hipStream_t s) {
-    if (p.M <= 4) launch_nt<DT, 1>(p, s);
-    else if (p.M <= 8) launch_nt<DT, 2>(p, s);
-    else if (p.M <= 16) launch_nt<DT, 4>(p, s);
-    else if (p.M <= 32) launch_nt<DT, 8>(p, s);
-    else launch_wide<DT, 64, 64, 4>(p, s);
+void launch(const RowsParams& p, const ActPlan& q, hipStream_t s) {
+    switch (q.rows) {
+        case 4: return launch_nt<DT, 1>(p, s);
+        case 8: return launch_nt<DT, 2>(p, s);
+        case 16: return launch_nt<DT, 4>(p, s);
+        case 32: return launch_nt<DT, 8>(p, s);
+        case 64: return launch_wide<DT, 64>(p, s);
+        default: return launch_wide<DT, 128>(p, s);
+    }
 }
 
 }  // namespace
@@ -68,9 +104,14 @@ using namespace nmm;
 
 extern "C" {
 
-size_t nmm_gemv_nt_act_workspace_size(const nmm_nt_act*) { return 0; }
+size_t nmm_gemv_nt_act_workspace_size(const nmm_nt_act* product) {
+    if (!product || product->M <= 0 || product->K <= 0 || product->N <= 0 || product->M >= kLim || product->K >= kLim ||
+        product->N >= kLim)
+        return 0;
+    return plan_act(product->M, product->K, product->N, product->gated != 0).ws_bytes;
+}
 
-nmm_status nmm_gemv_nt_act(const nmm_nt_act* product, void*, size_t, void* stream) {
+nmm_status nmm_gemv_nt_act(const nmm_nt_act* product, void* workspace, size_t workspace_bytes, void* stream) {
     if (!product) return NMM_ERR_NULL;
     const nmm_nt_act& a = *product;
     if (a.dt != NMM_F16 && a.dt != NMM_BF16) return NMM_ERR_DTYPE;
@@ -100,7 +141,17 @@ nmm_status nmm_gemv_nt_act(const nmm_nt_act* product, void*, size_t, void* strea
     if (rows_overlap(a.residual, 2 * a.ldr, 2 * a.N, a.y_f32, 4 * a.ldyf, 4 * a.N, a.M) ||
         rows_overlap(a.y, 2 * a.ldy, 2 * a.N, a.y_f32, 4 * a.ldyf, 4 * a.N, a.M))
         return NMM_ERR_ARG;
+    const ActPlan q = plan_act(a.M, a.K, a.N, a.gated != 0);
+    const nmm_status st = validate_workspace(workspace, workspace_bytes, q.ws_bytes);
+    if (st != NMM_OK) return st;
     RowsParams p{};
+    p.ks = q.ks;
+    p.slice_steps = q.slice_steps;
+    if (q.ks > 1) {
+        p.ld_part = cdiv(a.N, 4) * 4 * (a.gated ? 2 : 1);
+        p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kTicketBytes);
+    }
+    p.rot = rows::rotation(a.ldwt);
     p.x = static_cast<const uint16_t*>(a.x);
     if (a.K > 0) {             // (0: extents of nothing)
         p.ldx = a.ldx;
@@ -121,8 +172,8 @@ nmm_status nmm_gemv_nt_act(const nmm_nt_act* product, void*, size_t, void* strea
     p.yf = a.y_f32;
     p.ldyf = a.ldyf;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (a.dt == NMM_BF16) launch<NMM_BF16>(p, s);
-    else launch<NMM_F16>(p, s);
+    if (a.dt == NMM_BF16) launch<NMM_BF16>(p, q, s);
+    else launch<NMM_F16>(p, q, s);
     return hipGetLastError() == hipSuccess ? NMM_OK : NMM_ERR_HIP;
 }
 

@@ -46,7 +46,16 @@ struct RowsParams {
     const int32_t* offsets;      // those of the first expert here
     const int32_t* pairs;
     int local, top_k;
+    int ks, slice_steps;         // wide tiles of kDense: K in ks slices of slice_steps slots
+    float* part;                 // their sums: [ks][M][ld_part], a gate's columns, then those that it multiplies
+    int64_t ld_part;
+    int rot;                     // rounds by which the next block of columns starts its walk over K later
 };
+
+// Rows of the weight a multiple of 4 KB apart meet in few of the memory's channels, as all workgroups are at about the same k:
+// there the next block of columns starts its walk over K a round later (16 experts of 2048 x 7168, 16 rows each: 114 -> 94 us; 32 x
+// 16384 x 7168: 48 -> 45).  Elsewhere it only takes from L2 what workgroups at the same k share (7168 x 2 x 2048: 250 -> 259 us).
+inline int rotation(int64_t ld) { return ld * 2 % 4096 == 0 ? 1 : 0; }
 
 __device__ __forceinline__ float activate(float z, int act) {
     switch (act) {
@@ -163,11 +172,20 @@ struct Item {
     int e, first, m0, mrows, nb;      // first: the expert's first pair in the order by experts
 };
 
-// Item idx of this XCD (false: none).  The row tiles over the same weight rows follow each other, so the second one finds
-// them in the XCD's L2.
+// Blocks of columns that an XCD takes: every eighth, or where K is cut into 2, 4 or 8 slices every fourth, second or all of them
+// in one slice (xcd % ks).
+__device__ __forceinline__ int64_t blocks_of(const RowsParams& p) {
+    const int share = 8 / p.ks;
+    return (int64_t(p.n_blocks) + share - 1) / share;
+}
+
+// Item idx of this XCD (false: none): its blocks of columns of all experts, so that each XCD has the same share of every
+// expert's rows.  (An eighth of the experts each reads x into one L2 instead of eight, 0.95 instead of 1.12 GB for 16 experts of 128 rows on
+// average, but the XCD with the fullest ones ends last: 253 instead of 228 us.)  The row tiles over the same weight rows
+// follow each other, so the second one finds them in the XCD's L2.
 template <int MODE, int TM>
 __device__ __forceinline__ bool item_of(const RowsParams& p, const int* starts, int64_t idx, int xcd, Item* it) {
-    const int64_t nb8 = (p.n_blocks + 7) >> 3;
+    const int64_t nb8 = blocks_of(p);
     int lo = 0, tiles;
     int64_t rem = idx;
     if constexpr (MODE == kDense) {
@@ -190,7 +208,7 @@ __device__ __forceinline__ bool item_of(const RowsParams& p, const int* starts, 
         it->first = __builtin_amdgcn_readfirstlane(min(max(p.offsets[lo], 0), p.M));
     }
     const int nbi = static_cast<int>(rem / tiles);
-    it->nb = 8 * nbi + xcd;
+    it->nb = 8 / p.ks * nbi + xcd / p.ks;
     it->m0 = static_cast<int>(rem - int64_t(nbi) * tiles) * TM;
     const int count =
         MODE == kDense ? p.M : __builtin_amdgcn_readfirstlane(min(max(p.offsets[lo + 1], 0), p.M)) - it->first;
@@ -215,10 +233,10 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, j = lane & 15;
     const bool gated = MODE == kUp || (MODE == kDense && p.gated);
-    const int n_step = gated ? 16 : 16 * NT;
+    const int n_step = gated ? 8 * NT : 16 * NT;
 
     if constexpr (MODE != kDense) scan_tiles<TM, 64 * NW>(p, starts);
-    const int64_t nb8 = (p.n_blocks + 7) >> 3;
+    const int64_t nb8 = blocks_of(p);
     const int64_t total = (MODE == kDense ? (int64_t(p.M) + TM - 1) / TM : int64_t(__builtin_amdgcn_readfirstlane(starts[p.local]))) * nb8;
     const int groups = (p.K + kMfmaNtGroup - 1) / kMfmaNtGroup;
     const int rounds = (groups + NW - 1) / NW;       // the same for every wave; groups past K are zeros
@@ -254,8 +272,9 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
             const int c = j ^ (r & 15);
             if (q < 4) kc[q] = 8 * c;
             if (is_w) {
-                const int n = gated ? n0 + (r & 15) : n0 + r;
-                const int64_t row = gated && r >= 16 ? int64_t(p.N) + n : n;
+                constexpr int kHalf = 8 * NT;         // gated: the gate's rows, then as many that they are multiplied with
+                const int n = gated ? n0 + r % kHalf : n0 + r;
+                const int64_t row = gated && r >= kHalf ? int64_t(p.N) + n : n;
                 off[q] = n < p.N ? uint32_t(row * p.row_bytes) + 16u * c : kOutOfRange;
             } else {
                 bool ok = r < it.mrows;
@@ -280,7 +299,8 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_void*)(slot + q * kQuad), 16, o, 0, 0, 0);
             }
         };
-        auto group_of = [&](int r) { return r < rounds ? wave + r * NW : groups; };
+        const int start = static_cast<int>(unsigned(it.nb) * unsigned(p.rot) % unsigned(max(rounds, 1)));
+        auto group_of = [&](int r) { return r < rounds ? wave + (r + start < rounds ? r + start : r + start - rounds) * NW : groups; };
         // (the loads counted below are the ring's alone)
         __builtin_amdgcn_s_waitcnt(0);
 #pragma unroll
@@ -354,7 +374,7 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 a += *reinterpret_cast<const f32x4*>(src + w * NT * MT * kTileFloats);
-                if (NT > 1 && gated) b += *reinterpret_cast<const f32x4*>(src + (w * NT + 1) * MT * kTileFloats);
+                if (gated) b += *reinterpret_cast<const f32x4*>(src + (NT > 1 ? (w * NT + 1) * MT * kTileFloats : w * MT * kTileFloats + 8));
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {

@@ -1,13 +1,16 @@
 // The products of nt_rows.h for many rows of x a tile (device code).
 //
-// A workgroup of 8 waves owns a tile of BM rows of x and BN rows of the weight.  Slots of 64 k of both lie in a ring of S in
-// LDS, filled by LDS-direct loads of 8 rows x 128 bytes, S - 1 slots ahead, with one barrier a slot; a wave multiplies its
-// part of the tile with v_mfma_f32_16x16x32.  Chunk c of row r sits at place c ^ (r / 2 % 8) of its 128 bytes: LDS serves 256
-// bytes a cycle, the 16 rows of a fragment's quarter wave, which then lie in 16 different places.
+// A workgroup of 4 waves owns a tile of up to BM rows of x and BN rows of the weight.  Slots of 64 k of both lie in a ring of S in
+// LDS, filled by LDS-direct loads of 8 rows x 128 bytes, up to S slots ahead; a wave multiplies its part of the tile with
+// v_mfma_f32_16x16x32.  Chunk c of row r sits at place c ^ (r / 2 % 8) of its 128 bytes, so that the 16 rows of a fragment's
+// quarter wave lie in 16 different places (no bank conflict counted).
 // The weight is the A operand and x the B operand: a lane ends with four consecutive n of one m.  Where a gate
-// multiplies, a wave's rows of the weight are half the gate's and half those that they are multiplied with.
-// Two waves a SIMD, so that one reads fragments while the other's are multiplied: the reads wait for themselves (see
-// read_tiles), as the compiler makes a read of LDS wait for loads into other slots too.
+// multiplies, a wave's rows of the weight are half the gate's and half those that they are multiplied with.  The 16-row tiles of x are
+// dealt to the waves in turn, so that a tile with fewer rows than BM costs what its own rows do.
+//
+// LDS gives a CU about 110 bytes a cycle, and a wave's part of 64 x 64 reads as long as it multiplies, so the two run beside each
+// other: while one half of a slot is multiplied the next one's fragments are read, and the one barrier a slot lies between the
+// halves.  The loads are written as asm: the compiler makes a read of LDS wait for every LDS-direct load that it knows of.
 #pragma once
 
 #include "nt_rows.h"
@@ -21,39 +24,38 @@ constexpr int kWideK = 64;                      // k of a slot
 constexpr int kWideRow = 2 * kWideK;            // bytes of a row in a slot
 constexpr int kWideTile = 16 * kWideRow;        // and of 16 rows
 
+// At most N of this wave's loads are outstanding, none of its LDS reads; then every wave's.
 template <int N>
-__device__ __forceinline__ void wait_loads() {
+__device__ __forceinline__ void slot_barrier() {
     static_assert(N >= 0 && N < 64, "vmcnt holds 6 bits");
-    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
 }
 
-// The fragments of two tiles of the weight (at wa and kWideTile behind it) and of MT tiles of x, complete when this returns.
-template <int MT>
-__device__ __forceinline__ void read_tiles(i32x4 (&w)[2], i32x4 (&x)[MT], uint32_t wa, uint32_t xa) {
-    static_assert(MT == 1 || MT == 2 || MT == 4, "tiles of x");
-    if constexpr (MT == 1)
-        asm volatile("ds_read_b128 %0, %3\n\tds_read_b128 %2, %4\n\tds_read_b128 %1, %3 offset:%5\n\ts_waitcnt lgkmcnt(0)"
-                     : "=&v"(w[0]), "=&v"(w[1]), "=&v"(x[0]) : "v"(wa), "v"(xa), "n"(kWideTile) : "memory");
-    else if constexpr (MT == 2)
-        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %2, %5\n\tds_read_b128 %1, %4 offset:%6\n\t"
-                     "ds_read_b128 %3, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
-                     : "=&v"(w[0]), "=&v"(w[1]), "=&v"(x[0]), "=&v"(x[1]) : "v"(wa), "v"(xa), "n"(kWideTile) : "memory");
-    else
-        asm volatile("ds_read_b128 %0, %6\n\tds_read_b128 %2, %7\n\tds_read_b128 %1, %6 offset:%8\n\t"
-                     "ds_read_b128 %3, %7 offset:%8\n\tds_read_b128 %4, %7 offset:%9\n\tds_read_b128 %5, %7 offset:%10\n\t"
-                     "s_waitcnt lgkmcnt(0)"
-                     : "=&v"(w[0]), "=&v"(w[1]), "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-                     : "v"(wa), "v"(xa), "n"(kWideTile), "n"(2 * kWideTile), "n"(3 * kWideTile) : "memory");
+// 64 lanes x 16 bytes to LDS from `lds` on (the same in all lanes), lane l's behind lane l - 1's, from byte `offset` of the buffer.
+// Not said to touch memory, so that reads of other slots may move past it: what orders it is slot_barrier.
+// (m0 is reserved: nothing else in these kernels holds a value in it.)
+__device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t lds, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(lds), "v"(offset), "s"(rsrc));
+}
+
+// The buffer resource as its four words (address, no stride, extent, raw).
+__device__ __forceinline__ i32x4 rsrc_words(const void* base, uint32_t extent) {
+    const uint64_t a = reinterpret_cast<uint64_t>(base);
+    i32x4 r{int(uint32_t(a)), int(uint32_t(a >> 32) & 0xFFFFu), int(extent), kRsrcWord3};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
+    return r;
 }
 
 template <int DT, int MODE, int BM, int BN, int S>
 __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) {
-    constexpr int NT = 2, WN = BN / 16 / NT, WM = kWideWaves / WN;       // waves along n and m; a wave's 16-row tiles
+    constexpr int NT = BM >= 256 ? 4 : 2, WN = BN / 16 / NT, WM = kWideWaves / WN;   // a wave's tiles; waves along n and m
     constexpr int MT = BM / WM / 16;
-    constexpr int kLoads = (BM + BN) / 8 / kWideWaves;                   // loads of a slot per wave
+    constexpr int LW = BN / 64, kLoads = LW + BM / 64;                   // loads of a slot per wave, the weight's first
     constexpr int kSlot = (BM + BN) * kWideRow;
-    static_assert(WM * WN == kWideWaves && MT * WM * 16 == BM && kLoads * 8 * kWideWaves == BM + BN && BN % 64 == 0 && S >= 3,
-                  "whole tiles and loads a wave");
+    static_assert(MT * WM * 16 == BM && NT * WN * 16 == BN && NT % 2 == 0 && S >= 3, "whole tiles, gate and up");
+    constexpr int kPitch = BN + 4;                                       // floats of a row of sums
+    static_assert(BM * kPitch * 4 <= S * kSlot, "the sums fit the ring");
     __shared__ __attribute__((aligned(256))) uint8_t ring[S * kSlot];
     __shared__ int starts[MODE == kDense ? 1 : kMaxExperts + 1];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -64,34 +66,37 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
     const int n_step = gated ? BN / 2 : BN;
 
     if constexpr (MODE != kDense) scan_tiles<BM, kWideThreads>(p, starts);
-    const int64_t nb8 = (p.n_blocks + 7) >> 3;
+    const int64_t nb8 = blocks_of(p);
     const int64_t total = (MODE == kDense ? (int64_t(p.M) + BM - 1) / BM : int64_t(__builtin_amdgcn_readfirstlane(starts[p.local]))) * nb8;
-    const int steps = (p.K + kWideK - 1) / kWideK;
+    const int all_steps = (p.K + kWideK - 1) / kWideK;
     // the lane's chunk of a load: the same of every load of its wave (they are 64 rows apart)
     const int chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
     // fragments: row j of a tile, chunk g; chunk 4 + g lies 64 bytes away
-    const uint32_t base = uint32_t(reinterpret_cast<uintptr_t>((lds_void*)ring)) + j * kWideRow + ((g ^ (j >> 1)) << 4);
-    const uint32_t wa = base + wn * NT * kWideTile, xa = base + BN * kWideRow + wm * MT * kWideTile;
+    const int f0 = j * kWideRow + ((g ^ (j >> 1)) << 4);
+    const int wa = f0 + wn * NT * kWideTile, xa = f0 + BN * kWideRow + wm * kWideTile;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>((lds_void*)ring))) + 8 * wave * kWideRow;
 
     for (int64_t idx = blockIdx.x >> 3; idx < total; idx += gridDim.x >> 3) {
         Item it;
         if (!item_of<MODE, BM>(p, starts, idx, blockIdx.x & 7, &it)) continue;
+        // a slice of K is an XCD's, whose L2 then holds that slice of x alone
+        const int slice = MODE == kDense ? int(blockIdx.x & 7) % p.ks : 0;
+        const int first_step = MODE == kDense ? slice * p.slice_steps : 0;
+        const int steps = MODE == kDense ? min(all_steps - first_step, p.slice_steps) : all_steps;
         const int n0 = it.nb * n_step;
-        const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint8_t*>(p.w + it.e * p.w_stride), (short)0, (int)p.w_extent, kRsrcWord3);
+        const i32x4 wr = rsrc_words(p.w + it.e * p.w_stride, p.w_extent);
         const uint16_t* xb = p.x;
         uint32_t x_extent = p.x_extent;
         if constexpr (MODE != kUp) {
             xb += (int64_t(it.first) + it.m0) * p.ldx;
             x_extent = uint32_t((int64_t(it.mrows - 1) * p.ldx + (p.K + 7) / 8 * 8) * 2);
         }
-        const __amdgpu_buffer_rsrc_t xr =
-            __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(xb), (short)0, (int)x_extent, kRsrcWord3);
+        const i32x4 xr = rsrc_words(xb, x_extent);
         uint32_t off[kLoads];      // byte offset of the lane's chunk in slot 0; out of range where there is none
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r = 8 * (wave + kWideWaves * i) + (lane >> 3);
-            if (64 * i < BN) {     // (a row of the weight for every wave)
+            if (i < LW) {     // (a row of the weight for every wave)
                 constexpr int kWaveRows = BN / WN;
                 int64_t row = n0 + r;
                 bool ok = row < p.N;
@@ -113,17 +118,16 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
                 off[i] = ok ? uint32_t(row * p.ldx * 2) + 16u * chunk : kOutOfRange;
             }
         }
-        auto load_slot = [&](int step, int slot) {
+        // (N: how many of the loads the tile's rows need)
+        auto load_slot = [&](auto nc, int step, int slot) {
+            constexpr int N = decltype(nc)::value;
             const int kg = step * kWideK;
             // past K out of range, which the top bit says (extents are below 2^31)
             const uint32_t past = kg + 8 * chunk < p.K ? 0u : kOutOfRange;
+            const uint32_t to = ring_at + slot * kSlot;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const uint32_t o = (off[i] + uint32_t(kg) * 2u) | past;
-                uint8_t* const dst = ring + slot * kSlot + 8 * (wave + kWideWaves * i) * kWideRow;
-                if (64 * i < BN) __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void*)dst, 16, o, 0, 0, 0);
-                else __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_void*)dst, 16, o, 0, 0, 0);
-            }
+            for (int i = 0; i < N; ++i)
+                load_to_lds(i < LW ? wr : xr, to + 64 * i * kWideRow, (off[i] + uint32_t(kg) * 2u) | past);
         };
         f32x4 sum[NT][MT];
 #pragma unroll
@@ -132,67 +136,121 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
             for (int m = 0; m < MT; ++m) sum[t][m] = f32x4{0.f, 0.f, 0.f, 0.f};
 
         // (the loads counted below are the ring's alone; its slots are free)
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
+        slot_barrier<0>();
+        // Round r of the walk over K, which starts elsewhere for the next block of columns: rows that lie a multiple of some KB apart
+        // otherwise meet in a few of L2's channels, as all workgroups are at about the same k (rounds past the last: nothing).
+        const int start = static_cast<int>(unsigned(it.nb) * unsigned(p.rot) % unsigned(max(steps, 1)));
+        auto step_of = [&](int r) { return r >= steps ? all_steps : first_step + (r + start < steps ? r + start : r + start - steps); };
+        // M of the wave's MT tiles of x; CUT: K ends within a chunk
+        auto run = [&](auto mc, auto cutc) {
+            constexpr int M = decltype(mc)::value;
+            constexpr bool CUT = decltype(cutc)::value;
+            constexpr std::integral_constant<int, LW + (16 * WM * M + 63) / 64> n_loads;
+            struct Half {
+                i32x4 w[NT], x[M];
+            };
+            auto read = [&](Half& f, int slot, int h) {
+                const uint8_t* const at = ring + slot * kSlot;
 #pragma unroll
-        for (int s = 0; s < S - 1; ++s) load_slot(s, s);
-        int slot = 0;
-        for (int step = 0; step < steps; ++step) {
-            // this wave's loads of the slot have landed, then every wave's; all are done with the slot that is filled next
-            wait_loads<(S - 2) * kLoads>();
-            asm volatile("s_barrier" ::: "memory");
-            load_slot(step + S - 1, slot == 0 ? S - 1 : slot - 1);
-            const bool ragged = (step + 1) * kWideK > p.K && (p.K & 7);
+                for (int t = 0; t < NT; ++t) f.w[t] = *reinterpret_cast<const i32x4*>(at + (wa ^ (64 * h)) + t * kWideTile);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                i32x4 w[NT], x[MT];
-                read_tiles<MT>(w, x, (wa ^ (64u * h)) + slot * kSlot, (xa ^ (64u * h)) + slot * kSlot);
-                if (ragged) {      // clear what lies past K
+                for (int m = 0; m < M; ++m) f.x[m] = *reinterpret_cast<const i32x4*>(at + (xa ^ (64 * h)) + m * WM * kWideTile);
+            };
+            auto multiply = [&](Half& f, int step, int h) {
+                if constexpr (CUT) {      // clear what lies past K
                     const int left = p.K - (step * kWideK + 32 * h + 8 * g);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) w[t] = keep_first(w[t], left);
+                    for (int t = 0; t < NT; ++t) f.w[t] = keep_first(f.w[t], left);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) x[m] = keep_first(x[m], left);
+                    for (int m = 0; m < M; ++m) f.x[m] = keep_first(f.x[m], left);
                 }
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) sum[t][m] = mfma<DT>(w[t], x[m], sum[t][m]);
-            }
-            slot = slot == S - 1 ? 0 : slot + 1;
-        }
-
+                    for (int m = 0; m < M; ++m) sum[t][m] = mfma<DT>(f.w[t], f.x[m], sum[t][m]);
+            };
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int mr = (wm * MT + m) * 16 + j;
-            if (mr >= it.mrows) continue;
-            int64_t row = int64_t(it.first) + it.m0 + mr;
+            for (int s = 0; s < S; ++s) load_slot(n_loads, step_of(s), s);
+            slot_barrier<(S - 1) * n_loads.value>();
+            Half a, b;
+            read(a, 0, 0);
+            int slot = 0;
+            for (int r = 0; r < steps; ++r) {
+                const int step = step_of(r), next = slot == S - 1 ? 0 : slot + 1;
+                read(b, slot, 1);
+                multiply(a, step, 0);
+                // the next slot has landed, and all are done with this one
+                slot_barrier<(S - 2) * n_loads.value>();
+                load_slot(n_loads, step_of(r + S), slot);
+                read(a, next, 0);
+                multiply(b, step, 1);
+                slot = next;
+            }
+        };
+        constexpr int U = 1;
+        constexpr std::integral_constant<bool, false> whole;
+        if (p.K & 7) run(std::integral_constant<int, MT>{}, std::integral_constant<bool, true>{});
+        else if (MT <= U || it.mrows <= 16 * WM * U) run(std::integral_constant<int, U>{}, whole);
+        else if (MT <= 2 * U || it.mrows <= 32 * WM * U) run(std::integral_constant<int, MT < 2 * U ? MT : 2 * U>{}, whole);
+        else if (MT <= 3 * U || it.mrows <= 48 * WM * U) run(std::integral_constant<int, MT < 3 * U ? MT : 3 * U>{}, whole);
+        else run(std::integral_constant<int, MT>{}, whole);
+
+        // the sums through the ring's LDS, [m][row of the weight], so that rows of the result are written whole
+        slot_barrier<0>();
+        float* const tile = reinterpret_cast<float*>(ring);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+                *reinterpret_cast<f32x4*>(tile + ((wm + WM * m) * 16 + j) * kPitch + (wn * NT + t) * 16 + 4 * g) = sum[t][m];
+        slot_barrier<0>();
+        constexpr int kWaveRows = BN / WN;
+        const int quads = n_step / 4;
+        for (int o = tid; o < quads * it.mrows; o += kWideThreads) {
+            const int m = o / quads, c = (o - m * quads) * 4, n = n0 + c;
+            if (n >= p.N) continue;
+            const float* at = tile + m * kPitch;
+            at += gated ? c / (kWaveRows / 2) * kWaveRows + c % (kWaveRows / 2) : c;
+            const f32x4 v = *reinterpret_cast<const f32x4*>(at);
+            f32x4 v2{0.f, 0.f, 0.f, 0.f};
+            if (gated) v2 = *reinterpret_cast<const f32x4*>(at + kWaveRows / 2);
+            int64_t row = int64_t(it.first) + it.m0 + m;
             if constexpr (MODE == kDown) {
                 const int pair = p.pairs[row];
                 if (uint32_t(pair) >= uint32_t(p.M)) continue;
                 row = pair;
             }
-            auto finish = [&](int t, int n) {
-                float z[4], z2[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) z[i] = sum[t][m][i];
-                if (gated) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z2[i] = sum[t % (NT / 2) + NT / 2][m][i];
-                }
-                if (n < p.N) finish4<DT, MODE>(p, row, n, z, z2);
-            };
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (gated) {
-                    if (t < NT / 2) finish(t, n0 + (wn * (NT / 2) + t) * 16 + 4 * g);
-                } else {
-                    finish(t, n0 + (wn * NT + t) * 16 + 4 * g);
-                }
+            if (MODE == kDense && p.ks > 1) {              // a slice's sums: finish_kernel adds them
+                float* const part = p.part + (int64_t(slice) * p.M + row) * p.ld_part + n;
+                *reinterpret_cast<f32x4*>(part) = v;
+                if (gated) *reinterpret_cast<f32x4*>(part + p.ld_part / 2) = v2;
+                continue;
             }
+            float z[4] = {v[0], v[1], v[2], v[3]}, z2[4] = {v2[0], v2[1], v2[2], v2[3]};
+            finish4<DT, MODE>(p, row, n, z, z2);
         }
     }
-    __builtin_amdgcn_s_waitcnt(0);       // the ring's last loads into LDS have landed
+    slot_barrier<0>();       // the ring's last loads into LDS have landed
+}
+
+// The slices of K added in order, and what follows: four columns of a row a thread.
+constexpr int kFinishThreads = 256;
+template <int DT>
+__global__ __launch_bounds__(kFinishThreads) void finish_kernel(const RowsParams p) {
+    const int per_row = (p.N + 3) / 4;
+    const int64_t i = int64_t(blockIdx.x) * kFinishThreads + threadIdx.x;
+    const int64_t row = i / per_row;
+    const int n = static_cast<int>(i - row * per_row) * 4;
+    if (row >= p.M) return;
+    f32x4 a{0.f, 0.f, 0.f, 0.f}, b = a;
+    const float* part = p.part + row * p.ld_part + n;
+#pragma unroll 4
+    for (int q = 0; q < p.ks; ++q, part += int64_t(p.M) * p.ld_part) {
+        a += *reinterpret_cast<const f32x4*>(part);
+        if (p.gated) b += *reinterpret_cast<const f32x4*>(part + p.ld_part / 2);
+    }
+    float z[4] = {a[0], a[1], a[2], a[3]}, z2[4] = {b[0], b[1], b[2], b[3]};
+    finish4<DT, kDense>(p, row, n, z, z2);
 }
 
 }  // namespace rows
