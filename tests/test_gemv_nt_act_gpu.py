@@ -75,6 +75,20 @@ def test_integers_exact_at_odd_sizes(M, K, N):
     check(K + N, M, K, N, 0, True, torch.float16, True, bias=True, residual=True, pad=1)
 
 
+@pytest.mark.parametrize("M,K,N", [(33, 1024, 70), (64, 1031, 257), (65, 1500, 129), (128, 4099, 100), (129, 2048, 33), (200, 3000, 1000),
+                                   (300, 512, 2100), (1000, 600, 40), (5, 2048, 100), (20, 4096, 300), (2, 6144, 4100), (31, 2048, 8200)])
+def test_integers_exact_where_k_is_cut_or_walks_start_apart(M, K, N):
+    """K in one, two, four and eight slices, ending within a chunk of 8 and on one; rows of the weight 4 KB apart and not."""
+    check(M + K, M, K, N, 1, False, torch.bfloat16, True, bias=True, residual=M % 2 == 0)
+    check(M + N, M, K, N, 0, True, torch.float16, True, residual=M % 2 == 1)
+
+
+def test_one_workspace_for_every_size():
+    ws = nmm.Workspace()
+    for M, K, N in ((256, 2048, 300), (40, 1024, 100), (1, 512, 64), (128, 4096, 200), (300, 700, 30), (256, 2048, 300)):
+        check(M + K, M, K, N, 1, M % 3 == 0, torch.bfloat16, True, residual=True, workspace=ws)
+
+
 @pytest.mark.parametrize("act", range(5))
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
@@ -123,6 +137,16 @@ def test_a_value_that_is_not_finite_stays_in_its_row(M):
     keep = torch.ones_like(y, dtype=torch.bool)
     keep[hurt], keep[:, 5] = False, False
     assert torch.equal(y[keep], clean[keep]) and torch.isnan(y[hurt]).all()
+
+
+@pytest.mark.parametrize("M,K", [(70, 128), (200, 2048)])
+def test_residual_in_place_in_wide_tiles(M, K):
+    args, _ = make(M, M, K, 130, False, torch.bfloat16, False, True, True)
+    y = torch.zeros((M, 130), dtype=torch.bfloat16, device="cuda")
+    nmm.nmm_gemv_nt_act(args["x"], args["Wt"], y, act=4, bias=args["bias"], residual=args["residual"])
+    both = args["residual"].clone()
+    nmm.nmm_gemv_nt_act(args["x"], args["Wt"], both, act=4, bias=args["bias"], residual=both)
+    assert torch.equal(both, y)
 
 
 def test_residual_in_place_and_column_ranges():

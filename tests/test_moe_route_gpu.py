@@ -114,7 +114,7 @@ def test_masks():
     compare(out, logits, 4, SOFTMAX, mask=mask)
 
 
-@pytest.mark.parametrize("T,E,k", [(1023, 64, 8), (1024, 64, 8), (1025, 64, 8), (1026, 8, 8), (5000, 256, 2), (8192, 16, 1), (8193, 16, 1),
+@pytest.mark.parametrize("T,E,k", [(1023, 64, 8), (1024, 64, 8), (1025, 64, 8), (1026, 8, 8), (5000, 256, 2), (8192, 16, 1), (8193, 16, 1), (128, 1024, 8), (129, 1024, 8), (700, 1000, 8), (130, 100, 32),
                                    (20000, 20, 4)])
 def test_many_tokens(T, E, k):
     check(T, T, E, k, SIGMOID, bias=True, mask=T % 2 == 0, pad=3, renormalize=True)
@@ -135,6 +135,18 @@ def test_very_many_tokens_and_skew():
     assert torch.equal(out[2][1:].long(), torch.cumsum(torch.bincount(flat, minlength=E), 0)) and out[2][0] == 0
     p = torch.softmax(logits.double(), 1).gather(1, order)
     assert ((out[1].double() - p).abs() <= 2.0 ** -23 * p).all()
+
+
+def test_segments_longer_than_a_piece():
+    """More pairs a workgroup than it orders at once."""
+    T, E = 3000001, 8
+    logits = torch.randint(-3, 4, (T, E), device="cuda").float()
+    out = outputs(T, E, 1)
+    nmm.nmm_moe_route(logits, *out, score=SIGMOID)
+    order = torch.sort(logits, dim=1, descending=True, stable=True)[1][:, 0]
+    assert torch.equal(out[0][:, 0].long(), order)
+    assert torch.equal(out[3].long(), torch.sort(order, stable=True)[1])
+    assert torch.equal(out[2][1:].long(), torch.cumsum(torch.bincount(order, minlength=E), 0)) and out[2][0] == 0
 
 
 def test_no_tokens():
