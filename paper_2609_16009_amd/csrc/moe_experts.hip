@@ -88,10 +88,18 @@ uint32_t grid_of(const RowsParams& p, int64_t pairs, int64_t rows) {
     return static_cast<uint32_t>(std::min<int64_t>(cdiv(p.n_blocks, 8) * 8 * tiles, kGridMost));
 }
 
-// 32 rows of the weight and two waves a workgroup, of which three share a CU: one token's eight experts of 64 117 us (130 with four
-// waves, whose workgroups have a CU each).
+// 32 rows of the weight and two waves a workgroup, of which three share a CU: the eight experts of one token, W2 44.9 us (52.2 with four
+// waves, whose workgroups have a CU each).  Up to 8 rows of x and a K of eight groups for each of four waves W1 goes by 16 rows,
+// a gate's 8 and the 8 that it multiplies: 67.4 us of one token (73.0 in 32s), 41 of four experts of 4096 x 4096 (58); at 16 rows of x 439 and 432.
 template <int DT, int MODE, int XR>
 void launch_few(RowsParams p, int64_t pairs, hipStream_t s) {
+    if constexpr (MODE == rows::kUp && XR <= 2) {
+        if (p.K >= 4 * 8 * kMfmaNtGroup) {
+            p.n_blocks = static_cast<int>(cdiv(p.N, 8));
+            hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, 1, 4, 2>), dim3(grid_of(p, pairs, 4 * XR)), dim3(256), 0, s, p);
+            return;
+        }
+    }
     p.n_blocks = static_cast<int>(cdiv(p.N, MODE == rows::kUp ? 16 : 32));
     hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, 2, 2, 2>), dim3(grid_of(p, pairs, 4 * XR)), dim3(128), 0, s, p);
 }

@@ -225,7 +225,6 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
     constexpr int MT = XR > 4 ? 2 : 1;               // 16-row tiles of x
     constexpr int kLoads = 4 * NT + XR;              // loads of a group per wave
     constexpr int kSlot = kLoads * kQuad;            // LDS bytes of a group
-    static_assert(MODE != kUp || NT == 2, "gate and up rows");
     __shared__ __attribute__((aligned(256))) uint8_t smem[NW * D * kSlot];
     __shared__ __attribute__((aligned(16))) float red[NW * NT * MT * kTileFloats];
     __shared__ int starts[MODE == kDense ? 1 : kMaxExperts + 1];

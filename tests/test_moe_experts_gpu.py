@@ -97,7 +97,8 @@ def test_integers_exact_at_odd_sizes(hidden, inner, dt):
 
 
 @pytest.mark.parametrize("T,E,k,hidden,inner", [(20, 4, 2, 2048, 2048), (400, 2, 1, 72, 64), (400, 2, 1, 75, 67), (500, 3, 2, 64, 2048),
-                                                (64, 1024, 8, 128, 64), (600, 1024, 4, 64, 24), (1, 1024, 32, 64, 40), (700, 16, 2, 200, 88)])
+                                                (64, 1024, 8, 128, 64), (600, 1024, 4, 64, 24), (1, 1024, 32, 64, 40), (700, 16, 2, 200, 88), (3, 6, 2, 4096, 70),
+                                                (8, 5, 3, 4203, 33)])
 def test_integers_exact_in_every_tile(T, E, k, hidden, inner):
     """Tiles of 4 to 256 rows, as many experts as there may be, more items than workgroups, rows of the weights 4 KB apart."""
     for dt in (torch.bfloat16, torch.float16):
