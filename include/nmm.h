@@ -659,7 +659,7 @@ size_t nmm_gemv_nt_act_workspace_size(const nmm_nt_act* product);
  *   offsets      int32 [experts + 1];   pairs   int32 [tokens * top_k]: pairs[offsets[e] .. offsets[e + 1]) are the pairs
  *                t * top_k + i with chosen[t,i] = e, ascending; those behind offsets[experts] are left as they were.
  *   tokens       tokens * top_k < 2^26 (0: offsets are zeroed).
- * Deterministic.  Workspace: nmm_moe_route_workspace_size.
+ * No output may overlap an input or another output.  Deterministic.  Workspace: nmm_moe_route_workspace_size.
  */
 typedef enum { NMM_SCORE_SOFTMAX = 1, NMM_SCORE_SIGMOID = 2 } nmm_score;
 
@@ -690,7 +690,7 @@ size_t nmm_moe_route_workspace_size(const nmm_moe_router* router);
  *     y[t]    = dt(residual[t] + sum_i weights[t,i] (h[t,i] . W2[e]^T))            over the i whose expert is here
  * Sums are fp32; h is rounded to dt, the operand of the second product, and y once (nearest, ties to even).  The i of a token
  * are added in order; a token with none gets its residual, or zeros.  The weights of an expert are read once per
- * up to 128 of its rows, those of an expert that nobody chose not at all.
+ * up to 256 of its rows, those of an expert that nobody chose not at all.
  *   tokens, top_k, experts, first, local   tokens * top_k < 2^26, top_k 1 .. 32, experts 1 .. 1024,
  *                first >= 0, local >= 0, first + local <= experts.
  *   hidden, inner   > 0 (the sizes of x[t] and h[t,i]).

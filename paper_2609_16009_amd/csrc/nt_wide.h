@@ -1,6 +1,6 @@
 // The products of nt_rows.h for many rows of x a tile (device code).
 //
-// A workgroup of 4 waves owns a tile of up to BM rows of x and BN rows of the weight.  Slots of 64 k of both lie in a ring of S in
+// A workgroup of 8 waves owns a tile of up to BM rows of x and BN rows of the weight.  Slots of 64 k of both lie in a ring of S in
 // LDS, filled by LDS-direct loads of 8 rows x 128 bytes, up to S slots ahead; a wave multiplies its part of the tile with
 // v_mfma_f32_16x16x32.  Chunk c of row r sits at place c ^ (r / 2 % 8) of its 128 bytes, so that the 16 rows of a fragment's
 // quarter wave lie in 16 different places (no bank conflict counted).
@@ -8,9 +8,14 @@
 // multiplies, a wave's rows of the weight are half the gate's and half those that they are multiplied with.  The 16-row tiles of x are
 // dealt to the waves in turn, so that a tile with fewer rows than BM costs what its own rows do.
 //
-// LDS gives a CU about 110 bytes a cycle, and a wave's part of 64 x 64 reads as long as it multiplies, so the two run beside each
-// other: while one half of a slot is multiplied the next one's fragments are read, and the one barrier a slot lies between the
-// halves.  The loads are written as asm: the compiler makes a read of LDS wait for every LDS-direct load that it knows of.
+// Reading fragments (about 110 bytes a cycle and CU) takes as long as multiplying them, so the two run beside each other: while one
+// half of a slot is multiplied the next one's fragments are read, and the one barrier a slot lies between the halves.  The
+// loads are written as asm: the compiler makes a read of LDS wait for every LDS-direct load that it knows of.
+//
+// What bounds it: how fast a CU is given lines that its L2 does not hold, 25 to 50 GB/s whether 64 or 128 KB of loads are in flight, so
+// the weight's bytes and all 256 CUs streaming them.  16 experts of 128 rows on average, 2 x 2048 x 7168: 225 us for 0.94 GB of weights
+// (the loads alone 210, reads and products without loads 169); K in four slices for 256 rows of 2 x 2048 x 7168, 25 us, of which
+// 13 are the walk, 8 its sums to memory and 4 the start.
 #pragma once
 
 #include "nt_rows.h"
@@ -33,9 +38,10 @@ __device__ __forceinline__ void slot_barrier() {
 
 // 64 lanes x 16 bytes to LDS from `lds` on (the same in all lanes), lane l's behind lane l - 1's, from byte `offset` of the buffer.
 // Not said to touch memory, so that reads of other slots may move past it: what orders it is slot_barrier.
-// (m0 is reserved: nothing else in these kernels holds a value in it.)
+// (m0 is reserved: nothing else in these kernels holds a value in it.  The wait is what a load needs behind a vector instruction that
+// wrote its descriptor, which the compiler does not see to inside asm.)
 __device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t lds, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(lds), "v"(offset), "s"(rsrc));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(lds), "v"(offset), "s"(rsrc));
 }
 
 // The buffer resource as its four words (address, no stride, extent, raw).
@@ -137,8 +143,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
 
         // (the loads counted below are the ring's alone; its slots are free)
         slot_barrier<0>();
-        // Round r of the walk over K, which starts elsewhere for the next block of columns: rows that lie a multiple of some KB apart
-        // otherwise meet in a few of L2's channels, as all workgroups are at about the same k (rounds past the last: nothing).
+        // round r of the walk over K, which may start elsewhere for the next block of columns (rotation); past the last: nothing
         const int start = static_cast<int>(unsigned(it.nb) * unsigned(p.rot) % unsigned(max(steps, 1)));
         auto step_of = [&](int r) { return r >= steps ? all_steps : first_step + (r + start < steps ? r + start : r + start - steps); };
         // M of the wave's MT tiles of x; CUT: K ends within a chunk
@@ -187,12 +192,11 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
                 slot = next;
             }
         };
-        constexpr int U = 1;
         constexpr std::integral_constant<bool, false> whole;
         if (p.K & 7) run(std::integral_constant<int, MT>{}, std::integral_constant<bool, true>{});
-        else if (MT <= U || it.mrows <= 16 * WM * U) run(std::integral_constant<int, U>{}, whole);
-        else if (MT <= 2 * U || it.mrows <= 32 * WM * U) run(std::integral_constant<int, MT < 2 * U ? MT : 2 * U>{}, whole);
-        else if (MT <= 3 * U || it.mrows <= 48 * WM * U) run(std::integral_constant<int, MT < 3 * U ? MT : 3 * U>{}, whole);
+        else if (MT == 1 || it.mrows <= 16 * WM) run(std::integral_constant<int, 1>{}, whole);
+        else if (MT == 2 || it.mrows <= 32 * WM) run(std::integral_constant<int, MT < 2 ? MT : 2>{}, whole);
+        else if (MT == 3 || it.mrows <= 48 * WM) run(std::integral_constant<int, MT < 3 ? MT : 3>{}, whole);
         else run(std::integral_constant<int, MT>{}, whole);
 
         // the sums through the ring's LDS, [m][row of the weight], so that rows of the result are written whole
@@ -233,7 +237,8 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
     slot_barrier<0>();       // the ring's last loads into LDS have landed
 }
 
-// The slices of K added in order, and what follows: four columns of a row a thread.
+// The slices of K added in order, and what follows: four columns of a row a thread.  (A launch of its own, 5.2 us for four slices of 256 x
+// 4096 sums: with the last workgroup of a tile adding them, handed over in the launch, the call took 40 us instead of 33.)
 constexpr int kFinishThreads = 256;
 template <int DT>
 __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const RowsParams p) {
