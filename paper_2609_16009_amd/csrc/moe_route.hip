@@ -3,12 +3,16 @@
 // LPT lanes take a token, lane l of them the experts l PER .. l PER + PER - 1, all in fp64: which expert comes before which may
 // not depend on how a score was rounded.  Choosing is top_k rounds of a maximum over 64-bit keys that order as the values do
 // (upper halves, then lower ones among their equals, then the lowest index), 0 for what has been chosen or lies in a closed
-// group.  A wave a token (LPT 64) has the shorter chain for few tokens, four tokens a wave share every step's instructions.
+// group.  A wave a token (LPT 64) has the shorter chain, four tokens a wave share every step's instructions.
 //
 // The pairs are sorted by counting: a wave walks its stretch of pairs, 64 at a time, and learns from one ballot per bit of the
 // expert's number which lanes hold the same one, so that a pair's place is its expert's next place plus its rank among them.
 // Up to kOneLaunch pairs the last workgroup to finish its tokens does it (handoff.h), with more a second launch, to which
 // each workgroup of the first leaves the counts of its tokens.
+//
+// What bounds it: for few tokens the chain of dependent steps, top_k maxima over a wave among them (one token, 8 of 256 experts
+// in groups, 6.5 us; 64 tokens 11.1 with the hand-over); for many the maxima's instructions (32767 tokens, 6 of 60 experts: 13 us of 22.5)
+// and the places, of which each workgroup first adds up what all of those before it counted (9).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -23,9 +27,12 @@ namespace nmm {
 namespace {
 
 constexpr int kRouteWaves = 8, kRouteThreads = 64 * kRouteWaves;
-constexpr int64_t kOneLaunch = 1024;  // pairs
+// Pairs ordered in the first launch (1020 pairs of 60 experts 7.7 us, 9.8 in two launches; 1024 of 256 12.0 and 12.9), while they fit LDS.
+constexpr int64_t kOneLaunch = 1024;
+constexpr int64_t kSharedWaves = 2048;  // tokens from which four share a wave
 constexpr int64_t kPiece = 4096;      // pairs of a segment ordered at a time
-// Workgroups of the first launch: each of the second reads the counts of all of them.
+// Workgroups of the first launch: each of the second reads the counts of all of them (32767 tokens of 60 experts 22.3 us with 512, 23.5 with
+// 256, 35 with 128; 8192 of 256 experts 34.5, 32.9, 53).
 constexpr int64_t max_segments(int64_t experts) { return experts <= 64 ? 512 : 256; }
 constexpr int kMaxRouted = 1024;      // experts
 constexpr int kFewPairs = kRouteWaves * 32;
@@ -580,7 +587,9 @@ nmm_status plan_route(const nmm_moe_router& a, RoutePlan* q) {
         return NMM_ERR_SHAPE;
     *q = RoutePlan{};
     if (a.tokens * a.top_k > kOneLaunch) {
-        if (a.experts <= 128 && a.groups <= 16 && a.top_k <= 16) q->lanes = 16;
+        // (60 experts, 512 tokens 10.3 us by 16 lanes and 9.1 by 64, 2048 10.9 and 11.1, 32767 22.3 and 33.0; 128 experts, 512 tokens 13.3
+        // and 10.6, 8192 15.7 and 20.0.  More experts would be more than 8 of them a lane, more groups or choices more than its lanes.)
+        if (a.tokens >= kSharedWaves && a.experts <= 128 && a.groups <= 16 && a.top_k <= 16) q->lanes = 16;
         const int64_t whole = kRouteWaves * (64 / q->lanes);
         q->chunk = static_cast<int>(cdiv(cdiv(a.tokens, max_segments(a.experts)), whole) * whole);
         q->segments = static_cast<int>(cdiv(a.tokens, q->chunk));

@@ -21,25 +21,33 @@ constexpr int kCols = 128;                 // rows of the weight a tile of wide_
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Tiles of 16 rows of the weight.
+int64_t rows16(int64_t N, bool gated) { return cdiv(gated ? 2 * N : N, 16); }
+
 struct ActPlan {
     int rows = 0;                // of x a tile: 4, 8, 16, 32 (rows_kernel) or 64, 128 (wide_kernel)
     int ks = 1, slice_steps = 0; // slices of K, slots of each
     size_t ws_bytes = 0;
 };
 
-// Up to 32 rows of x the weight's rows are dealt to workgroups in 16s where that is one a CU at most, else in 32s (launch_nt).  More
-// rows take tiles of 64 or 128 rows of x and 128 of the weight, and K is cut into slices, an XCD's each, while that leaves
-// at most a workgroup per CU and four slots a slice: 256 rows x 7168 x 2 x 2048 75 us whole, 32 in four slices; 128 x 16384 x 7168
-// 60 in four slices, 80 whole.
+// Up to 32 rows of x, and more where the weight is small, go by rows_kernel: up to 256 workgroups of 32 rows of x and 16 of the weight
+// while K is at most 4096, up to 1024 while it is at most 2048 (launch_nt then takes 32 of the weight).  64 rows x 512 x 512 5.0 us, in a tile of
+// wide_kernel 9.2; 64 x 2048 x 2048 7.9 and 12.2, 256 x 2048 x 2048 13.0 and 15.4 to 20.6, 64 x 7168 x 2048 15.3 and 14.8, 64 x 4096 x
+// 4096 (512 workgroups) 20.2 and 15.4.
+// Else tiles of 64 or 128 rows of x and 128 of the weight: 64 where they number 64 at most, so that K still goes in four slices (256 rows
+// x 7168 x 1024 17.7 us against 20.5 in 128s; 100 x 16384 x 7168, 112 of them, 75.7 against 54.3).  K is cut into slices, an XCD's each, while
+// that leaves at most a workgroup per CU and four slots a slice: 256 rows x 7168 x 2 x 2048 75 us whole, 32 in four slices; 128 x
+// 16384 x 7168 60 in four slices, 80 whole.
 ActPlan plan_act(int64_t M, int64_t K, int64_t N, bool gated) {
     ActPlan q;
-    if (M <= 32) {
+    const int64_t few = cdiv(M, 32) * rows16(N, gated);
+    if (M <= 32 || (few <= kCus && K <= 4096) || (few <= 4 * kCus && K <= 2048)) {
         q.rows = M <= 4 ? 4 : M <= 8 ? 8 : M <= 16 ? 16 : 32;
         return q;
     }
-    const int64_t steps = cdiv(K, rows::kWideK);
-    q.rows = M <= 64 ? 64 : 128;
-    const int64_t tiles = cdiv(M, q.rows) * cdiv(N, gated ? kCols / 2 : kCols);
+    const int64_t steps = cdiv(K, rows::kWideK), blocks = cdiv(N, gated ? kCols / 2 : kCols);
+    q.rows = M <= 64 || cdiv(M, 64) * blocks <= kCus / 4 ? 64 : 128;
+    const int64_t tiles = cdiv(M, q.rows) * blocks;
     while (q.ks < 8 && tiles * q.ks * 2 <= kCus && steps >= q.ks * 8) q.ks *= 2;
     q.slice_steps = static_cast<int>(std::max<int64_t>(1, cdiv(steps, q.ks)));
     if (q.ks > 1) q.ws_bytes = size_t(kTicketBytes) + size_t(q.ks) * M * cdiv(N, 4) * 4 * (gated ? 2 : 1) * 4;
@@ -57,10 +65,9 @@ void launch_rows(RowsParams p, hipStream_t s) {
 template <int DT, int XR>
 void launch_nt(const RowsParams& p, hipStream_t s) {
     // 16 rows of the weight a workgroup, its four waves sharing K, while every one finds a CU of its own (gated, one row x 7168 x 2 x 2048
-    // 12.0 us against 14.4 in 32s; 32 x 4096 x 4096 13.9 and 15.7); else 32 rows and two waves, so that three workgroups share a
-    // CU (32 x 16384 x 7168 45.2 us against 58.8, one row x 7168 x 2 x 8192 37.8 against 37.2)
-    const int64_t rows16 = cdiv(p.gated ? 2 * int64_t(p.N) : p.N, 16);
-    if (rows16 <= kCus) launch_rows<DT, XR, 1, 4, 2>(p, s);
+    // 11.5 us against 16.9 in 32s; 8 x 4096 x 4096 9.9 and 12.0); else 32 rows and two waves, so that three workgroups share a
+    // CU (32 x 16384 x 7168 45.1 us against 58.5, 8 x 4096 x 5120 12.1 and 12.6, one row x 7168 x 8192 20.3 both)
+    if (cdiv(p.M, 4 * XR) * rows16(p.N, p.gated != 0) <= kCus) launch_rows<DT, XR, 1, 4, 2>(p, s);
     else launch_rows<DT, XR, 2, 2, 2>(p, s);
 }
 

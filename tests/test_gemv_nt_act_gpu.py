@@ -228,3 +228,71 @@ def test_binding_refuses():
             bad()
     with pytest.raises(nmm.NmmError, match="NMM_ERR_ARG"):
         act(x, Wt, y, act=9)
+
+
+# Tiles of 64 and of 128 rows: K past 4096, or weights of many rows.
+@pytest.mark.parametrize("K", [4097, 4104, 4160, 4223, 4224, 5000, 8192])
+@pytest.mark.parametrize("M,N", [(33, 1), (48, 70), (64, 128), (65, 129), (130, 200), (257, 63)])
+def test_integers_exact_in_tiles_of_64(M, N, K):
+    check(M + K, M, K, N, 1, False, torch.bfloat16, True, bias=True, residual=M % 2 == 0, pad=K % 2)
+    check(M + N, M, K, N, 0, True, torch.float16, True, residual=M % 2 == 1)
+
+
+@pytest.mark.parametrize("M,N,K", [(129, 2900, 2100), (200, 2177, 2056), (400, 5000, 1), (400, 5000, 65), (257, 8000, 130), (400, 4990, 192),
+                                   (1000, 1100, 300), (300, 4100, 2304)])
+def test_integers_exact_in_tiles_of_128(M, N, K):
+    check(M + K, M, K, N, 1, False, torch.bfloat16, True, bias=True, residual=True)
+    check(M + K, M, K, N // 2, 0, True, torch.float16, True, residual=True, pad=1)
+
+
+@pytest.mark.parametrize("M,N", [(70, 300), (129, 2900)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_every_activation_in_tiles(M, N, gated):
+    for act in range(5):
+        check(act, M, 4110 if M == 70 else 2060, N, act, gated, torch.float16 if act % 2 else torch.bfloat16, bias=True, residual=True)
+
+
+@pytest.mark.parametrize("M,K,N", [(70, 4200, 260), (300, 2300, 2100), (400, 64, 2501)])
+def test_tiles_in_place_on_streams_and_captured(M, K, N):
+    args, _ = make(M, M, K, N, True, torch.bfloat16, False, True, True)
+    call = lambda y, r, **kw: nmm.nmm_gemv_nt_act(args["x"], args["Wt"], y, K=K, act=2, gated=True, bias=args["bias"], residual=r, **kw)
+    ref = torch.zeros((M, N), dtype=torch.bfloat16, device="cuda")
+    call(ref, args["residual"])
+    y = args["residual"].clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    call(y, y, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(y, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(y, args["residual"])
+    for i in range(4):
+        args["x"].mul_(-1)
+        y.zero_()
+        graph.replay()
+        call(ref, args["residual"])
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref), i
+
+
+@pytest.mark.parametrize("M,N", [(100, 40), (400, 5000)])
+def test_a_value_that_is_not_finite_stays_in_its_row_of_a_tile(M, N):
+    K = 4300 if M == 100 else 140
+    args, _ = make(M, M, K, N, True, torch.bfloat16, False, False, False)
+    clean, y = (torch.zeros((M, N), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    nmm.nmm_gemv_nt_act(args["x"], args["Wt"], clean, K=K, act=2, gated=True)
+    args["x"][M // 2, 17] = float("nan")
+    args["Wt"][5, 3] = float("inf")
+    nmm.nmm_gemv_nt_act(args["x"], args["Wt"], y, K=K, act=2, gated=True)
+    keep = torch.ones_like(y, dtype=torch.bool)
+    keep[M // 2], keep[:, 5] = False, False
+    assert torch.equal(y[keep], clean[keep]) and torch.isnan(y[M // 2]).all()
+
+
+def test_no_products_in_tiles_leave_the_epilogue():
+    r = torch.randn((400, 5000), device="cuda").to(torch.float16)
+    x, Wt = torch.zeros((400, 8), dtype=torch.float16, device="cuda"), torch.zeros((5000, 8), dtype=torch.float16, device="cuda")
+    y = torch.zeros_like(r)
+    nmm.nmm_gemv_nt_act(x, Wt, y, K=0, residual=r)
+    assert torch.equal(y, r)

@@ -204,3 +204,25 @@ def test_binding_refuses():
             nmm.nmm_moe_route(logits, **kw)
     with pytest.raises(nmm.NmmError, match="NMM_ERR_SHAPE"):
         nmm.nmm_moe_route(logits, c, w, o, p, score=SOFTMAX, groups=3)
+
+
+@pytest.mark.parametrize("T,E,k,groups,top", [(2047, 64, 8, 1, 1), (2048, 64, 8, 1, 1), (2049, 60, 6, 1, 1), (2051, 1, 1, 1, 1), (2500, 5, 5, 1, 1),
+                                              (3001, 128, 16, 16, 8), (2100, 128, 17, 1, 1), (2300, 96, 8, 32, 16), (4096, 120, 4, 8, 2),
+                                              (2222, 129, 8, 1, 1), (2050, 33, 16, 1, 1), (70000, 17, 2, 1, 1)])
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_tokens_that_share_a_wave(T, E, k, groups, top, score):
+    kw = dict(groups=groups, top_groups=top, group_top=1 + T % 2) if groups > 1 else {}
+    check(T, T, E, k, score, bias=T % 3 == 0, mask=T % 2 == 0, renormalize=T % 3 == 1, scale=1.5, **kw)
+    check(T, T, E, k, score, dt=torch.bfloat16, pad=3, **kw)                  # ties among bf16 logits
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_values_that_are_not_finite_in_shared_waves(score):
+    rng = np.random.default_rng(3)
+    for E, k in ((16, 4), (100, 9)):
+        l = rng.standard_normal((2049, E))
+        l[rng.random(l.shape) < 0.1] = np.nan
+        l[1::2] = np.where(np.isnan(l[1::2]), np.inf, l[1::2])
+        l[2::3][rng.random(l[2::3].shape) < 0.2] = -np.inf
+        l[5], l[6], l[7] = np.nan, -np.inf, np.inf
+        check(0, 2049, E, k, score, logits=l, renormalize=True)
