@@ -267,3 +267,44 @@ def test_binding_refuses():
     for bad in (dict(first=1), dict(act=7), dict(offsets=c.route[2][:8])):
         with pytest.raises(nmm.NmmError):
             nmm.nmm_moe_experts(**{**base, **bad})
+
+
+# Experts of more than 2^19 weights take tiles of 128 rows from 41 rows on average, of 256 from 97.
+@TYPES
+@pytest.mark.parametrize("T,E,k", [(82, 2, 1), (130, 3, 2), (128, 2, 1), (195, 2, 1), (300, 2, 1), (700, 4, 2)])
+@pytest.mark.parametrize("hidden,inner", [(1032, 520), (1037, 531), (2048, 264), (264, 2048)])
+def test_integers_exact_in_wide_tiles_of_larger_experts(T, E, k, hidden, inner, dt):
+    Case(T, T, E, k, hidden, inner, dt, integer=True, residual=T % 3 == 0, pad=T % 2).check(1)
+
+
+@pytest.mark.parametrize("act", range(5))
+def test_every_activation_in_wide_tiles_of_larger_experts(act):
+    for T, E, dt in ((130, 2, torch.bfloat16), (260, 2, torch.float16)):
+        Case(T + act, T, E, 1, 1030, 528, dt, residual=act % 2 == 1).check(act)
+
+
+@pytest.mark.parametrize("T,k", [(15, 4), (16, 4), (17, 4), (40, 2), (64, 8)])
+def test_many_small_experts(T, k):
+    """Tiles of 64 for experts of a few rows, from 16 tokens on."""
+    for hidden, inner in ((520, 260), (521, 259)):
+        Case(T, T, 64, k, hidden, inner, integer=True, residual=T % 2 == 0).check(1)
+
+
+@pytest.mark.parametrize("T,E", [(130, 2), (300, 3)])
+def test_captured_wide_tiles_follow_the_choice(T, E):
+    rng = np.random.default_rng(T)
+    a = Case(T, T, E, 1, 1032, 520, residual=True)
+    a.run()
+    y = torch.full_like(a.out, 7.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.run(y=y)
+    for i in range(4):
+        a.chosen = rng.integers(-1 if i % 2 else 0, 1 + i % E, (T, 1)).astype(np.int32)         # padded tokens, experts without rows
+        for t, v in zip(a.route, (a.chosen, a.weights, *order(a.chosen, E))):
+            t.copy_(dev(v))
+        y.fill_(7.0)
+        graph.replay()
+        a.check()
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, y), i
