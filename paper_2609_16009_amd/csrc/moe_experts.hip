@@ -5,9 +5,9 @@
 // part is kept in 32 bits and added in order, so that results do not depend on which workgroup ends first (atomics would).  h is rounded
 // to the matrix cores' type, one rounding of half a step that an expert's second product cannot avoid.
 //
-// What bounds it: the chosen experts' weights, each read once.  Hidden 7168, inner 2048: one token's 8 experts (705 MB) 121 us in the
-// three launches, 64 tokens on 64 experts (5.6 GB) 942, 1024 tokens on the 16 of 64 experts that are here (1.4 GB, and 180 GFLOP)
-// 399; of these up 67, 581, 225, down 45, 328, 136.
+// What bounds it: the chosen experts' weights, each read once.  Hidden 7168, inner 2048: one token's 8 experts (705 MB) 119 us in the
+// three launches, 64 tokens on 64 experts (5.6 GB) 915 to 960, 1024 tokens on the 16 of 64 experts that are here (1.4 GB, and 180 GFLOP)
+// 382 to 399; of these up 67 to 69, 581 to 630, 226, down 45, 328 to 338, 132.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
