@@ -141,11 +141,12 @@ __device__ __forceinline__ void finish4(const RowsParams& p, int64_t row, int n,
 }
 
 // The tiles of TM rows of each expert here: starts[e] counts those of the experts before e.  offsets are not trusted: a
-// count is cut to [0, pairs], a first pair likewise.
+// count is cut to [0, pairs], a first pair likewise, and tiles in all to those that pairs in some order can fill.
 template <int TM, int THREADS>
 __device__ __forceinline__ void scan_tiles(const RowsParams& p, int* starts) {
     const int lane = threadIdx.x & 63;
     if (threadIdx.x < 64) {
+        const int most = p.M / TM + p.local;
         int carry = 0;
         if (lane == 0) starts[0] = 0;
         for (int e0 = 0; e0 < p.local; e0 += 64) {
@@ -160,8 +161,8 @@ __device__ __forceinline__ void scan_tiles(const RowsParams& p, int* starts) {
                 const int o = __shfl_up(c, d);
                 if (lane >= d) c += o;
             }
-            if (e < p.local) starts[e + 1] = carry + c;
-            carry += __shfl(c, 63);
+            if (e < p.local) starts[e + 1] = min(carry + c, most);      // (64 experts have less than 2^31 tiles)
+            carry = min(carry + __shfl(c, 63), most);
         }
     }
     __syncthreads();

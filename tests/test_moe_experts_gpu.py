@@ -308,3 +308,19 @@ def test_captured_wide_tiles_follow_the_choice(T, E):
         a.check()
         torch.cuda.synchronize()
         assert torch.equal(a.out, y), i
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 8, 8), (6, 8, 4), (14, 16, 4), (40, 64, 8), (64, 8, 4), (200, 2, 2)])
+def test_experts_that_all_claim_every_pair(T, E, k):
+    """Offsets of no choice: only so many tiles are walked as a choice can fill, and nothing is written beside y."""
+    a = Case(T, T, E, k, 88, 48, integer=True)
+    a.run(1)
+    right = a.out.clone()
+    a.route[2].copy_(dev(np.array([0, T * k] * E, dtype=np.int32)[:E + 1]))
+    whole = torch.full((T + 2, 93), 7.0, dtype=a.dt, device="cuda")
+    a.run(1, y=whole[1:-1])
+    torch.cuda.synchronize()
+    assert (whole[0] == 7).all() and (whole[-1] == 7).all() and (whole[:, 88:] == 7).all()
+    a.route[2].copy_(dev(order(a.chosen, E)[0]))
+    a.run(1)
+    assert torch.equal(a.out, right)
