@@ -146,10 +146,10 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
         // round r of the walk over K, which may start elsewhere for the next block of columns (rotation); past the last: nothing
         const int start = static_cast<int>(unsigned(it.nb) * unsigned(p.rot) % unsigned(max(steps, 1)));
         auto step_of = [&](int r) { return r >= steps ? all_steps : first_step + (r + start < steps ? r + start : r + start - steps); };
-        // M of the wave's MT tiles of x; CUT: K ends within a chunk
-        auto run = [&](auto mc, auto cutc) {
+        const int cut = p.K & 7 ? all_steps - 1 : all_steps;     // the step in which K ends within a chunk
+        // M of the wave's MT tiles of x
+        auto run = [&](auto mc) {
             constexpr int M = decltype(mc)::value;
-            constexpr bool CUT = decltype(cutc)::value;
             constexpr std::integral_constant<int, LW + (16 * WM * M + 63) / 64> n_loads;
             struct Half {
                 i32x4 w[NT], x[M];
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
                 for (int m = 0; m < M; ++m) f.x[m] = *reinterpret_cast<const i32x4*>(at + (xa ^ (64 * h)) + m * WM * kWideTile);
             };
             auto multiply = [&](Half& f, int step, int h) {
-                if constexpr (CUT) {      // clear what lies past K
+                if (step == cut) {      // clear what lies past K
                     const int left = p.K - (step * kWideK + 32 * h + 8 * g);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) f.w[t] = keep_first(f.w[t], left);
@@ -192,12 +192,10 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
                 slot = next;
             }
         };
-        constexpr std::integral_constant<bool, false> whole;
-        if (p.K & 7) run(std::integral_constant<int, MT>{}, std::integral_constant<bool, true>{});
-        else if (MT == 1 || it.mrows <= 16 * WM) run(std::integral_constant<int, 1>{}, whole);
-        else if (MT == 2 || it.mrows <= 32 * WM) run(std::integral_constant<int, MT < 2 ? MT : 2>{}, whole);
-        else if (MT == 3 || it.mrows <= 48 * WM) run(std::integral_constant<int, MT < 3 ? MT : 3>{}, whole);
-        else run(std::integral_constant<int, MT>{}, whole);
+        if (MT == 1 || it.mrows <= 16 * WM) run(std::integral_constant<int, 1>{});
+        else if (MT == 2 || it.mrows <= 32 * WM) run(std::integral_constant<int, MT < 2 ? MT : 2>{});
+        else if (MT == 3 || it.mrows <= 48 * WM) run(std::integral_constant<int, MT < 3 ? MT : 3>{});
+        else run(std::integral_constant<int, MT>{});
 
         // the sums through the ring's LDS, [m][row of the weight], so that rows of the result are written whole
         slot_barrier<0>();
