@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "moe_tiles.h"
 #include "nmm_internal.h"
 #include "nt_rows.h"
 #include "nt_wide.h"
@@ -129,32 +130,26 @@ void launch_wide(RowsParams p, int64_t pairs, hipStream_t s) {
     hipLaunchKernelGGL((rows::wide_kernel<DT, MODE, BM, BN, 3>), dim3(grid_of(p, pairs, BM)), dim3(rows::kWideThreads), 0, s, p);
 }
 
-// A token chooses an expert once, so few tokens say how many rows an expert has at most.  With more, tiles hold about twice
-// the rows that experts have on average, so that nearly all read their weights once: 16 experts of 7168 and 2048, 16 rows
-// each 249 us in tiles of 64 (257 of 128), 64 rows 293 in tiles of 128 (310 of 64), 128 rows 360 of 256 (393 of 128);
-// 64 experts of 8 rows 916 in tiles of 16 (930 of 64).
-// Small experts have shorter walks, whose starts and ends count: up to 1024 x 512 tiles of 64 whatever the rows (16 experts of 128 rows 35
-// us, 47 in 256s, of 512 rows 81 and 92), and many of them up to 2048 x 1024 from 16 tokens on rather than tiles of 16 (64 experts of 1024 x 512,
-// 8 rows 49 us and 68, 2 rows 45 and 59; of 2048 x 1024, 8 rows 158 and 169, 2 rows 138 both; 16 experts of 512 x 256, 16 rows 18.4 and
-// 15.3; 8 tokens on 64 of them 24 and 19).
 template <int DT, int MODE>
-void launch_rows(const RowsParams& p, int64_t tokens, int64_t pairs, int64_t experts, hipStream_t s) {
-    const int64_t expert = int64_t(p.K) * p.N;
-    const bool many_small = tokens >= 16 && expert <= int64_t(1) << 21 && expert >= (int64_t(1) << 23) / p.local;
-    if (tokens <= 4) launch_few<DT, MODE, 1>(p, pairs, s);
-    else if (tokens <= 8) launch_few<DT, MODE, 2>(p, pairs, s);
-    else if (!many_small && (tokens <= 16 || pairs <= 10 * experts)) launch_few<DT, MODE, 4>(p, pairs, s);
-    else if (expert <= int64_t(1) << 19 || pairs <= 40 * experts) launch_wide<DT, MODE, 64>(p, pairs, s);
-    else if (pairs <= 96 * experts) launch_wide<DT, MODE, 128>(p, pairs, s);
-    else launch_wide<DT, MODE, 256>(p, pairs, s);
+void launch_rows(const RowsParams& p, int tile_rows, int64_t pairs, hipStream_t s) {
+    switch (tile_rows) {
+        case 4: return launch_few<DT, MODE, 1>(p, pairs, s);
+        case 8: return launch_few<DT, MODE, 2>(p, pairs, s);
+        case 16: return launch_few<DT, MODE, 4>(p, pairs, s);
+        case 64: return launch_wide<DT, MODE, 64>(p, pairs, s);
+        case 128: return launch_wide<DT, MODE, 128>(p, pairs, s);
+        default: return launch_wide<DT, MODE, 256>(p, pairs, s);
+    }
 }
 
 template <int DT>
 void launch(const RowsParams& up, const RowsParams& down, const CombineParams& c, const nmm_moe_ffn& a, int64_t pairs,
             hipStream_t s) {
     if (a.local > 0) {
-        launch_rows<DT, rows::kUp>(up, a.tokens, pairs, a.experts, s);
-        launch_rows<DT, rows::kDown>(down, a.tokens, pairs, a.experts, s);
+        // (the first product's rows are addressed from x on, which is below 2^31 bytes)
+        launch_rows<DT, rows::kUp>(up, rows::tile_rows_of(up.K, up.N, a.tokens, pairs, a.experts, a.local), pairs, s);
+        launch_rows<DT, rows::kDown>(
+            down, rows::tile_rows_in_reach(down.K, down.N, a.tokens, pairs, a.experts, a.local, down.ldx), pairs, s);
     }
     hipLaunchKernelGGL((combine_kernel<DT>), dim3(static_cast<uint32_t>(a.tokens * c.col_blocks)), dim3(kCombineThreads), 0, s, c);
 }

@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "bf16_cast.h"
+#include "moe_tiles.h"
 #include "nmm_internal.h"
 #include "nt_ring.h"
 
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
         uint32_t x_extent = p.x_extent;
         if constexpr (MODE != kUp) {
             xb += (int64_t(it.first) + it.m0) * p.ldx;
-            x_extent = uint32_t((int64_t(it.mrows - 1) * p.ldx + (p.K + 7) / 8 * 8) * 2);
+            x_extent = uint32_t(tile_bytes(it.mrows, p.ldx, p.K));
         }
         const __amdgpu_buffer_rsrc_t xr =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(xb), (short)0, (int)x_extent, kRsrcWord3);

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
         uint32_t x_extent = p.x_extent;
         if constexpr (MODE != kUp) {
             xb += (int64_t(it.first) + it.m0) * p.ldx;
-            x_extent = uint32_t((int64_t(it.mrows - 1) * p.ldx + (p.K + 7) / 8 * 8) * 2);
+            x_extent = uint32_t(tile_bytes(it.mrows, p.ldx, p.K));
         }
         const i32x4 xr = rsrc_words(xb, x_extent);
         uint32_t off[kLoads];      // byte offset of the lane's chunk in slot 0; out of range where there is none
