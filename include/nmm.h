@@ -693,7 +693,7 @@ size_t nmm_moe_route_workspace_size(const nmm_moe_router* router);
  * up to 256 of its rows, those of an expert that nobody chose not at all.
  *   tokens, top_k, experts, first, local   tokens * top_k < 2^26, top_k 1 .. 32, experts 1 .. 1024,
  *                first >= 0, local >= 0, first + local <= experts.
- *   hidden, inner   > 0 (the sizes of x[t] and h[t,i]).
+ *   hidden, inner   > 0 (the sizes of x[t] and h[t,i]) and below 2^29; every leading dimension below 2^31.
  *   x, ldx       [tokens, ldx] of type dt, 16-byte aligned, ldx >= hidden and a multiple of 8; below 2^31 bytes in all.
  *   W1, ldw1, stride1   [local][2 inner, ldw1]: gate rows, then up rows; 16-byte aligned, ldw1 >= hidden, both multiples of 8.
  *   W2, ldw2, stride2   [local][hidden, ldw2], likewise, ldw2 >= inner.  The matrices of one expert below 2^31 bytes each; strides

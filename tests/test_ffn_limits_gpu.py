@@ -51,3 +51,30 @@ def test_rows_of_h_that_add_up_to_gigabytes(T, inner):
     h = (x @ gate.T).clamp(min=0) * (x @ up.T)
     want = (residual.double().cpu() + h @ down.T).to(torch.bfloat16)
     assert torch.equal(y.cpu(), want)
+
+
+@pytest.mark.parametrize("T,top_k,hidden", [((1 << 24) + 77, 1, 8), ((1 << 23) + 5, 2, 17)])
+def test_tokens_past_a_launch_of_the_sums(T, top_k, hidden):
+    """More blocks than a launch of the sums has: each token's are there, and nothing beside them."""
+    inner, up8 = 8, (hidden + 7) // 8 * 8
+    g = torch.Generator(device="cuda").manual_seed(top_k)
+    w1, w2 = integers(g, 2, 2 * inner, up8), integers(g, 2, hidden, inner)
+    x = integers(g, T, up8)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    chosen = torch.randint(0, 2, (T, 1), generator=g, **i32) if top_k == 1 else torch.randint(0, 2, (T, 1), generator=g, **i32) ^ torch.arange(2, **i32)
+    flat = chosen.reshape(-1)
+    offsets = torch.zeros(3, **i32)
+    offsets[1:] = torch.cumsum(torch.bincount(flat, minlength=2), 0)
+    pairs = torch.sort(flat, stable=True)[1].to(torch.int32)
+    weights = torch.tensor([0.5, 2.0], device="cuda")[torch.randint(0, 2, (T, top_k), generator=g, device="cuda")]
+    residual = integers(g, T, hidden)
+    whole = torch.full((T + 2, hidden), 7.0, dtype=torch.bfloat16, device="cuda")
+    nmm.nmm_moe_experts(x, w1, w2, chosen, weights, offsets, pairs, whole[1:-1], act=nmm.NMM_ACT_NONE, hidden=hidden, residual=residual)
+    assert (whole[0] == 7).all() and (whole[-1] == 7).all()
+    # integers of 2^20 at most: fp32 holds every sum
+    want = residual.float()
+    for e in range(2):
+        z = x[:, :hidden].float() @ w1[e, :, :hidden].float().T
+        h = (z[:, :inner] * z[:, inner:]).to(torch.bfloat16).float()
+        want += (h @ w2[e].float().T) * torch.where(chosen == e, weights, 0.0).sum(1, keepdim=True)
+    assert torch.equal(whole[1:-1], want.to(torch.bfloat16))
