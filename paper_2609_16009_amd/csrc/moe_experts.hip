@@ -133,12 +133,12 @@ void launch_few(RowsParams p, int64_t pairs, hipStream_t s) {
     if constexpr (MODE == rows::kUp && XR <= 2) {
         if (p.K >= 4 * 8 * kMfmaNtGroup) {
             p.n_blocks = static_cast<int>(cdiv(p.N, 8));
-            hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, 1, 4, 2>), dim3(grid_of(p, pairs, 4 * XR)), dim3(256), 0, s, p);
+            hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, 1, 4>), dim3(grid_of(p, pairs, 4 * XR)), dim3(256), 0, s, p);
             return;
         }
     }
     p.n_blocks = static_cast<int>(cdiv(p.N, MODE == rows::kUp ? 16 : 32));
-    hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, 2, 2, 2>), dim3(grid_of(p, pairs, 4 * XR)), dim3(128), 0, s, p);
+    hipLaunchKernelGGL((rows::rows_kernel<DT, MODE, XR, 2, 2>), dim3(grid_of(p, pairs, 4 * XR)), dim3(128), 0, s, p);
 }
 
 template <int DT, int MODE, int BM>

@@ -54,12 +54,12 @@ ActPlan plan_act(int64_t M, int64_t K, int64_t N, bool gated) {
     return q;
 }
 
-template <int DT, int XR, int NT, int NW, int D>
+template <int DT, int XR, int NT, int NW>
 void launch_rows(RowsParams p, hipStream_t s) {
     p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? 8 * NT : 16 * NT));
     const int64_t items = cdiv(p.n_blocks, 8) * 8 * cdiv(p.M, 4 * XR);
     const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(64 * NW);
-    hipLaunchKernelGGL((rows::rows_kernel<DT, rows::kDense, XR, NT, NW, D>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((rows::rows_kernel<DT, rows::kDense, XR, NT, NW>), grid, block, 0, s, p);
 }
 
 template <int DT, int XR>
@@ -67,8 +67,8 @@ void launch_nt(const RowsParams& p, hipStream_t s) {
     // 16 rows of the weight a workgroup, its four waves sharing K, while every one finds a CU of its own (gated, one row x 7168 x 2 x 2048
     // 11.5 us against 16.9 in 32s; 8 x 4096 x 4096 9.9 and 12.0); else 32 rows and two waves, so that three workgroups share a
     // CU (32 x 16384 x 7168 45.1 us against 58.5, 8 x 4096 x 5120 12.1 and 12.6, one row x 7168 x 8192 20.3 both)
-    if (cdiv(p.M, 4 * XR) * rows16(p.N, p.gated != 0) <= kCus) launch_rows<DT, XR, 1, 4, 2>(p, s);
-    else launch_rows<DT, XR, 2, 2, 2>(p, s);
+    if (cdiv(p.M, 4 * XR) * rows16(p.N, p.gated != 0) <= kCus) launch_rows<DT, XR, 1, 4>(p, s);
+    else launch_rows<DT, XR, 2, 2>(p, s);
 }
 
 template <int DT, int BM>

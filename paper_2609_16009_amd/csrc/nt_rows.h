@@ -224,8 +224,9 @@ __device__ __forceinline__ bool item_of(const RowsParams& p, const int* starts, 
 // What bounds it: the weight's bytes, read once.  32 rows x 16384 x 7168 45 us (5.2 TB/s), eight experts' W1 of 2 x 2048 x 7168 for one
 // token 67 (7.0 TB/s), 64 experts' for 64 tokens 581 (6.5 TB/s), where a copy moves 5.0; a weight of 59 MB 12 us, of which 2 are a launch
 // and 2 the first loads.
-template <int DT, int MODE, int XR, int NT, int NW, int D>
+template <int DT, int MODE, int XR, int NT, int NW>
 __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
+    constexpr int D = 2;                             // groups of a ring
     constexpr int TM = 4 * XR;
     constexpr int MT = XR > 4 ? 2 : 1;               // 16-row tiles of x
     constexpr int kLoads = 4 * NT + XR;              // loads of a group per wave
@@ -354,9 +355,6 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
         for (int r = 0; r < rounds; r += D) {
             consume(std::integral_constant<int, 0>{}, r);
             if (r + 1 < rounds) consume(std::integral_constant<int, 1>{}, r + 1);
-            if constexpr (D > 2) {
-                if (r + 2 < rounds) consume(std::integral_constant<int, 2>{}, r + 2);
-            }
         }
 
         // the waves' sums through LDS: lane (g, j) holds n = 4 g + i, m = j of each tile

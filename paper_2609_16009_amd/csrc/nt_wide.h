@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
     constexpr int MT = BM / WM / 16;
     constexpr int LW = BN / 64, kLoads = LW + BM / 64;                   // loads of a slot per wave, the weight's first
     constexpr int kSlot = (BM + BN) * kWideRow;
-    static_assert(MT * WM * 16 == BM && NT * WN * 16 == BN && NT % 2 == 0 && S >= 3, "whole tiles, gate and up");
+    static_assert((MT == 2 || MT == 4) && MT * WM * 16 == BM && NT * WN * 16 == BN && NT % 2 == 0 && S >= 3, "whole tiles, gate and up");
     constexpr int kPitch = BN + 4;                                       // floats of a row of sums
     static_assert(BM * kPitch * 4 <= S * kSlot, "the sums fit the ring");
     __shared__ __attribute__((aligned(256))) uint8_t ring[S * kSlot];
@@ -192,9 +192,9 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
                 slot = next;
             }
         };
-        if (MT == 1 || it.mrows <= 16 * WM) run(std::integral_constant<int, 1>{});
-        else if (MT == 2 || it.mrows <= 32 * WM) run(std::integral_constant<int, MT < 2 ? MT : 2>{});
-        else if (MT == 3 || it.mrows <= 48 * WM) run(std::integral_constant<int, MT < 3 ? MT : 3>{});
+        if (it.mrows <= 16 * WM) run(std::integral_constant<int, 1>{});
+        else if (MT == 2 || it.mrows <= 32 * WM) run(std::integral_constant<int, 2>{});
+        else if (it.mrows <= 48 * WM) run(std::integral_constant<int, MT - 1>{});
         else run(std::integral_constant<int, MT>{});
 
         // the sums through the ring's LDS, [m][row of the weight], so that rows of the result are written whole
