@@ -38,5 +38,42 @@ constexpr int tile_rows_in_reach(int64_t K, int64_t N, int64_t tokens, int64_t p
     return rows;
 }
 
+// The walk over the items of a launch: an item is a tile of an expert's rows and a block of columns.  offsets are not trusted: they
+// are cut to [0, pairs], a count below zero is none, and tiles in all are cut to those that pairs in some order can fill.
+constexpr int cut_offset(int offset, int pairs) {
+    const int o = offset > 0 ? offset : 0;
+    return o < pairs ? o : pairs;
+}
+constexpr int tiles_of(int first, int end, int tile) { return end > first ? int(unsigned(end - first + tile - 1) / unsigned(tile)) : 0; }
+constexpr int most_tiles(int pairs, int tile, int local) { return pairs / tile + local; }
+
+// The expert whose tile is the u-th: starts[e] <= u < starts[e + 1], u < starts[local].
+constexpr int expert_of(const int* starts, int local, int u) {
+    int lo = 0, hi = local;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (starts[mid] <= u) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Blocks of columns that an XCD takes: every eighth, or where K is cut into 2, 4 or 8 slices every fourth, second or all of them
+// in one slice (xcd % ks).
+constexpr int64_t blocks_of_xcd(int n_blocks, int ks) {
+    const int share = 8 / ks;
+    return (int64_t(n_blocks) + share - 1) / share;
+}
+
+// Item `rem` of an XCD's items of an expert that has `tiles` tiles: the row tiles over the same weight rows follow each other, so
+// the second one finds them in the XCD's L2.
+struct Place {
+    int nb, m0;
+};
+constexpr Place place_of(int64_t rem, int tiles, int tile, int ks, int xcd) {
+    const int nbi = static_cast<int>(rem / tiles);
+    return {8 / ks * nbi + xcd / ks, static_cast<int>(rem - int64_t(nbi) * tiles) * tile};
+}
+
 }  // namespace rows
 }  // namespace nmm

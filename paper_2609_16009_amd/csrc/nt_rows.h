@@ -141,22 +141,18 @@ __device__ __forceinline__ void finish4(const RowsParams& p, int64_t row, int n,
     store4<DT>(p.y + row * p.ldy, n, p.N, v);
 }
 
-// The tiles of TM rows of each expert here: starts[e] counts those of the experts before e.  offsets are not trusted: a
-// count is cut to [0, pairs], a first pair likewise, and tiles in all to those that pairs in some order can fill.
+// The tiles of TM rows of each expert here: starts[e] counts those of the experts before e.
 template <int TM, int THREADS>
 __device__ __forceinline__ void scan_tiles(const RowsParams& p, int* starts) {
     const int lane = threadIdx.x & 63;
     if (threadIdx.x < 64) {
-        const int most = p.M / TM + p.local;
+        const int most = most_tiles(p.M, TM, p.local);
         int carry = 0;
         if (lane == 0) starts[0] = 0;
         for (int e0 = 0; e0 < p.local; e0 += 64) {
             const int e = e0 + lane;
             int c = 0;
-            if (e < p.local) {
-                const int a = min(max(p.offsets[e], 0), p.M), b = min(max(p.offsets[e + 1], 0), p.M);
-                c = b > a ? (b - a + TM - 1) / TM : 0;
-            }
+            if (e < p.local) c = tiles_of(cut_offset(p.offsets[e], p.M), cut_offset(p.offsets[e + 1], p.M), TM);
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
                 const int o = __shfl_up(c, d);
@@ -174,46 +170,33 @@ struct Item {
     int e, first, m0, mrows, nb;      // first: the expert's first pair in the order by experts
 };
 
-// Blocks of columns that an XCD takes: every eighth, or where K is cut into 2, 4 or 8 slices every fourth, second or all of them
-// in one slice (xcd % ks).
-__device__ __forceinline__ int64_t blocks_of(const RowsParams& p) {
-    const int share = 8 / p.ks;
-    return (int64_t(p.n_blocks) + share - 1) / share;
-}
+__device__ __forceinline__ int64_t blocks_of(const RowsParams& p) { return blocks_of_xcd(p.n_blocks, p.ks); }
 
 // Item idx of this XCD (false: none): its blocks of columns of all experts, so that each XCD has the same share of every
 // expert's rows.  (An eighth of the experts each reads x into one L2 instead of eight, 0.95 instead of 1.12 GB for 16 experts of 128 rows on
-// average, but the XCD with the fullest ones ends last: 253 instead of 228 us.)  The row tiles over the same weight rows
-// follow each other, so the second one finds them in the XCD's L2.
+// average, but the XCD with the fullest ones ends last: 253 instead of 228 us.)
 template <int MODE, int TM>
 __device__ __forceinline__ bool item_of(const RowsParams& p, const int* starts, int64_t idx, int xcd, Item* it) {
-    const int64_t nb8 = blocks_of(p);
-    int lo = 0, tiles;
+    int tiles, count;
     int64_t rem = idx;
+    it->e = 0;
+    it->first = 0;
     if constexpr (MODE == kDense) {
         tiles = static_cast<int>((int64_t(p.M) + TM - 1) / TM);
-        it->e = 0;
-        it->first = 0;
+        count = p.M;
     } else {
-        const int u = static_cast<int>(idx / nb8);
-        int hi = p.local;                       // starts[lo] <= u < starts[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (starts[mid] <= u) lo = mid;
-            else hi = mid;
-        }
-        lo = __builtin_amdgcn_readfirstlane(lo);
-        const int s = __builtin_amdgcn_readfirstlane(starts[lo]);
-        tiles = __builtin_amdgcn_readfirstlane(starts[lo + 1]) - s;
+        const int64_t nb8 = blocks_of(p);
+        const int e = __builtin_amdgcn_readfirstlane(expert_of(starts, p.local, static_cast<int>(idx / nb8)));
+        const int s = __builtin_amdgcn_readfirstlane(starts[e]);
+        tiles = __builtin_amdgcn_readfirstlane(starts[e + 1]) - s;
         rem = idx - s * nb8;
-        it->e = lo;
-        it->first = __builtin_amdgcn_readfirstlane(min(max(p.offsets[lo], 0), p.M));
+        it->e = e;
+        it->first = __builtin_amdgcn_readfirstlane(cut_offset(p.offsets[e], p.M));
+        count = __builtin_amdgcn_readfirstlane(cut_offset(p.offsets[e + 1], p.M)) - it->first;
     }
-    const int nbi = static_cast<int>(rem / tiles);
-    it->nb = 8 / p.ks * nbi + xcd / p.ks;
-    it->m0 = static_cast<int>(rem - int64_t(nbi) * tiles) * TM;
-    const int count =
-        MODE == kDense ? p.M : __builtin_amdgcn_readfirstlane(min(max(p.offsets[lo + 1], 0), p.M)) - it->first;
+    const Place at = place_of(rem, tiles, TM, p.ks, xcd);
+    it->nb = at.nb;
+    it->m0 = at.m0;
     it->mrows = min(TM, count - it->m0);
     return it->nb < p.n_blocks;
 }
