@@ -3,7 +3,10 @@
 //   down     part[p] = h[s] W2^T, p = pairs[s]              fp32
 //   combine  y[t] = dt(residual[t] + sum_i weights[t,i] part[t top_k + i])      in the order of i
 // part is kept in 32 bits and added in order, so that results do not depend on which workgroup ends first (atomics would).  h is rounded
-// to the matrix cores' type, one rounding of half a step that an expert's second product cannot avoid.
+// to 16 bits, by choice: two words of them would keep its 32-bit value, at twice the bytes of h, LDS for it and reads of its fragments, and
+// twice the matrix instructions, where wide tiles take as long to read fragments as to multiply them and 256 rows leave no LDS.  The
+// rounding is half a step of each h, so y is off by at most about what its own rounding may be (bf16, no residual, 2.1e-3 to 2.4e-3 of y
+// in the 2-norm against 1.6e-3 to 1.7e-3 with h in 32 bits; fp16 2.3e-4 to 3.0e-4 against 2.1e-4).
 //
 // What bounds it: the chosen experts' weights, each read once.  Hidden 7168, inner 2048: one token's 8 experts (705 MB) 119 us in the
 // three launches, 64 tokens on 64 experts (5.6 GB) 915 to 960, 1024 tokens on the 16 of 64 experts that are here (1.4 GB, and 180 GFLOP)
@@ -125,9 +128,9 @@ uint32_t grid_of(const RowsParams& p, int64_t pairs, int64_t rows) {
     return static_cast<uint32_t>(std::min<int64_t>(cdiv(p.n_blocks, 8) * 8 * tiles, kGridMost));
 }
 
-// 32 rows of the weight and two waves a workgroup, of which three share a CU: the eight experts of one token, W2 44.9 us (52.2 with four
-// waves, whose workgroups have a CU each).  Up to 8 rows of x and a K of eight groups for each of four waves W1 goes by 16 rows,
-// a gate's 8 and the 8 that it multiplies: 67.4 us of one token (73.0 in 32s), 41 of four experts of 4096 x 4096 (58); at 16 rows of x 439 and 432.
+// 32 rows of the weight and two waves a workgroup, of which three share a CU up to 8 rows of x (45 to 49 KB of LDS) and two at 16 (57 KB): the
+// eight experts of one token, W2 44.9 us (52.2 with four waves, whose workgroups have a CU each).  Up to 8 rows of x and a K of eight groups
+// for each of four waves W1 goes by 16 rows, a gate's 8 and the 8 that it multiplies: 67.4 us of one token (73.0 in 32s), 41 of four experts of 4096 x 4096 (58); at 16 rows of x 439 and 432.
 template <int DT, int MODE, int XR>
 void launch_few(RowsParams p, int64_t pairs, hipStream_t s) {
     if constexpr (MODE == rows::kUp && XR <= 2) {

@@ -65,8 +65,9 @@ void launch_rows(RowsParams p, hipStream_t s) {
 template <int DT, int XR>
 void launch_nt(const RowsParams& p, hipStream_t s) {
     // 16 rows of the weight a workgroup, its four waves sharing K, while every one finds a CU of its own (gated, one row x 7168 x 2 x 2048
-    // 11.5 us against 16.9 in 32s; 8 x 4096 x 4096 9.9 and 12.0); else 32 rows and two waves, so that three workgroups share a
-    // CU (32 x 16384 x 7168 45.1 us against 58.5, 8 x 4096 x 5120 12.1 and 12.6, one row x 7168 x 8192 20.3 both)
+    // 11.5 us against 16.9 in 32s; 8 x 4096 x 4096 9.9 and 12.0); else 32 rows and two waves, of which three workgroups share a CU up to 16
+    // rows of x (41 to 53 KB of LDS) and two at 32 (74 KB), where 16s have a CU each at 32 rows (32 x 16384 x 7168 45.1 us
+    // against 58.5, 8 x 4096 x 5120 12.1 and 12.6, one row x 7168 x 8192 20.3 both)
     if (cdiv(p.M, 4 * XR) * rows16(p.N, p.gated != 0) <= kCus) launch_rows<DT, XR, 1, 4>(p, s);
     else launch_rows<DT, XR, 2, 2>(p, s);
 }

@@ -55,7 +55,8 @@ struct RowsParams {
 
 // Rows of the weight a multiple of 4 KB apart meet in few of the memory's channels, as all workgroups are at about the same k:
 // there the next block of columns starts its walk over K a round later (16 experts of 2048 x 7168, 16 rows each: 114 -> 94 us; 32 x
-// 16384 x 7168: 48 -> 45).  Elsewhere it only takes from L2 what workgroups at the same k share (7168 x 2 x 2048: 250 -> 259 us).
+// 16384 x 7168: 48 -> 45; 128 rows each 138 -> 131.5, though each L2 then reads h about four times, 0.73 instead of 0.55 GB in all: an expert's
+// workgroups are at different k, and W passes through L2 between them).  Elsewhere it only takes from L2 what workgroups at the same k share (7168 x 2 x 2048: 250 -> 259 us).
 inline int rotation(int64_t ld) { return ld * 2 % 4096 == 0 ? 1 : 0; }
 
 __device__ __forceinline__ float activate(float z, int act) {
@@ -203,7 +204,9 @@ __device__ __forceinline__ bool item_of(const RowsParams& p, const int* starts, 
 
 // Few rows of x a tile (4 XR): a workgroup owns 16 NT rows of the weight (gated: half of them the gate's, half those that they are
 // multiplied with) and all of K, which its NW waves share in groups of 128, as in mfma_nt_kernel: rings of D groups private to a
-// wave, no barrier in the loop.  Sums are fp32 in the matrix cores, two chains a wave, the waves' added in wave order.
+// wave, no barrier in the loop.  Sums are fp32 in the matrix cores, two chains a wave, the waves' added in wave order: relative 2-norm
+// error 2.7e-7 (16 rows of the weight, four waves) and 4.0e-7 (32, two) at K = 16384, where mfma_nt_kernel's sums in fp64 have 5e-8.  A y of 16
+// bits hides that; sums in fp64 would be eight vector instructions more for every two matrix instructions.
 // What bounds it: the weight's bytes, read once.  32 rows x 16384 x 7168 45 us (5.2 TB/s), eight experts' W1 of 2 x 2048 x 7168 for one
 // token 67 (7.0 TB/s), 64 experts' for 64 tokens 581 (6.5 TB/s), where a copy moves 5.0; a weight of 59 MB 12 us, of which 2 are a launch
 // and 2 the first loads.

@@ -14,8 +14,9 @@
 //
 // What bounds it: how fast a CU is given lines that its L2 does not hold, 25 to 50 GB/s whether 64 or 128 KB of loads are in flight, so
 // the weight's bytes and all 256 CUs streaming them.  16 experts of 128 rows on average, 2 x 2048 x 7168: 225 us for 0.94 GB of weights
-// (the loads alone 210, reads and products without loads 169); K in four slices for 256 rows of 2 x 2048 x 7168, 25 us, of which
-// 13 are the walk, 8 its sums to memory and 4 the start.
+// (the loads alone 210, reads and products without loads 169); K in four slices for 256 rows of 2 x 2048 x 7168, 21.4 us, of which
+// 13 to 14 are the walk over 28 slots (the slope over K), 2 to 3 its sums to memory (21.4 and 19.0 to 19.4 without their stores) and the rest the start
+// and the end.  Sums are fp32 in the matrix cores, one chain over K or a slice: relative 2-norm error 8.2e-7 at K = 16384 whole.
 #pragma once
 
 #include "nt_rows.h"
