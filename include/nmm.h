@@ -608,9 +608,9 @@ size_t nmm_latent_attention_batch_workspace_size(const nmm_latent_attn_batch* at
  *     y[m,n] = v[m,n] + residual[m,n]
  * Gated weights hold the gate's N rows, then the N rows of what it is multiplied with.  Products and everything
  * after them are fp32, y is rounded once (nearest, ties to even).  Any M (blocks of up to 128 rows, each reading Wt once).
- * A product is 1 to 8 fp32 sums over parts of K (fewer the larger M and N are), added in fp32; nmm_gemv_nt adds its matrix cores'
- * products in fp64.  What that costs is hidden by a y of 16 bits and shows in y_f32, relative 2-norm error of standard normal
- * operands against nmm_gemv_nt's 5e-8 (bf16) and 6e-8 (fp16) from 2 rows on: K = 512 6e-8 to 1.5e-7, 7168 1.8e-7 to 5.4e-7, 16384 2.7e-7 to 8.2e-7.
+ * A product is up to 8 fp32 sums over parts of K, added in fp32 (relative 2-norm error 6e-8 to 1.5e-7 at K = 512, up to 8.2e-7 at 16384), which
+ * a y of 16 bits hides.  Where y_f32 is asked for, sums over at most 128 of k go into fp64 as in nmm_gemv_nt (6e-8 to 9e-8 at
+ * any K; nmm_gemv_nt 5e-8 to 6e-8), for y as well, which may so differ in its last bit from a call without y_f32.
  *   act          none; relu: max(z, 0), NaN kept; silu: z / (1 + e^-z); gelu: z / 2 (1 + erf(z / sqrt 2)); gelu_tanh:
  *                z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
  *   x, ldx, Wt, ldwt   as for nmm_gemv_nt; the extent of Wt counts its N or 2 N rows.
@@ -691,7 +691,7 @@ size_t nmm_moe_route_workspace_size(const nmm_moe_router* router);
  * that this GPU holds (first 0 and local = experts: all of them).  With e = chosen[t,i] - first:
  *     h[t,i]  = dt(act(x[t] . W1[e, :inner]^T) * (x[t] . W1[e, inner:]^T))
  *     y[t]    = dt(residual[t] + sum_i weights[t,i] (h[t,i] . W2[e]^T))            over the i whose expert is here
- * Sums are fp32 (as nmm_gemv_nt_act's); h is rounded to dt and y once (nearest, ties to even).  That h has 16 bits is this
+ * Sums are fp32 (as nmm_gemv_nt_act's of a y of 16 bits); h is rounded to dt and y once (nearest, ties to even).  That h has 16 bits is this
  * operator's choice, for its speed.  It moves y by up to about as much as y's own rounding does (against 64 bits, relative
  * 2-norm error 1.7e-3 to 1.9e-3 in bf16 under a residual and 2.1e-3 to 2.4e-3 without one, where h in 32 bits gives 1.7e-3; fp16 2.1e-4 to 3.0e-4
  * and 2.1e-4), and in fp16 an h past 65504 is infinite.  The i of a token

@@ -59,7 +59,8 @@ void launch_rows(RowsParams p, hipStream_t s) {
     p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? 8 * NT : 16 * NT));
     const int64_t items = cdiv(p.n_blocks, 8) * 8 * cdiv(p.M, 4 * XR);
     const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(64 * NW);
-    hipLaunchKernelGGL((rows::rows_kernel<DT, rows::kDense, XR, NT, NW>), grid, block, 0, s, p);
+    if (p.yf) hipLaunchKernelGGL((rows::rows_kernel<DT, rows::kDense, XR, NT, NW, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((rows::rows_kernel<DT, rows::kDense, XR, NT, NW>), grid, block, 0, s, p);
 }
 
 template <int DT, int XR>
@@ -77,7 +78,8 @@ void launch_wide(RowsParams p, hipStream_t s) {
     p.n_blocks = static_cast<int>(cdiv(p.N, p.gated ? kCols / 2 : kCols));
     const int64_t items = cdiv(p.n_blocks, 8 / p.ks) * 8 * cdiv(p.M, BM);
     const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(items, kGridMost))), block(rows::kWideThreads);
-    hipLaunchKernelGGL((rows::wide_kernel<DT, rows::kDense, BM, kCols, 3>), grid, block, 0, s, p);
+    if (p.yf) hipLaunchKernelGGL((rows::wide_kernel<DT, rows::kDense, BM, kCols, 3, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((rows::wide_kernel<DT, rows::kDense, BM, kCols, 3>), grid, block, 0, s, p);
     if (p.ks == 1) return;
     const dim3 all(static_cast<uint32_t>(cdiv(p.M * cdiv(p.N, 4), rows::kFinishThreads)));
     hipLaunchKernelGGL((rows::finish_kernel<DT>), all, dim3(rows::kFinishThreads), 0, s, p);

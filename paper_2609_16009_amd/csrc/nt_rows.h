@@ -202,15 +202,32 @@ __device__ __forceinline__ bool item_of(const RowsParams& p, const int* starts, 
     return it->nb < p.n_blocks;
 }
 
+// A lane's four values of a tile summed in fp64, where F64: what the matrix cores have added up in fp32 so far is taken into it.
+template <bool F64>
+struct Sum64 {
+    __device__ __forceinline__ f32x4 rounded(f32x4 sum) const { return sum; }
+};
+template <>
+struct Sum64<true> {
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    __device__ __forceinline__ void take(f32x4& sum) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += double(sum[i]);
+        sum = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ f32x4 rounded(f32x4) const { return f32x4{float(v[0]), float(v[1]), float(v[2]), float(v[3])}; }
+};
+
 // Few rows of x a tile (4 XR): a workgroup owns 16 NT rows of the weight (gated: half of them the gate's, half those that they are
 // multiplied with) and all of K, which its NW waves share in groups of 128, as in mfma_nt_kernel: rings of D groups private to a
 // wave, no barrier in the loop.  Sums are fp32 in the matrix cores, two chains a wave, the waves' added in wave order: relative 2-norm
-// error 2.7e-7 (16 rows of the weight, four waves) and 4.0e-7 (32, two) at K = 16384, where mfma_nt_kernel's sums in fp64 have 5e-8.  A y of 16
-// bits hides that; sums in fp64 would be eight vector instructions more for every two matrix instructions.
+// error 2.7e-7 (16 rows of the weight, four waves) and 4.0e-7 (32, two) at K = 16384.  A y of 16 bits hides that; where results are asked for in
+// fp32 (F64), a wave takes its sums of two matrix instructions each into fp64, as mfma_nt_kernel does: 5.6e-8 (fp16 7.0e-8), 32 rows x 16384 x
+// 7168 45.1 us instead of 43.5, the others as fast.
 // What bounds it: the weight's bytes, read once.  32 rows x 16384 x 7168 45 us (5.2 TB/s), eight experts' W1 of 2 x 2048 x 7168 for one
 // token 67 (7.0 TB/s), 64 experts' for 64 tokens 581 (6.5 TB/s), where a copy moves 5.0; a weight of 59 MB 12 us, of which 2 are a launch
 // and 2 the first loads.
-template <int DT, int MODE, int XR, int NT, int NW>
+template <int DT, int MODE, int XR, int NT, int NW, bool F64 = false>
 __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
     constexpr int D = 2;                             // groups of a ring
     constexpr int TM = 4 * XR;
@@ -298,6 +315,7 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
         for (int d = 0; d < D; ++d) load_group(group_of(d), ring + d * kSlot);
 
         f32x4 sum[NT][MT][2];
+        Sum64<F64> all[NT][MT];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -337,6 +355,15 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
             half(std::integral_constant<int, 0>{});
             half(std::integral_constant<int, 1>{});
             load_group(group_of(r + D), ring + kOff);
+            if constexpr (F64) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        all[t][mt].take(sum[t][mt][0]);
+                        all[t][mt].take(sum[t][mt][1]);
+                    }
+            }
         };
         for (int r = 0; r < rounds; r += D) {
             consume(std::integral_constant<int, 0>{}, r);
@@ -351,7 +378,7 @@ __global__ __launch_bounds__(64 * NW) void rows_kernel(const RowsParams p) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
                 *reinterpret_cast<f32x4*>(red + ((wave * NT + t) * MT + mt) * kTileFloats + j * kRedPitch + 4 * g) =
-                    sum[t][mt][0] + sum[t][mt][1];
+                    all[t][mt].rounded(sum[t][mt][0] + sum[t][mt][1]);
         __syncthreads();
         const int quads = n_step / 4;
         for (int o = tid; o < quads * it.mrows; o += 64 * NW) {

@@ -16,7 +16,9 @@
 // the weight's bytes and all 256 CUs streaming them.  16 experts of 128 rows on average, 2 x 2048 x 7168: 225 us for 0.94 GB of weights
 // (the loads alone 210, reads and products without loads 169); K in four slices for 256 rows of 2 x 2048 x 7168, 21.4 us, of which
 // 13 to 14 are the walk over 28 slots (the slope over K), 2 to 3 its sums to memory (21.4 and 19.0 to 19.4 without their stores) and the rest the start
-// and the end.  Sums are fp32 in the matrix cores, one chain over K or a slice: relative 2-norm error 8.2e-7 at K = 16384 whole.
+// and the end.  Sums are fp32 in the matrix cores, one chain over K or a slice: relative 2-norm error 8.2e-7 at K = 16384 whole.  Where results are
+// asked for in fp32 (F64), chains of four matrix instructions are taken into fp64 every other slot: 6.5e-8 to 7.7e-8 (fp16 9.1e-8) and 29.5 instead of 25.9 us
+// for 256 rows of 2 x 2048 x 7168, 76 instead of 63 for 1024 of 4096 x 7168 (every fourth slot: 9.8e-8, 1.2e-7, 28.1 and 71).
 #pragma once
 
 #include "nt_rows.h"
@@ -54,7 +56,7 @@ __device__ __forceinline__ i32x4 rsrc_words(const void* base, uint32_t extent) {
     return r;
 }
 
-template <int DT, int MODE, int BM, int BN, int S>
+template <int DT, int MODE, int BM, int BN, int S, bool F64 = false>
 __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) {
     constexpr int NT = BM >= 256 ? 4 : 2, WN = BN / 16 / NT, WM = kWideWaves / WN;   // a wave's tiles; waves along n and m
     constexpr int MT = BM / WM / 16;
@@ -137,6 +139,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
                 load_to_lds(i < LW ? wr : xr, to + 64 * i * kWideRow, (off[i] + uint32_t(kg) * 2u) | past);
         };
         f32x4 sum[NT][MT];
+        Sum64<F64> all[NT][MT];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -191,6 +194,14 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
                 read(a, next, 0);
                 multiply(b, step, 1);
                 slot = next;
+                if constexpr (F64) {
+                    if (r & 1 || r == steps - 1) {
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int m = 0; m < M; ++m) all[t][m].take(sum[t][m]);
+                    }
+                }
             }
         };
         if (it.mrows <= 16 * WM) run(std::integral_constant<int, 1>{});
@@ -205,7 +216,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const RowsParams p) 
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
-                *reinterpret_cast<f32x4*>(tile + ((wm + WM * m) * 16 + j) * kPitch + (wn * NT + t) * 16 + 4 * g) = sum[t][m];
+                *reinterpret_cast<f32x4*>(tile + ((wm + WM * m) * 16 + j) * kPitch + (wn * NT + t) * 16 + 4 * g) = all[t][m].rounded(sum[t][m]);
         slot_barrier<0>();
         constexpr int kWaveRows = BN / WN;
         const int quads = n_step / 4;
